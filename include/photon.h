@@ -131,6 +131,76 @@ PHOTON_API int32_t photon_coarse_decode_attn_static(const void* q, const void* k
                                          int32_t n_splits, photon_dtype dt, void* stream);
 
 /* --------------------------------------------------------------------------
+ * K/V cache in 4 bits (MXFP4, OCP microscaling formats): a variant of the
+ * coarsest stream's cache (Eq. 12-13) in 17 bytes per 32 elements.
+ *
+ * Format.  A block is 32 consecutive elements of a position's row of one head
+ * (the last block of a head size that is no multiple of 32 is filled with
+ * zeros).  Its scale is X = 2^e, e = floor(log2 max|x|) - 2, at least -127, kept
+ * as the byte e + 127; every element is the E2M1 value (0, 0.5, 1, 1.5, 2, 3, 4,
+ * 6 with a sign) nearest to x / X, ties to the even code, magnitudes above 6
+ * kept as 6.  A block with a NaN or an infinity in it gets the scale byte 255,
+ * and reads back as NaN; so do the bytes 253 and 254, which are never written.
+ *
+ * Layout.  A cache (one for K, one for V) is [Bt][H_kv][tiles][tile bytes] with
+ * tiles = ceil(S_max / 64) and photon_mxfp4_tile_bytes(d_h) bytes per tile of 64
+ * positions: d_p = photon_kv_row_elems(d_h), NB = d_p / 32, 32 * d_p bytes of
+ * codes, then 64 * NB scale bytes.  With kk the position in the tile, block b:
+ *   K codes   element e of the block in byte ((kk / 16) * NB + b) * 256 + (kk % 16) * 16 + e / 2
+ *   K scale   x = (kk / 16) * NB + b: byte ((x % 4) * 16 + kk % 16) * NB + x / 4 of the scales
+ *   V codes   element d of the row, w = (kk / 32) * 2 * NB + d / 16: in byte
+ *             (w / 4) * 1024 + (kk % 32 / 8 * 16 + d % 16) * 16 + (w % 4) * 4 + kk % 8 / 2
+ *   V scale   byte kk * NB + b of the scales
+ * Of a byte's two codes the one of the even element (K) or position (V) is in
+ * the low half.  Positions never written may hold anything.
+ *
+ * Caches must be 16-byte aligned.  Rows (q, k, v, out) need the alignment of
+ * their elements only; whole multiples of 16 bytes (pointer, stride, d_h) are
+ * read fastest.  d_h in [1, 128], S_max < 2^31, dt fp32 or bf16.
+ * Bt == 0 or T == 0 is a no-op.
+ * -------------------------------------------------------------------------- */
+PHOTON_API int32_t photon_mxfp4_tile_bytes(int32_t d_h);   /* 0 when d_h is outside [1, 128] */
+PHOTON_API size_t photon_mxfp4_cache_bytes(int32_t Bt, int32_t H_kv, int32_t d_h, int64_t S_max);   /* of K or of V */
+
+/* Quantises T new rows per sequence into the cache: row t of sequence b becomes the entry at position start[b] + t.
+ *   k, v       rows [Bt*T] of [H_kv, d_h] dt, row_stride elements from one to the next (parts of a wider matrix, such as a
+ *              QKV projection's, included)
+ *   start      [Bt] int32, device, or NULL: 0 (a prompt)
+ *   n_new      [Bt] int32, device, or NULL: T; only the first n_new[b] rows of sequence b are used (a padded batch)
+ *   status     NULL, or a device word that PHOTON_STATUS_CACHE_FULL is ORed into when a row has no place: entries outside
+ *              [0, S_max) are not written
+ * The entries around the written ones keep their bits. */
+PHOTON_API int32_t photon_mxfp4_cache_write(const void* k, const void* v, int64_t row_stride, void* k_cache, void* v_cache,
+                                            const int32_t* start, const int32_t* n_new, int32_t* status, int32_t Bt, int32_t T,
+                                            int32_t H_kv, int32_t d_h, int64_t S_max, photon_dtype dt, void* stream);
+
+/* Reads entries back: row t of sequence b receives the values at position start[b] + t, exact in either dt (but for bf16
+ * values whose scale is so small that they are below bf16's subnormals).  Arguments as for the write; rows past n_rows[b],
+ * and rows whose position is outside [0, S_max), are left as they were. */
+PHOTON_API int32_t photon_mxfp4_cache_read(const void* k_cache, const void* v_cache, const int32_t* start, const int32_t* n_rows,
+                                           void* k, void* v, int64_t row_stride, int32_t Bt, int32_t T, int32_t H_kv, int32_t d_h,
+                                           int64_t S_max, photon_dtype dt, void* stream);
+
+/* Attention of T new queries per sequence over the cache; H / H_kv consecutive query heads share a K/V head.  The last
+ * n_new[b] of the seq_len[b] entries are the queries' own (written before): query t < n_new[b] sees the first
+ * seq_len[b] - n_new[b] + t + 1 entries,
+ *     out[b,t,h,:] = softmax(scale * q[b,t,h,:] . K) V   over them; none: zeros.
+ *   q        rows [Bt*T] of [H, d_h] dt, q_stride elements from one to the next
+ *   seq_len  [Bt] int32, device; values outside [0, S_max] count as the nearer end
+ *   n_new    [Bt] int32, device, or NULL: T; queries past n_new[b] are skipped, their rows of out left as they were
+ *   out      [Bt, T, H, d_h] dt
+ * Scores, softmax and sums are in fp32 (with bf16 rows the softmax weights enter the products with V as bf16).  The
+ * positions are split over n_splits workgroups per stream (0 = choose from the shape); partial results are merged in
+ * a fixed order, so the result is run-to-run deterministic for a given n_splits.  n_splits > 1 needs a workspace of
+ * photon_mxfp4_decode_attn_workspace_bytes() bytes (no initialisation; calls that share one must be stream-ordered). */
+PHOTON_API size_t photon_mxfp4_decode_attn_workspace_bytes(int32_t Bt, int32_t T, int32_t H, int32_t d_h, int32_t n_splits);
+PHOTON_API int32_t photon_mxfp4_decode_attn_auto_splits(int32_t Bt, int32_t T, int32_t H, int32_t H_kv, int64_t S_max);
+PHOTON_API int32_t photon_mxfp4_decode_attn(const void* q, int64_t q_stride, const void* k_cache, const void* v_cache,
+                                            const int32_t* seq_len, const int32_t* n_new, void* out, int32_t Bt, int32_t T, int32_t H,
+                                            int32_t H_kv, int32_t d_h, int64_t S_max, float scale, int32_t n_splits, void* workspace,
+                                            size_t workspace_bytes, photon_dtype dt, void* stream);
+
+/* --------------------------------------------------------------------------
  * Chunk-local causal attention of the local decoders (paper Eq. 6-7): every
  * chunk is an independent window of W positions; query i (0 <= i < q_len) sits
  * at window position q_pos + i and attends to keys 0 .. q_pos + i of its own

@@ -92,6 +92,66 @@ def e4m3_round(x):
     return e4m3_decode(e4m3_encode(x))
 
 
+# MXFP4 (OCP microscaling formats): blocks of 32 values under one scale 2^e
+# (stored as e + 127, 255 = NaN), elements in E2M1 (1 sign, 2 exponent bits with
+# bias 1, 1 mantissa bit; largest value 6).  e = floor(log2 max|x|) - 2, the
+# exponent that puts the block's largest value into E2M1's top binade.
+def mxfp4_decode(codes, scales):
+    """Values [..., 32 n] of element codes [..., 32 n] under scale bytes [..., n]."""
+    c = np.asarray(codes).astype(np.int64)
+    s, e, m = c >> 3, (c >> 1) & 3, c & 1
+    v = np.where(e > 0, np.ldexp(1.0 + m / 2.0, e - 1), m / 2.0)
+    v = np.where(s == 1, -v, v)
+    b = np.repeat(np.asarray(scales).astype(np.int64), 32, axis=-1)
+    return np.where(b == 255, np.nan, np.ldexp(v, b - 127))
+
+
+def mxfp4_encode(x):
+    """(codes, scale bytes) of x [..., 32 n]: nearest E2M1 value of x / 2^e, ties
+    to the even mantissa, magnitudes beyond 6 stored as 6.  A block that holds a
+    NaN or an infinity has scale byte 255 (its codes mean nothing: 0 here)."""
+    x = f64(x)
+    blocks = x.reshape(x.shape[:-1] + (x.shape[-1] // 32, 32))
+    finite = np.isfinite(blocks).all(-1)
+    blocks = np.where(finite[..., None], blocks, 0.0)
+    a = np.abs(blocks)
+    top = a.max(-1)
+    e = np.where(top > 0, np.frexp(top)[1] - 1 - 2, -127)
+    e = np.maximum(e, -127)
+    y = np.ldexp(a, -e[..., None])
+    ye = np.clip(np.frexp(y)[1] - 1, 0, 2)              # binade of the result, subnormals below 1
+    q = np.rint(np.ldexp(y, 1 - ye))                    # in steps of 2^(ye-1); rint: ties to even
+    y = np.minimum(np.ldexp(q, ye - 1), 6.0)
+    ye = np.where(y >= 1, np.frexp(y)[1] - 1, 0)
+    code = np.where(y >= 1, 2 * (ye + 1) + np.rint(2 * (np.ldexp(y, -ye) - 1)), 2 * y).astype(np.uint8)
+    code = code | (np.signbit(blocks) << 3).astype(np.uint8)
+    return code.reshape(x.shape), np.where(finite, e + 127, 255).astype(np.uint8)
+
+
+def mxfp4_round(x):
+    """x [..., d] as it reads back from MXFP4 storage (the last block of a row filled with zeros)."""
+    x = f64(x)
+    d = x.shape[-1]
+    p = np.concatenate([x, np.zeros(x.shape[:-1] + (-d % 32,))], -1)
+    return mxfp4_decode(*mxfp4_encode(p))[..., :d]
+
+
+def mxfp4_decode_attn(q, k, v, seq_len, n_new, scale):
+    """T queries per sequence, q [Bt, T, H, d]; query t < n_new[b] sees the first
+    seq_len[b] - n_new[b] + t + 1 entries of k, v [Bt, H_kv, S, d] (none: zeros);
+    rows past n_new[b] are zeros here."""
+    q, k, v = f64(q), f64(k), f64(v)
+    out = np.zeros_like(q)
+    group = q.shape[2] // k.shape[1]
+    for b in range(q.shape[0]):
+        for t in range(int(n_new[b])):
+            n = int(seq_len[b]) - int(n_new[b]) + t + 1
+            for h in range(q.shape[2]):
+                if n > 0:
+                    out[b, t, h] = attend(q[b, t, h], k[b, h // group, :n], v[b, h // group, :n], scale)
+    return out
+
+
 def kv_store(cfg, x):
     """What the coarse K/V cache holds for the value x: x itself, or its E4M3
     rounding when the configuration stores the cache in 8 bits (reading G19)."""

@@ -14,6 +14,7 @@ from .binding import (  # noqa: F401
     PhotonState,
     lib_path,
     load_library,
+    mxfp4_cache,
     pad_kv_rows,
     photon_chunk_local_attn,
     photon_chunker_project,
@@ -34,6 +35,13 @@ from .binding import (  # noqa: F401
     photon_last_error,
     photon_linear,
     photon_mfma_probe,
+    photon_mxfp4_cache_bytes,
+    photon_mxfp4_cache_read,
+    photon_mxfp4_cache_write,
+    photon_mxfp4_decode_attn,
+    photon_mxfp4_decode_attn_auto_splits,
+    photon_mxfp4_decode_attn_workspace_bytes,
+    photon_mxfp4_tile_bytes,
     photon_persistent_trace,
     photon_prefill,
     photon_prefill_workspace_bytes,

@@ -45,6 +45,13 @@ def load_library() -> C.CDLL:
         "photon_coarse_decode_attn_static": (i32, [vp, vp, vp, vp, vp, i32, i32, i32, i64, f32, i32, i32, vp]),
         "photon_chunk_local_attn": (i32, [vp, vp, vp, vp, i64, i32, i32, i32, i32, i32, f32, i32, vp]),
         "photon_linear": (i32, [vp, vp, vp, f32, vp, vp, vp, i32, i32, i32, i32, i32, vp]),
+        "photon_mxfp4_tile_bytes": (i32, [i32]),
+        "photon_mxfp4_cache_bytes": (sz, [i32, i32, i32, i64]),
+        "photon_mxfp4_cache_write": (i32, [vp, vp, i64, vp, vp, vp, vp, vp, i32, i32, i32, i32, i64, i32, vp]),
+        "photon_mxfp4_cache_read": (i32, [vp, vp, vp, vp, vp, vp, i64, i32, i32, i32, i32, i64, i32, vp]),
+        "photon_mxfp4_decode_attn_workspace_bytes": (sz, [i32, i32, i32, i32, i32]),
+        "photon_mxfp4_decode_attn_auto_splits": (i32, [i32, i32, i32, i32, i64]),
+        "photon_mxfp4_decode_attn": (i32, [vp, i64, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i64, f32, i32, vp, sz, i32, vp]),
     }
     for name, (res, args) in sigs.items():
         if not hasattr(lib, name):
@@ -300,6 +307,130 @@ def photon_linear(x, w, out, gain=None, rms_eps: float = 1e-5, bias=None, res=No
         epilogue |= PHOTON_LINEAR_OUT_BF16
     _check(lib.photon_linear(_ptr(x), _ptr(w), _ptr(gain), rms_eps, _ptr(bias), _ptr(res), _ptr(out), M, N, K, epilogue,
                              _dt(w), _stream()))
+    return out
+
+
+# --------------------------------------------------------------------------
+# K/V cache in 4 bits (MXFP4)
+# --------------------------------------------------------------------------
+MXFP4_TILE = 64
+
+
+def photon_mxfp4_tile_bytes(d_h: int) -> int:
+    """Bytes of a cache tile (64 positions of one K/V head)."""
+    n = int(load_library().photon_mxfp4_tile_bytes(d_h))
+    if n == 0:
+        raise PhotonError(-1, f"head size {d_h} is outside [1, 128]")
+    return n
+
+
+def photon_mxfp4_cache_bytes(Bt: int, H_kv: int, d_h: int, S_max: int) -> int:
+    return int(load_library().photon_mxfp4_cache_bytes(Bt, H_kv, d_h, S_max))
+
+
+def mxfp4_cache(Bt: int, H_kv: int, d_h: int, S_max: int, device="cuda") -> torch.Tensor:
+    """An empty K or V cache in MXFP4 for S_max positions (rounded up to whole tiles): uint8 [Bt, H_kv, tiles, tile bytes]."""
+    tiles = (S_max + MXFP4_TILE - 1) // MXFP4_TILE
+    return torch.zeros((Bt, H_kv, tiles, photon_mxfp4_tile_bytes(d_h)), dtype=torch.uint8, device=device)
+
+
+def _mx_caches(k_cache: torch.Tensor, v_cache: torch.Tensor, Bt: int, d_h: int):
+    """(H_kv, S_max) of a pair of caches that fit Bt sequences and head size d_h."""
+    for c in (k_cache, v_cache):
+        if c.dtype != torch.uint8 or c.dim() != 4:
+            raise PhotonError(-1, "an MXFP4 cache is a uint8 tensor [Bt, H_kv, tiles, tile bytes]")
+    if k_cache.shape != v_cache.shape or k_cache.shape[0] != Bt or k_cache.shape[3] != photon_mxfp4_tile_bytes(d_h):
+        raise PhotonError(-1, f"caches {tuple(k_cache.shape)} and {tuple(v_cache.shape)} do not hold {Bt} sequences of head size {d_h}")
+    return k_cache.shape[1], k_cache.shape[2] * MXFP4_TILE
+
+
+def _mx_row_stride(t: torch.Tensor) -> int:
+    """Elements from one row [heads, d_h] of [Bt, T, heads, d_h] to the next."""
+    Bt, T, H, d_h = t.shape
+    sb, st, sh, sd = t.stride()
+    stride = st if T > 1 else sb if Bt > 1 else H * d_h
+    if (sd != 1 and d_h > 1) or (sh != d_h and H > 1) or (T > 1 and Bt > 1 and sb != T * st):
+        raise PhotonError(-1, f"rows [Bt, T, heads, d_h] must be one stride apart, each of them contiguous: strides {tuple(t.stride())}")
+    return stride
+
+
+def _mx_counts(t: Optional[torch.Tensor], Bt: int, name: str) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype != torch.int32 or t.numel() != Bt:
+        raise PhotonError(-1, f"{name} must hold an int32 per sequence")
+    return _ptr(t)
+
+
+def _mx_call(fn, tensors, *args) -> None:
+    """fn(*args, stream) on the current stream of the tensors' device, with that device current."""
+    device = tensors[0].device
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device != device):
+            raise PhotonError(-1, f"all tensors must live in the memory of one device: {device} and {t.device}")
+    if device.index == torch.cuda.current_device():
+        _check(fn(*args, _stream()))
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, _stream()))
+
+
+def _mx_rows(k, v, k_cache, v_cache, start, n_new):
+    """Arguments that the cache's write and read share, with what they come to."""
+    if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in (torch.float32, torch.bfloat16):
+        raise PhotonError(-1, "k and v must be fp32 or bf16 tensors [Bt, T, H_kv, d_h] of one shape and dtype")
+    Bt, T, H_kv, d_h = k.shape
+    stride = _mx_row_stride(k)
+    if _mx_row_stride(v) != stride:
+        raise PhotonError(-1, f"k and v rows must have one stride: {stride} and {_mx_row_stride(v)}")
+    heads, S_max = _mx_caches(k_cache, v_cache, Bt, d_h)
+    if heads != H_kv:
+        raise PhotonError(-1, f"rows of {H_kv} heads do not fit a cache of {heads}")
+    return (stride, _ptr(k_cache), _ptr(v_cache), _mx_counts(start, Bt, "start"), _mx_counts(n_new, Bt, "n_new"),
+            (Bt, T, H_kv, d_h, S_max, PHOTON_F32 if k.dtype == torch.float32 else PHOTON_BF16))
+
+
+def photon_mxfp4_cache_write(k, v, k_cache, v_cache, start=None, n_new=None, status=None) -> None:
+    """Rows k, v [Bt, T, H_kv, d_h] (views of a wider matrix included) become the entries start[b] .. of the caches (see
+    mxfp4_cache); start, n_new int32 [Bt] or None (0, T); status: int32 word that receives PHOTON_STATUS_CACHE_FULL."""
+    stride, kc, vc, first, count, shape = _mx_rows(k, v, k_cache, v_cache, start, n_new)
+    if status is not None and (status.dtype != torch.int32 or status.numel() < 1):
+        raise PhotonError(-1, "status must be an int32 tensor")
+    _mx_call(load_library().photon_mxfp4_cache_write, (k, v, k_cache, v_cache, start, n_new, status), k.data_ptr(), v.data_ptr(), stride, kc, vc,
+             first, count, _ptr(status), *shape)
+
+
+def photon_mxfp4_cache_read(k_cache, v_cache, k, v, start=None, n_rows=None) -> None:
+    """The entries start[b] .. of the caches into rows k, v [Bt, T, H_kv, d_h]; rows past n_rows[b] stay as they are."""
+    stride, kc, vc, first, count, shape = _mx_rows(k, v, k_cache, v_cache, start, n_rows)
+    _mx_call(load_library().photon_mxfp4_cache_read, (k, v, k_cache, v_cache, start, n_rows), kc, vc, first, count, k.data_ptr(), v.data_ptr(),
+             stride, *shape)
+
+
+def photon_mxfp4_decode_attn_workspace_bytes(Bt: int, T: int, H: int, d_h: int, n_splits: int) -> int:
+    return int(load_library().photon_mxfp4_decode_attn_workspace_bytes(Bt, T, H, d_h, n_splits))
+
+
+def photon_mxfp4_decode_attn_auto_splits(Bt: int, T: int, H: int, H_kv: int, S_max: int) -> int:
+    return int(load_library().photon_mxfp4_decode_attn_auto_splits(Bt, T, H, H_kv, S_max))
+
+
+def photon_mxfp4_decode_attn(q, k_cache, v_cache, seq_len, out, n_new=None, scale: Optional[float] = None, n_splits: int = 0,
+                             workspace: Optional[torch.Tensor] = None):
+    """q (rows one stride apart), out (contiguous) [Bt, T, H, d_h] fp32 or bf16; caches as mxfp4_cache makes them; seq_len int32
+    [Bt], the T (n_new[b]) queries' own entries counted; returns out."""
+    if q.dim() != 4 or q.shape != out.shape or q.dtype != out.dtype or q.dtype not in (torch.float32, torch.bfloat16):
+        raise PhotonError(-1, "q and out must be fp32 or bf16 tensors [Bt, T, H, d_h] of one shape and dtype")
+    if seq_len is None:
+        raise PhotonError(-1, "seq_len is missing")
+    Bt, T, H, d_h = q.shape
+    H_kv, S_max = _mx_caches(k_cache, v_cache, Bt, d_h)
+    if scale is None:
+        scale = 1.0 / math.sqrt(d_h)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _mx_call(load_library().photon_mxfp4_decode_attn, (q, k_cache, v_cache, seq_len, n_new, out, workspace), q.data_ptr(), _mx_row_stride(q),
+             _ptr(k_cache), _ptr(v_cache), _mx_counts(seq_len, Bt, "seq_len"), _mx_counts(n_new, Bt, "n_new"), _ptr(out), Bt, T, H, H_kv, d_h,
+             S_max, scale, n_splits, _ptr(workspace), ws_bytes, PHOTON_F32 if q.dtype == torch.float32 else PHOTON_BF16)
     return out
 
 
