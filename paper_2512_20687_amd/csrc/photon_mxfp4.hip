@@ -11,6 +11,8 @@
 
 namespace photon {
 
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+
 // ------------------------------------------------------------------ rows in and out
 //
 // A wave takes the positions of one tile of one stream, 8 positions x 64 elements at a time ("a pass"): lane 8 r + x holds 8
@@ -250,73 +252,493 @@ __global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_read_kernel(const uint8_t
 }
 
 // ------------------------------------------------------------------ attention
+//
+// Score and value products run on the matrix cores in bf16, in which every stored value is exact; fp32 operands (the query, a
+// weight) enter as three bf16 parts of 8 bits each, which are exact too, so with fp32 rows nothing is rounded below fp32.
+//
+// A wave takes 64 positions at a time: NB loads of 16 bytes a lane of K, as many of V, and the scale bytes.
+//   Scores: S^T = Q K^T with the queries (or the parts of one query) as the four rows i of every row group g = 0..3 of a
+//     16 x 16 x 32 MFMA and positions as columns.  A lane's K chunk is 32 elements of one position under one scale, so its
+//     conversion takes the scale along, and the four MFMAs that consume it contract over all of the chunks of a column.  Which of
+//     them belong to one position differs by NB: row group g has the query where the chunks belong to positions 16 g .. + 15
+//     (or could), zeros elsewhere, and picks the load that holds them.  Lane l ends up with the scores of position l: softmax
+//     costs one exponential per lane and query, and no lane repeats another's.
+//   Values: O = (P X) V with the weights times V's scale as rows (a scale per 32 elements: one such operand per block) and the
+//     elements of V as columns.  The weights change from a lane per position to operand order through LDS.
+//   The reference of the exponentials is the largest score when it was last raised, which happens when one exceeds it by more
+//     than MX_RAISE: fp32 and bf16 lose nothing by weights up to 2^MX_RAISE, and the usual tile needs no maximum.
+constexpr float MX_RAISE = 16.f;
+constexpr int MX_P_PITCH = 72;                   // bf16 elements of a weight row in LDS: 64 positions, rows on different banks
 
-// One wave per query: a lane per position for the scores, a lane per element for the values.
-template <typename T, int NB>
-__global__ __launch_bounds__(64) void mxfp4_attn_kernel(const T* __restrict__ q, int64_t q_stride, const uint8_t* __restrict__ kc,
-                                                        const uint8_t* __restrict__ vc, const int32_t* __restrict__ seq_len,
-                                                        const int32_t* __restrict__ n_new, T* __restrict__ out, int Tq, int H, int H_kv, int d_h,
-                                                        int64_t S_max, float scale_log2e) {
-  constexpr int DP = NB * MX_BLOCK;
-  const int lane = threadIdx.x;
-  const int h = blockIdx.x % H, t = blockIdx.x / H % Tq, b = blockIdx.x / H / Tq;
-  int m = n_new ? n_new[b] : Tq;
-  m = m < 0 ? 0 : m > Tq ? Tq : m;
-  if (t >= m) return;
-  int64_t n = seq_len[b];
-  n = n < 0 ? 0 : n > S_max ? S_max : n;
-  n = n - m + t + 1;
-  n = n < 0 ? 0 : n;
-  __shared__ float qs[DP], pb[MX_TILE][NB];
-  q += ((int64_t)b * Tq + t) * q_stride + (int64_t)h * d_h;
-  for (int i = lane; i < DP; i += 64) qs[i] = i < d_h ? to_f32<T>(q[i]) * scale_log2e : 0.f;
-  __syncthreads();
-  const int64_t tiles = (S_max + MX_TILE - 1) / MX_TILE, stream = (int64_t)b * H_kv + h / (H / H_kv);
-  float top = NEG_BIG, sum = 0.f, o[2] = {0.f, 0.f};
-  for (int64_t base = 0; base < n; base += MX_TILE) {
-    const uint8_t* kt = kc + (stream * tiles + base / MX_TILE) * mx_tile_bytes(DP);
-    const uint8_t* vt = vc + (stream * tiles + base / MX_TILE) * mx_tile_bytes(DP);
-    const bool seen = base + lane < n;
-    float s = 0.f;
-    for (int block = 0; block < NB; ++block) {
-      const uint4_t c = load16(kt + mx_k_chunk<NB>(lane, block));
-      const uint32_t byte = kt[mx_k_scale<NB>(lane, block)];
-      for (int j = 0; j < 4; ++j) {
-        float x[8];
-        mx_values8(c[j], byte, x);
-        for (int e = 0; e < 8; ++e) s = fmaf(x[e], qs[block * 32 + j * 8 + e], s);
-      }
-    }
-    s = seen ? s : NEG_BIG;
-    float mx = s;
-    for (int d = 1; d < 64; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
-    mx = fmaxf(mx, top);
-    const float old = fast_exp2(top - mx), p = seen ? fast_exp2(s - mx) : 0.f;
-    top = mx;
-    sum = sum * old + wave_sum(p);
-    o[0] *= old;
-    o[1] *= old;
-    for (int block = 0; block < NB; ++block) {
-      const uint32_t byte = vt[mx_v_scale<NB>(lane, block)];
-      float x[8];
-      mx_values8(2u, byte, x);       // 1 under this scale
-      pb[lane][block] = seen ? p * x[0] : 0.f;
-    }
-    __syncthreads();
-    for (int u = 0; u < 2; ++u) {
-      const int dim = lane + 64 * u;
-      if (dim >= DP) continue;
-      for (int kk = 0; kk < MX_TILE; kk += 8) {
-        float x[8];
-        mx_values8(*reinterpret_cast<const uint32_t*>(vt + mx_v_word<NB>(kk, dim)), 127u, x);
-        for (int e = 0; e < 8; ++e) o[u] = fmaf(pb[kk + e][dim >> 5], x[e], o[u]);
-      }
-    }
-    __syncthreads();
+template <typename T, int NB, int NQ> struct MxAttn {
+  static constexpr int DP = NB * MX_BLOCK;
+  static constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
+  static constexpr int SETS = NQ == 1 ? 1 : PARTS * (NQ / 4);       // score operands: parts (one query: its parts are rows of one)
+  static constexpr int QSETS = NQ == 1 || PARTS == 1 ? 1 : NQ / 4;  // weight operands of a block
+  static constexpr int P_ROWS = NQ == 1 ? 4 * NB : PARTS == 1 ? NQ : 12 * QSETS;
+  static constexpr int ACC = 2 * NB;                                // column tiles of 16 elements
+  // per wave: weight rows, and the staged queries or the wave's result
+  static constexpr int P_BYTES = P_ROWS * MX_P_PITCH * 2;
+  static constexpr int O_BYTES = NQ * (DP + 2) * 4;
+  static constexpr int WAVE_BYTES = (P_BYTES > O_BYTES ? P_BYTES : O_BYTES) + 15 & ~15;
+};
+
+__device__ __forceinline__ bf16x8_t mx_operand(uint32_t w, float scale) {
+  uint4_t r;
+  r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
+  r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
+  r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
+  r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
+  return as_bf16x8(r);
+}
+
+// x = a + b + c, each with 8 significant bits (in the upper halves of the words): exact but for subnormals.
+__device__ __forceinline__ void mx_split3(float x, float& a, float& b, float& c) {
+  a = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+  const float r = x - a;
+  b = __uint_as_float(__float_as_uint(r) & 0xffff0000u);
+  c = r - b;
+}
+
+__device__ __forceinline__ float mx_wave_max(float x) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) x = fmaxf(x, __shfl_xor(x, d));
+  return x;
+}
+
+// LDS traffic of one wave is in order; this keeps the compiler from moving it.
+__device__ __forceinline__ void mx_wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+struct MxQueries {
+  const int32_t *seq_len, *n_new;
+  int64_t q_stride, S_max;
+  int T, H, H_kv, d_h, group, groups, n_splits;    // group: query heads of a K/V head; groups: workgroups that share its T * group queries
+  float scale_log2e;
+};
+
+// A split's tiles of n positions.
+__device__ __forceinline__ int mx_split_tiles(int64_t n, int n_splits) {
+  const int tiles = (int)((n + MX_TILE - 1) / MX_TILE);
+  return (tiles + n_splits - 1) / n_splits;
+}
+// Positions that count for sequence b, and its queries.
+__device__ __forceinline__ void mx_sequence(const MxQueries& a, int b, int64_t& n, int& m) {
+  n = a.seq_len[b];
+  n = n < 0 ? 0 : n > a.S_max ? a.S_max : n;
+  m = a.n_new ? a.n_new[b] : a.T;
+  m = m < 0 ? 0 : m > a.T ? a.T : m;
+}
+
+template <typename T, int NB, int NQ>
+__global__ __launch_bounds__(512) void mxfp4_attn_kernel(const T* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
+                                                         T* __restrict__ out, float* __restrict__ ws, MxQueries a) {
+  using C = MxAttn<T, NB, NQ>;
+  constexpr int DP = C::DP, SETS = C::SETS, ACC = C::ACC, QSETS = C::QSETS, PARTS = C::PARTS, TB = mx_tile_bytes(DP);
+  extern __shared__ __align__(16) char mx_lds[];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, waves = blockDim.x >> 6;
+  const int c = lane & 15, kg = lane >> 4;
+
+  unsigned unit = blockIdx.x;
+  const int chunk = unit % (unsigned)a.groups;
+  unit /= (unsigned)a.groups;
+  const int split = unit % (unsigned)a.n_splits;
+  const int64_t stream = unit / (unsigned)a.n_splits;
+  const int b = (int)(stream / a.H_kv), hk = (int)(stream - (int64_t)b * a.H_kv);
+
+  int64_t n;
+  int m;
+  mx_sequence(a, b, n, m);
+  const int first_q = chunk * NQ, queries = m * a.group - first_q;           // of this workgroup, at most NQ count
+  if (queries <= 0) return;
+  // query i of the workgroup is row first_q + i: token t = row / group, head hk * group + row % group; it sees seen[i] positions
+  int64_t seen[NQ];
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    const int t = (first_q + (i < queries ? i : queries - 1)) / a.group;
+    const int64_t s = n - m + t + 1;
+    seen[i] = s < 0 ? 0 : s;
   }
-  out += (((int64_t)b * Tq + t) * H + h) * d_h;
-  for (int u = 0; u < 2; ++u)
-    if (lane + 64 * u < d_h) out[lane + 64 * u] = from_f32<T>(n > 0 ? o[u] / sum : 0.f);
+  const int64_t hi = seen[NQ - 1], lo = seen[0];                             // seen grows with i
+  const int per = mx_split_tiles(n, a.n_splits);
+  const int begin = split * per;
+  int end = (int)((hi + MX_TILE - 1) / MX_TILE);
+  if (a.n_splits > 1 && begin >= (int)((n + MX_TILE - 1) / MX_TILE)) return;  // the merge knows that this split holds nothing
+  end = end < begin + per ? end : begin + per;
+
+  const int64_t tiles = (a.S_max + MX_TILE - 1) / MX_TILE;
+  const uint8_t* kt = kc + stream * tiles * TB + lane * 16;
+  const uint8_t* vt = vc + stream * tiles * TB + lane * 16;
+  const uint8_t* kst = kc + stream * tiles * TB + NB * 1024 + lane * NB;
+  const uint8_t* vst = vc + stream * tiles * TB + NB * 1024 + lane * NB;
+
+  struct Tile { uint4_t k[NB], v[NB]; uint32_t ks, vs; };
+  auto load_scales = [&](const uint8_t* p) -> uint32_t {
+    if constexpr (NB == 1) return *p;
+    else if constexpr (NB == 2) return *reinterpret_cast<const uint16_t*>(p);
+    else return *reinterpret_cast<const uint32_t*>(p);
+  };
+  auto load = [&](int tile, Tile& x) {
+    const int64_t at = (int64_t)tile * TB;
+    x.ks = load_scales(kst + at);
+#pragma unroll
+    for (int t = 0; t < NB; ++t) x.k[t] = load16_stream(kt + at + t * 1024);
+    x.vs = load_scales(vst + at);
+#pragma unroll
+    for (int t = 0; t < NB; ++t) x.v[t] = load16_stream(vt + at + t * 1024);
+  };
+
+  Tile cur, nxt;
+  int tile = begin + wave;
+  if (tile < end) load(tile, cur);
+
+  // queries: in LDS, then into the operands of the score products
+  float* qs = reinterpret_cast<float*>(mx_lds);
+  for (int x = tid; x < NQ * DP; x += blockDim.x) {
+    const int i = x / DP, d = x % DP;
+    float v = 0.f;
+    if (i < queries && d < a.d_h) {
+      const int row = first_q + i, t = row / a.group, h = hk * a.group + row % a.group;
+      v = to_f32<T>(q[((int64_t)b * a.T + t) * a.q_stride + (int64_t)h * a.d_h + d]);
+    }
+    qs[x] = v;
+  }
+  __syncthreads();
+  bf16x8_t aq[SETS][4];
+  {
+    const int g = c >> 2, i = c & 3;                                         // operand row c = 4 g + i
+    const int block = NB == 1 ? 0 : NB == 2 ? kg & 1 : kg;
+    const bool mine = NB == 1 ? g == kg : NB == 2 ? (g & 1) == (kg >> 1) : true;
+#pragma unroll
+    for (int s = 0; s < SETS; ++s) {
+      const int part = NQ == 1 ? i : s % PARTS, qi = NQ == 1 ? 0 : (s / PARTS) * 4 + i;
+      const bool there = mine && part < PARTS;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint4_t w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float x[2];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const float v = qs[qi * DP + block * 32 + j * 8 + 2 * e + u];
+            float p0, p1, p2;
+            mx_split3(v, p0, p1, p2);
+            x[u] = !there ? 0.f : part == 0 ? p0 : part == 1 ? p1 : p2;
+          }
+          w[e] = (__float_as_uint(x[0]) >> 16) | (__float_as_uint(x[1]) & 0xffff0000u);
+        }
+        aq[s][j] = as_bf16x8(w);
+      }
+    }
+  }
+  __syncthreads();                                                           // the staged queries make room for the weights
+
+  char* own = mx_lds + wave * C::WAVE_BYTES;
+  uint16_t* pw = reinterpret_cast<uint16_t*>(own);
+  const uint16_t* pr = pw + kg * 8;
+  float top[NQ], sum[NQ];
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) { top[i] = NEG_BIG; sum[i] = 0.f; }
+  f32x4_t acc[QSETS][ACC];
+#pragma unroll
+  for (int s = 0; s < QSETS; ++s)
+#pragma unroll
+    for (int t = 0; t < ACC; ++t) acc[s][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+
+  auto consume = [&](int tile_at, const Tile& x) {
+    const int64_t base = (int64_t)tile_at * MX_TILE;
+    float kf[NB], vf[NB];
+    bool kbad[NB], odd = false;
+#pragma unroll
+    for (int t = 0; t < NB; ++t) {
+      const uint32_t kx = (x.ks >> (8 * t)) & 255u, vx = (x.vs >> (8 * t)) & 255u;
+      kf[t] = __uint_as_float(kx << 23);
+      vf[t] = __uint_as_float(vx << 23);
+      kbad[t] = kx > (uint32_t)MX_LAST_SCALE;
+      odd = odd || kbad[t] || vx > (uint32_t)MX_LAST_SCALE;
+    }
+    // Tiles that some query does not see whole, or that hold a NaN block: positions that nobody sees must not reach a sum, not
+    // even times zero, and a NaN must reach its own position only, not the others of its column.
+    const bool slow = base + MX_TILE > lo || __builtin_amdgcn_ballot_w64(odd) != 0;
+    bool nan_here = false;
+    if (slow) {
+#pragma unroll
+      for (int t = 0; t < NB; ++t) {
+        const int64_t key = base + (t * 4 + kg) / NB * 16 + c;
+        const bool bad = kbad[t] && key < hi;
+        if (kbad[t] || key >= hi) kf[t] = 1.f;
+        const uint64_t mask = __builtin_amdgcn_ballot_w64(bad);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)                                          // chunks u of this load that belong to position `lane`
+          if ((t * 4 + u) / NB == kg) nan_here = nan_here || ((mask >> (u * 16 + c)) & 1u);
+        if (vf[t] > __uint_as_float((uint32_t)MX_LAST_SCALE << 23)) vf[t] = base + lane < hi ? __uint_as_float(0x7fc00000u) : 1.f;
+      }
+    }
+    float s[NQ];
+#pragma unroll
+    for (int t = 0; t < NB; ++t) {
+      f32x4_t d[SETS];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bf16x8_t bop = mx_operand(x.k[t][j], kf[t]);
+#pragma unroll
+        for (int u = 0; u < SETS; ++u)
+          d[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(aq[u][j], bop, j == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : d[u], 0, 0, 0);
+      }
+      const bool pick = NB == 1 || t == 0 || (NB == 2 ? (kg >> 1) == t : kg == t);
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) {
+        float y;
+        if constexpr (NQ == 1) y = PARTS == 3 ? (d[0][2] + d[0][1]) + d[0][0] : d[0][0];
+        else y = PARTS == 3 ? (d[(i / 4) * 3 + 2 < SETS ? (i / 4) * 3 + 2 : 0][i % 4] + d[(i / 4) * 3 + 1 < SETS ? (i / 4) * 3 + 1 : 0][i % 4]) + d[(i / 4) * 3 < SETS ? (i / 4) * 3 : 0][i % 4] : d[i / 4][i % 4];
+        s[i] = pick ? y : s[i];
+      }
+    }
+    bool raise = false;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      s[i] *= a.scale_log2e;
+      if (slow) {
+        if (nan_here) s[i] = __uint_as_float(0x7fc00000u);
+        if (base + lane >= seen[i]) s[i] = NEG_BIG;
+      }
+      raise = raise || s[i] > top[i] + MX_RAISE;
+    }
+    if (__builtin_amdgcn_ballot_w64(raise) != 0) {
+      float shrink[NQ];
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) {
+        const float higher = fmaxf(top[i], mx_wave_max(s[i]));
+        shrink[i] = fast_exp2(top[i] - higher);
+        top[i] = higher;
+        sum[i] *= shrink[i];
+      }
+#pragma unroll
+      for (int u = 0; u < QSETS; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          // row 4 kg + r of the value products: the query it belongs to
+          float f;
+          if constexpr (NQ == 1) f = shrink[0];
+          else if constexpr (PARTS == 3 || NQ == 4) f = shrink[(4 * u + r) % NQ];
+          else f = kg == 0 ? shrink[r] : shrink[(4 + r) % NQ];
+#pragma unroll
+          for (int t = 0; t < ACC; ++t) acc[u][t][r] *= f;
+        }
+    }
+    float p[NQ];
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      p[i] = fast_exp2(s[i] - top[i]);
+      if (slow && base + lane >= seen[i]) p[i] = 0.f;
+      sum[i] += p[i];
+    }
+    if constexpr (NQ == 1) {
+      // rows 4 block + part
+      mx_wave_order();
+#pragma unroll
+      for (int t = 0; t < NB; ++t) {
+        float y = p[0] * vf[t];
+        if (slow && base + lane >= seen[0]) y = 0.f;
+        uint16_t* w = pw + 4 * t * MX_P_PITCH + lane;
+        if constexpr (PARTS == 3) {
+          float p0, p1, p2;
+          mx_split3(y, p0, p1, p2);
+          w[0] = (uint16_t)(__float_as_uint(p0) >> 16);
+          w[MX_P_PITCH] = (uint16_t)(__float_as_uint(p1) >> 16);
+          w[2 * MX_P_PITCH] = (uint16_t)(__float_as_uint(p2) >> 16);
+        } else {
+          w[0] = (uint16_t)f32_to_bf16_bits(y);
+        }
+      }
+      mx_wave_order();
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bf16x8_t aop = as_bf16x8(*reinterpret_cast<const uint4_t*>(pr + (c % C::P_ROWS) * MX_P_PITCH + h * 32));
+#pragma unroll
+        for (int t = 0; t < ACC; ++t) {
+          const int w = h * ACC + t;
+          acc[0][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(aop, mx_operand(x.v[w >> 2][w & 3], 1.f), acc[0][t], 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int blk = 0; blk < NB; ++blk) {
+        mx_wave_order();
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+          float y = p[i] * vf[blk];
+          if (slow && base + lane >= seen[i]) y = 0.f;
+          if constexpr (PARTS == 3) {
+            // rows 12 set + 4 part + query
+            uint16_t* w = pw + (12 * (i / 4) + i % 4) * MX_P_PITCH + lane;
+            float p0, p1, p2;
+            mx_split3(y, p0, p1, p2);
+            w[0] = (uint16_t)(__float_as_uint(p0) >> 16);
+            w[4 * MX_P_PITCH] = (uint16_t)(__float_as_uint(p1) >> 16);
+            w[8 * MX_P_PITCH] = (uint16_t)(__float_as_uint(p2) >> 16);
+          } else {
+            pw[i * MX_P_PITCH + lane] = (uint16_t)f32_to_bf16_bits(y);
+          }
+        }
+        mx_wave_order();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int w = h * ACC + 2 * blk;
+          const bf16x8_t v0 = mx_operand(x.v[w >> 2][w & 3], 1.f), v1 = mx_operand(x.v[(w + 1) >> 2][(w + 1) & 3], 1.f);
+#pragma unroll
+          for (int u = 0; u < QSETS; ++u) {
+            const int row = PARTS == 3 ? 12 * u + (c < 12 ? c : c - 12) : c % NQ;
+            const bf16x8_t aop = as_bf16x8(*reinterpret_cast<const uint4_t*>(pr + row * MX_P_PITCH + h * 32));
+            acc[u][2 * blk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(aop, v0, acc[u][2 * blk], 0, 0, 0);
+            acc[u][2 * blk + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(aop, v1, acc[u][2 * blk + 1], 0, 0, 0);
+          }
+        }
+      }
+    }
+  };
+
+  while (tile < end) {
+    int next = tile + waves;
+    if (next < end) load(next, nxt);
+    consume(tile, cur);
+    tile = next;
+    if (tile >= end) break;
+    next = tile + waves;
+    if (next < end) load(next, cur);
+    consume(tile, nxt);
+    tile = next;
+  }
+
+  // The wave's result: sums over lanes, parts put together, into LDS.
+  mx_wave_order();
+  float* ow = reinterpret_cast<float*>(own);
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    const float l = wave_sum(sum[i]);
+    if (lane == 0) { ow[i * (DP + 2)] = top[i]; ow[i * (DP + 2) + 1] = l; }
+  }
+#pragma unroll
+  for (int u = 0; u < QSETS; ++u)
+#pragma unroll
+    for (int t = 0; t < ACC; ++t) {
+      if constexpr (NQ == 1) {
+        const float y = PARTS == 3 ? (acc[0][t][2] + acc[0][t][1]) + acc[0][t][0] : acc[0][t][0];
+        if (kg == t / 2) ow[2 + 16 * t + c] = y;
+      } else if constexpr (PARTS == 3) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float y = kg < 3 ? acc[u][t][r] : 0.f;
+          y += __shfl_xor(y, 32);
+          y += __shfl_xor(y, 16);
+          if (kg == 0) ow[(4 * u + r) * (DP + 2) + 2 + 16 * t + c] = y;
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (4 * kg + r < NQ) ow[(4 * kg + r) * (DP + 2) + 2 + 16 * t + c] = acc[0][t][r];
+      }
+    }
+  __syncthreads();
+  // The waves' results, in order.
+  for (int x = tid; x < NQ * DP; x += blockDim.x) {
+    const int i = x / DP, d = x % DP;
+    if (i >= queries) break;
+    const char* at = mx_lds + (i * (DP + 2)) * 4;
+    float mx = NEG_BIG;
+    for (int w = 0; w < waves; ++w) mx = fmaxf(mx, reinterpret_cast<const float*>(at + w * C::WAVE_BYTES)[0]);
+    float l = 0.f, o = 0.f;
+    for (int w = 0; w < waves; ++w) {
+      const float* pw_ = reinterpret_cast<const float*>(at + w * C::WAVE_BYTES);
+      const float f = fast_exp2(pw_[0] - mx);
+      l = fmaf(pw_[1], f, l);
+      o = fmaf(pw_[2 + d], f, o);
+    }
+    const int row = first_q + i, t = row / a.group, h = hk * a.group + row % a.group;
+    const int64_t to = ((int64_t)b * a.T + t) * a.H + h;
+    if (a.n_splits == 1) {
+      if (d < a.d_h) out[to * a.d_h + d] = from_f32<T>(seen[i < NQ ? i : 0] > 0 ? o / l : 0.f);
+    } else {
+      float* p = ws + (to * a.n_splits + split) * (DP + 2);
+      if (d == 0) { p[0] = mx; p[1] = l; }
+      p[2 + d] = o;
+    }
+  }
+}
+
+// The splits' results of one query, in order.
+template <typename T, int NB>
+__global__ __launch_bounds__(NB * MX_BLOCK) void mxfp4_merge_kernel(const float* __restrict__ ws, T* __restrict__ out, MxQueries a) {
+  constexpr int DP = NB * MX_BLOCK;
+  const int h = blockIdx.x % (unsigned)a.H;
+  const int64_t row = blockIdx.x / (unsigned)a.H;
+  const int b = (int)(row / a.T), t = (int)(row - (int64_t)b * a.T), d = threadIdx.x;
+  int64_t n;
+  int m;
+  mx_sequence(a, b, n, m);
+  if (t >= m) return;
+  const int per = mx_split_tiles(n, a.n_splits), tiles = (int)((n + MX_TILE - 1) / MX_TILE);
+  const int used = per == 0 ? 0 : (tiles + per - 1) / per;
+  const int64_t to = row * a.H + h;
+  const float* p = ws + to * a.n_splits * (DP + 2);
+  float mx = NEG_BIG, l = 0.f, o = 0.f;
+  for (int s = 0; s < used; ++s) mx = fmaxf(mx, p[s * (DP + 2)]);
+  for (int s = 0; s < used; ++s) {
+    const float f = fast_exp2(p[s * (DP + 2)] - mx);
+    l = fmaf(p[s * (DP + 2) + 1], f, l);
+    o = fmaf(p[s * (DP + 2) + 2 + d], f, o);
+  }
+  if (d < a.d_h) out[to * a.d_h + d] = from_f32<T>(n - m + t + 1 > 0 ? o / l : 0.f);
+}
+
+// Queries that share what a workgroup reads.  fp32: at most 4 (the operands of 8 are 96 registers a lane: 120 spilled).
+int mx_query_rows(int64_t queries, bool f32) { return queries <= 1 ? 1 : queries <= 4 || f32 ? 4 : 8; }
+
+int mx_auto_splits(int Bt, int T, int H, int H_kv, int64_t S_max) {
+  const int64_t queries = (int64_t)T * (H / H_kv), rows = mx_query_rows(queries, true);
+  const int64_t groups = (int64_t)Bt * H_kv * ((queries + rows - 1) / rows), tiles = (S_max + MX_TILE - 1) / MX_TILE;
+  int64_t splits = 1024 / groups;
+  const int64_t most = tiles / 16;                       // at least two tiles a wave
+  splits = splits > most ? most : splits;
+  return (int)(splits < 1 ? 1 : splits > 1024 ? 1024 : splits);
+}
+
+template <typename T, int NB, int NQ>
+int32_t mx_launch_attn(const void* q, const void* kc, const void* vc, void* out, void* ws, const MxQueries& a, int Bt, hipStream_t st) {
+  const int64_t tiles = (a.S_max + MX_TILE - 1) / MX_TILE, per = (tiles + a.n_splits - 1) / a.n_splits;
+  const int64_t workgroups = (int64_t)Bt * a.H_kv * a.n_splits * a.groups;
+  PHOTON_REQUIRE(workgroups <= 0x7fffffff, PHOTON_ERR_UNSUPPORTED, "photon_mxfp4_decode_attn: %lld workgroups", (long long)workgroups);
+  const int waves = per >= 8 ? 8 : per > 2 ? 4 : per > 1 ? 2 : 1;
+  const int lds = waves * MxAttn<T, NB, NQ>::WAVE_BYTES, staged = NQ * NB * MX_BLOCK * 4;
+  PHOTON_LAUNCH(KC_COARSE_ATTN, st, (mxfp4_attn_kernel<T, NB, NQ>), dim3((unsigned)workgroups), dim3(waves * 64),
+                lds > staged ? lds : staged, st, (const T*)q, (const uint8_t*)kc, (const uint8_t*)vc, (T*)out, (float*)ws, a);
+  const int32_t rc = check_launch("mxfp4_attn_kernel");
+  if (rc != PHOTON_OK || a.n_splits == 1) return rc;
+  PHOTON_LAUNCH(KC_COARSE_MERGE, st, (mxfp4_merge_kernel<T, NB>), dim3((unsigned)(Bt * a.T * a.H)), dim3(NB * MX_BLOCK), 0, st, (const float*)ws, (T*)out, a);
+  return check_launch("mxfp4_merge_kernel");
+}
+
+template <typename T, int NB>
+int32_t mx_launch_attn_q(const void* q, const void* kc, const void* vc, void* out, void* ws, MxQueries a, int Bt, hipStream_t st) {
+  const int64_t queries = (int64_t)a.T * a.group, rows = mx_query_rows(queries, sizeof(T) == 4);
+  a.groups = (int)((queries + rows - 1) / rows);
+  if (rows == 1) return mx_launch_attn<T, NB, 1>(q, kc, vc, out, ws, a, Bt, st);
+  if (rows == 4) return mx_launch_attn<T, NB, 4>(q, kc, vc, out, ws, a, Bt, st);
+  if constexpr (sizeof(T) == 2) return mx_launch_attn<T, NB, 8>(q, kc, vc, out, ws, a, Bt, st);
+  return fail(PHOTON_ERR_UNSUPPORTED, "attention: %d query rows", (int)rows);
+}
+
+template <typename T>
+int32_t mx_launch_attn_t(const void* q, const void* kc, const void* vc, void* out, void* ws, const MxQueries& a, int Bt, hipStream_t st) {
+  switch (kv_row_elems(a.d_h)) {
+    case 32: return mx_launch_attn_q<T, 1>(q, kc, vc, out, ws, a, Bt, st);
+    case 64: return mx_launch_attn_q<T, 2>(q, kc, vc, out, ws, a, Bt, st);
+    default: return mx_launch_attn_q<T, 4>(q, kc, vc, out, ws, a, Bt, st);
+  }
 }
 
 }  // namespace photon
@@ -430,7 +852,8 @@ extern "C" size_t photon_mxfp4_decode_attn_workspace_bytes(int32_t Bt, int32_t T
 }
 
 extern "C" int32_t photon_mxfp4_decode_attn_auto_splits(int32_t Bt, int32_t T, int32_t H, int32_t H_kv, int64_t S_max) {
-  return 1;
+  if (Bt <= 0 || T <= 0 || H_kv <= 0 || H < H_kv || S_max <= 0) return 1;
+  return mx_auto_splits(Bt, T, H, H_kv, S_max);
 }
 
 extern "C" int32_t photon_mxfp4_decode_attn(const void* q, int64_t q_stride, const void* k_cache, const void* v_cache, const int32_t* seq_len,
@@ -457,12 +880,10 @@ extern "C" int32_t photon_mxfp4_decode_attn(const void* q, int64_t q_stride, con
     PHOTON_REQUIRE(workspace != nullptr && aligned16(workspace) && workspace_bytes >= need, PHOTON_ERR_WORKSPACE,
                    "%s: n_splits=%d needs a 16-byte aligned workspace of %zu bytes (got %zu)", __func__, n_splits, need, workspace_bytes);
   }
-  hipStream_t st = (hipStream_t)stream;
-  const int d_p = photon_kv_row_elems(d_h);
-#define MX_ATTN(T_, NB)                                                                                                    \
-  PHOTON_LAUNCH(KC_COARSE_ATTN, st, (mxfp4_attn_kernel<T_, NB>), dim3((unsigned)(Bt * T * H)), dim3(64), 0, st, (const T_*)q, q_stride, \
-                (const uint8_t*)k_cache, (const uint8_t*)v_cache, seq_len, n_new, (T_*)out, T, H, H_kv, d_h, S_max, scale * LOG2E)
-#define MX_ATTN_NB(T_) do { if (d_p == 32) MX_ATTN(T_, 1); else if (d_p == 64) MX_ATTN(T_, 2); else MX_ATTN(T_, 4); } while (0)
-  if (dt == PHOTON_F32) MX_ATTN_NB(float); else MX_ATTN_NB(bf16_t);
-  return check_launch("mxfp4_attn_kernel");
+  MxQueries a;
+  a.seq_len = seq_len; a.n_new = n_new; a.q_stride = q_stride; a.S_max = S_max;
+  a.T = T; a.H = H; a.H_kv = H_kv; a.d_h = d_h; a.group = H / H_kv; a.groups = 1; a.n_splits = n_splits;
+  a.scale_log2e = scale * LOG2E;
+  if (dt == PHOTON_F32) return mx_launch_attn_t<float>(q, k_cache, v_cache, out, workspace, a, Bt, (hipStream_t)stream);
+  return mx_launch_attn_t<bf16_t>(q, k_cache, v_cache, out, workspace, a, Bt, (hipStream_t)stream);
 }
