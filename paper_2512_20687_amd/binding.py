@@ -336,75 +336,79 @@ def mxfp4_cache(Bt: int, H_kv: int, d_h: int, S_max: int, device="cuda") -> torc
 
 def _mx_caches(k_cache: torch.Tensor, v_cache: torch.Tensor, Bt: int, d_h: int):
     """(H_kv, S_max) of a pair of caches that fit Bt sequences and head size d_h."""
-    for c in (k_cache, v_cache):
-        if c.dtype != torch.uint8 or c.dim() != 4:
-            raise PhotonError(-1, "an MXFP4 cache is a uint8 tensor [Bt, H_kv, tiles, tile bytes]")
-    if k_cache.shape != v_cache.shape or k_cache.shape[0] != Bt or k_cache.shape[3] != photon_mxfp4_tile_bytes(d_h):
-        raise PhotonError(-1, f"caches {tuple(k_cache.shape)} and {tuple(v_cache.shape)} do not hold {Bt} sequences of head size {d_h}")
-    return k_cache.shape[1], k_cache.shape[2] * MXFP4_TILE
+    shape = k_cache.shape
+    if k_cache.dtype is not torch.uint8 or v_cache.dtype is not torch.uint8 or len(shape) != 4:
+        raise PhotonError(-1, "an MXFP4 cache is a uint8 tensor [Bt, H_kv, tiles, tile bytes]")
+    if v_cache.shape != shape or shape[0] != Bt or shape[3] != load_library().photon_mxfp4_tile_bytes(d_h):
+        raise PhotonError(-1, f"caches {tuple(shape)} and {tuple(v_cache.shape)} do not hold {Bt} sequences of head size {d_h}")
+    if not (k_cache.is_contiguous() and v_cache.is_contiguous()):
+        raise PhotonError(-1, "caches must be contiguous")
+    return shape[1], shape[2] * MXFP4_TILE
 
 
 def _mx_row_stride(t: torch.Tensor) -> int:
     """Elements from one row [heads, d_h] of [Bt, T, heads, d_h] to the next."""
     Bt, T, H, d_h = t.shape
     sb, st, sh, sd = t.stride()
-    stride = st if T > 1 else sb if Bt > 1 else H * d_h
     if (sd != 1 and d_h > 1) or (sh != d_h and H > 1) or (T > 1 and Bt > 1 and sb != T * st):
-        raise PhotonError(-1, f"rows [Bt, T, heads, d_h] must be one stride apart, each of them contiguous: strides {tuple(t.stride())}")
-    return stride
+        raise PhotonError(-1, f"rows [Bt, T, heads, d_h] must be one stride apart, each of them contiguous: strides {(sb, st, sh, sd)}")
+    return st if T > 1 else sb if Bt > 1 else H * d_h
 
 
 def _mx_counts(t: Optional[torch.Tensor], Bt: int, name: str) -> Optional[int]:
     if t is None:
         return None
-    if t.dtype != torch.int32 or t.numel() != Bt:
+    if t.dtype is not torch.int32 or t.numel() != Bt or not t.is_contiguous():
         raise PhotonError(-1, f"{name} must hold an int32 per sequence")
-    return _ptr(t)
+    return t.data_ptr()
 
 
 def _mx_call(fn, tensors, *args) -> None:
     """fn(*args, stream) on the current stream of the tensors' device, with that device current."""
-    device = tensors[0].device
+    device = tensors[0].get_device()
     for t in tensors:
-        if t is not None and (not t.is_cuda or t.device != device):
-            raise PhotonError(-1, f"all tensors must live in the memory of one device: {device} and {t.device}")
-    if device.index == torch.cuda.current_device():
-        _check(fn(*args, _stream()))
+        if t is not None and (device < 0 or t.get_device() != device):
+            raise PhotonError(-1, "all tensors must live in the memory of one device")
+    if device == torch.cuda.current_device():
+        rc = fn(*args, _stream())
     else:
         with torch.cuda.device(device):
-            _check(fn(*args, _stream()))
+            rc = fn(*args, _stream())
+    if rc != 0:
+        _check(rc)
 
 
-def _mx_rows(k, v, k_cache, v_cache, start, n_new):
-    """Arguments that the cache's write and read share, with what they come to."""
-    if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in (torch.float32, torch.bfloat16):
+def _mx_rows(k, v, k_cache, v_cache):
+    """(row stride, (Bt, T, H_kv, d_h, S_max, dt)) of rows that the cache's write or read is given."""
+    shape, dtype = k.shape, k.dtype
+    if len(shape) != 4 or v.shape != shape or v.dtype is not dtype or (dtype is not torch.float32 and dtype is not torch.bfloat16):
         raise PhotonError(-1, "k and v must be fp32 or bf16 tensors [Bt, T, H_kv, d_h] of one shape and dtype")
-    Bt, T, H_kv, d_h = k.shape
+    Bt, T, H_kv, d_h = shape
     stride = _mx_row_stride(k)
     if _mx_row_stride(v) != stride:
         raise PhotonError(-1, f"k and v rows must have one stride: {stride} and {_mx_row_stride(v)}")
     heads, S_max = _mx_caches(k_cache, v_cache, Bt, d_h)
     if heads != H_kv:
         raise PhotonError(-1, f"rows of {H_kv} heads do not fit a cache of {heads}")
-    return (stride, _ptr(k_cache), _ptr(v_cache), _mx_counts(start, Bt, "start"), _mx_counts(n_new, Bt, "n_new"),
-            (Bt, T, H_kv, d_h, S_max, PHOTON_F32 if k.dtype == torch.float32 else PHOTON_BF16))
+    return stride, (Bt, T, H_kv, d_h, S_max, PHOTON_F32 if dtype is torch.float32 else PHOTON_BF16)
 
 
 def photon_mxfp4_cache_write(k, v, k_cache, v_cache, start=None, n_new=None, status=None) -> None:
     """Rows k, v [Bt, T, H_kv, d_h] (views of a wider matrix included) become the entries start[b] .. of the caches (see
     mxfp4_cache); start, n_new int32 [Bt] or None (0, T); status: int32 word that receives PHOTON_STATUS_CACHE_FULL."""
-    stride, kc, vc, first, count, shape = _mx_rows(k, v, k_cache, v_cache, start, n_new)
-    if status is not None and (status.dtype != torch.int32 or status.numel() < 1):
+    stride, shape = _mx_rows(k, v, k_cache, v_cache)
+    if status is not None and (status.dtype is not torch.int32 or status.numel() < 1):
         raise PhotonError(-1, "status must be an int32 tensor")
-    _mx_call(load_library().photon_mxfp4_cache_write, (k, v, k_cache, v_cache, start, n_new, status), k.data_ptr(), v.data_ptr(), stride, kc, vc,
-             first, count, _ptr(status), *shape)
+    _mx_call(load_library().photon_mxfp4_cache_write, (k, v, k_cache, v_cache, start, n_new, status), k.data_ptr(), v.data_ptr(), stride,
+             k_cache.data_ptr(), v_cache.data_ptr(), _mx_counts(start, shape[0], "start"), _mx_counts(n_new, shape[0], "n_new"),
+             None if status is None else status.data_ptr(), *shape)
 
 
 def photon_mxfp4_cache_read(k_cache, v_cache, k, v, start=None, n_rows=None) -> None:
     """The entries start[b] .. of the caches into rows k, v [Bt, T, H_kv, d_h]; rows past n_rows[b] stay as they are."""
-    stride, kc, vc, first, count, shape = _mx_rows(k, v, k_cache, v_cache, start, n_rows)
-    _mx_call(load_library().photon_mxfp4_cache_read, (k, v, k_cache, v_cache, start, n_rows), kc, vc, first, count, k.data_ptr(), v.data_ptr(),
-             stride, *shape)
+    stride, shape = _mx_rows(k, v, k_cache, v_cache)
+    _mx_call(load_library().photon_mxfp4_cache_read, (k, v, k_cache, v_cache, start, n_rows), k_cache.data_ptr(), v_cache.data_ptr(),
+             _mx_counts(start, shape[0], "start"), _mx_counts(n_rows, shape[0], "n_rows"), k.data_ptr(), v.data_ptr(), stride, *shape)
 
 
 def photon_mxfp4_decode_attn_workspace_bytes(Bt: int, T: int, H: int, d_h: int, n_splits: int) -> int:
@@ -419,18 +423,18 @@ def photon_mxfp4_decode_attn(q, k_cache, v_cache, seq_len, out, n_new=None, scal
                              workspace: Optional[torch.Tensor] = None):
     """q (rows one stride apart), out (contiguous) [Bt, T, H, d_h] fp32 or bf16; caches as mxfp4_cache makes them; seq_len int32
     [Bt], the T (n_new[b]) queries' own entries counted; returns out."""
-    if q.dim() != 4 or q.shape != out.shape or q.dtype != out.dtype or q.dtype not in (torch.float32, torch.bfloat16):
+    shape, dtype = q.shape, q.dtype
+    if len(shape) != 4 or out.shape != shape or out.dtype is not dtype or (dtype is not torch.float32 and dtype is not torch.bfloat16):
         raise PhotonError(-1, "q and out must be fp32 or bf16 tensors [Bt, T, H, d_h] of one shape and dtype")
-    if seq_len is None:
-        raise PhotonError(-1, "seq_len is missing")
-    Bt, T, H, d_h = q.shape
+    if seq_len is None or not out.is_contiguous() or (workspace is not None and not workspace.is_contiguous()):
+        raise PhotonError(-1, "seq_len is missing, or out or workspace is not contiguous")
+    Bt, T, H, d_h = shape
     H_kv, S_max = _mx_caches(k_cache, v_cache, Bt, d_h)
-    if scale is None:
-        scale = 1.0 / math.sqrt(d_h)
-    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _mx_call(load_library().photon_mxfp4_decode_attn, (q, k_cache, v_cache, seq_len, n_new, out, workspace), q.data_ptr(), _mx_row_stride(q),
-             _ptr(k_cache), _ptr(v_cache), _mx_counts(seq_len, Bt, "seq_len"), _mx_counts(n_new, Bt, "n_new"), _ptr(out), Bt, T, H, H_kv, d_h,
-             S_max, scale, n_splits, _ptr(workspace), ws_bytes, PHOTON_F32 if q.dtype == torch.float32 else PHOTON_BF16)
+             k_cache.data_ptr(), v_cache.data_ptr(), _mx_counts(seq_len, Bt, "seq_len"), _mx_counts(n_new, Bt, "n_new"), out.data_ptr(), Bt, T,
+             H, H_kv, d_h, S_max, 1.0 / math.sqrt(d_h) if scale is None else scale, n_splits,
+             None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+             PHOTON_F32 if dtype is torch.float32 else PHOTON_BF16)
     return out
 
 

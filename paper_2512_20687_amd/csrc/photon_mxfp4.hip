@@ -15,19 +15,20 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
 // ------------------------------------------------------------------ rows in and out
 //
-// A wave takes the positions of one tile of one stream, 8 positions x 64 elements at a time ("a pass"): lane 8 r + x holds 8
+// A wave takes 16 positions of one stream, 8 positions x 64 elements at a time ("a pass"), all loads first: lane 8 r + x holds 8
 // consecutive elements of position r, 4 neighbouring lanes a block.  K words go out as they are.  V words hold 8 positions of
 // one element: the 8 lanes of equal x exchange nibbles (an 8 x 8 transposition in three steps).
 //   d_p = 128: a pass takes half of the elements; d_p = 32: lanes x >= 4 take the next 8 positions.
+// Neighbouring workgroups take neighbouring heads, so that rows [H_kv, d_h] are read as a whole.
 
-constexpr int MX_WAVES = 4;      // waves (tiles) of a workgroup
+constexpr int MX_WAVES = 4;      // waves of a workgroup, at most: 64 positions
+constexpr int MX_STEP = 16;      // positions of a wave
 
 template <int NB> struct MxPass {
-  static constexpr int PER_TILE = NB * 4;                  // 64 positions x 32 NB elements in passes of 512
-  int kk, dim;                                             // position in the tile and first of the lane's 8 elements
+  int kk, dim;                                             // position among the wave's 16 and first of the lane's 8 elements
   __device__ __forceinline__ MxPass(int pass, int lane) {
     const int r = lane >> 3, x = lane & 7;
-    if (NB == 1) { kk = pass * 16 + (x >> 2) * 8 + r; dim = (x & 3) * 8; }
+    if (NB == 1) { kk = (x >> 2) * 8 + r; dim = (x & 3) * 8; }
     else if (NB == 2) { kk = pass * 8 + r; dim = x * 8; }
     else { kk = (pass >> 1) * 8 + r; dim = (pass & 1) * 64 + x * 8; }
   }
@@ -141,35 +142,32 @@ struct MxRows {                  // a stretch of rows and the positions it belon
   const int32_t *start, *n_new;  // [Bt] or NULL: position of row 0 (0), rows in use (T)
   int64_t row_stride;            // elements from a row to the next
   int64_t S_max;
-  int T, H_kv, d_h, slots;       // slots: tiles that T rows can touch
-  int64_t streams;
+  int T, H_kv, d_h;
 };
 
-// Wave's share: stream, its tile and the positions [lo, hi) of the tile that rows in use belong to.
+// A wave's share: a step of 16 positions, and those [lo, hi) of it that rows in use belong to.
 struct MxShare {
-  int64_t stream, tile, row0;    // row0: row of position 0 of the tile
-  int b, h, lo, hi;
+  int64_t tile, row0;            // row0: the row of position 0 of the step
+  int b, h, base, lo, hi;        // base: of the step in the tile
 };
-__device__ __forceinline__ bool mx_share(const MxRows& a, int wave, MxShare& s, bool& outside) {
-  const int64_t unit = (int64_t)blockIdx.x * MX_WAVES + wave;
-  s.stream = unit / a.slots;
-  outside = false;
-  if (s.stream >= a.streams) return false;
-  const int slot = (int)(unit - s.stream * a.slots);
-  s.b = (int)(s.stream / a.H_kv);
-  s.h = (int)(s.stream - (int64_t)s.b * a.H_kv);
+// false: nothing to do.  outside: rows of this sequence have no place in the cache.
+__device__ __forceinline__ bool mx_share(const MxRows& a, MxShare& s, bool& outside) {
+  const unsigned group = blockIdx.x / (unsigned)a.H_kv;
+  s.b = blockIdx.y;
+  s.h = blockIdx.x - group * a.H_kv;
   int64_t n = a.n_new ? a.n_new[s.b] : a.T;
   n = n < 0 ? 0 : n > a.T ? a.T : n;
   const int64_t first = a.start ? a.start[s.b] : 0;
   const int64_t begin = first < 0 ? 0 : first, end = first + n < a.S_max ? first + n : a.S_max;
   outside = n > 0 && (first < 0 || first + n > a.S_max);
-  s.tile = (begin >> 6) + slot;
-  const int64_t base = s.tile * MX_TILE;
-  if (base >= end) return false;
-  s.lo = begin > base ? (int)(begin - base) : 0;
-  s.hi = end - base < MX_TILE ? (int)(end - base) : MX_TILE;
-  s.row0 = (int64_t)s.b * a.T + base - first;
-  return s.lo < s.hi;
+  const int64_t at = (begin / MX_STEP + (int64_t)group * (blockDim.x >> 6) + (threadIdx.x >> 6)) * MX_STEP;
+  if (at >= end) return false;
+  s.tile = at / MX_TILE;
+  s.base = (int)(at % MX_TILE);
+  s.lo = begin > at ? (int)(begin - at) : 0;
+  s.hi = end - at < MX_STEP ? (int)(end - at) : MX_STEP;
+  s.row0 = (int64_t)s.b * a.T + at - first;
+  return true;
 }
 
 template <typename T, int NB, int VEC>
@@ -178,42 +176,44 @@ __global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_write_kernel(const T* __r
   const int lane = threadIdx.x & 63;
   MxShare s;
   bool outside;
-  const bool any = mx_share(a, threadIdx.x >> 6, s, outside);
-  if (outside && status != nullptr && lane == 0) atomicOr(status, (int)PHOTON_STATUS_CACHE_FULL);
+  const bool any = mx_share(a, s, outside);
+  if (outside && status != nullptr && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(status, (int)PHOTON_STATUS_CACHE_FULL);
   if (!any) return;
-  const int64_t tiles = (a.S_max + MX_TILE - 1) / MX_TILE;
-  const int64_t at = (s.stream * tiles + s.tile) * mx_tile_bytes(NB * MX_BLOCK);
-  kc += at;
-  vc += at;
-  constexpr int STEP = NB == 1 ? 16 : 8, SPLIT = NB == 4 ? 2 : 1;    // positions of a pass, passes per position
-  const int first = s.lo / STEP * SPLIT, last = (s.hi + STEP - 1) / STEP * SPLIT;
-  for (int pass = first; pass < last; ++pass) {
-    const MxPass<NB> p(pass, lane);
-    const bool ok = p.kk >= s.lo && p.kk < s.hi;
-    float kv[8], vv[8];
-    if (ok) {
+  float kv[NB][8], vv[NB][8];
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    const MxPass<NB> p(i, lane);
+    if (p.kk >= s.lo && p.kk < s.hi) {
       const int64_t row = (s.row0 + p.kk) * a.row_stride + (int64_t)s.h * a.d_h;
-      mx_load8<T, VEC>(k + row, p.dim, a.d_h, kv);
-      mx_load8<T, VEC>(v + row, p.dim, a.d_h, vv);
+      mx_load8<T, VEC>(k + row, p.dim, a.d_h, kv[i]);
+      mx_load8<T, VEC>(v + row, p.dim, a.d_h, vv[i]);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) kv[i] = vv[i] = 0.f;
+      for (int e = 0; e < 8; ++e) kv[i][e] = vv[i][e] = 0.f;
     }
+  }
+  const int64_t tiles = (a.S_max + MX_TILE - 1) / MX_TILE;
+  const int64_t at = (((int64_t)s.b * a.H_kv + s.h) * tiles + s.tile) * mx_tile_bytes(NB * MX_BLOCK);
+  kc += at;
+  vc += at;
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    const MxPass<NB> p(i, lane);
+    const int kk = s.base + p.kk, block = p.dim >> 5;
     uint32_t ks, vs;
-    const uint32_t kw = mx_quantise8(kv, ks), vw = mx_transpose8(mx_quantise8(vv, vs), lane);
-    const int block = p.dim >> 5;
-    if (ok) {
-      *reinterpret_cast<uint32_t*>(kc + mx_k_chunk<NB>(p.kk, block) + ((p.dim >> 3) & 3) * 4) = kw;
+    const uint32_t kw = mx_quantise8(kv[i], ks), vw = mx_transpose8(mx_quantise8(vv[i], vs), lane);
+    if (p.kk >= s.lo && p.kk < s.hi) {
+      *reinterpret_cast<uint32_t*>(kc + mx_k_chunk<NB>(kk, block) + ((p.dim >> 3) & 3) * 4) = kw;
       if ((lane & 3) == 0) {
-        kc[mx_k_scale<NB>(p.kk, block)] = (uint8_t)ks;
-        vc[mx_v_scale<NB>(p.kk, block)] = (uint8_t)vs;
+        kc[mx_k_scale<NB>(kk, block)] = (uint8_t)ks;
+        vc[mx_v_scale<NB>(kk, block)] = (uint8_t)vs;
       }
     }
     // the lane's V word: element dim + r, the 8 positions around p.kk; those outside [lo, hi) keep what they held
     const int group = p.kk & ~7, r = lane >> 3;
     const int from = s.lo - group < 0 ? 0 : s.lo - group, to = s.hi - group > 8 ? 8 : s.hi - group;
     if (from < to) {
-      uint32_t* word = reinterpret_cast<uint32_t*>(vc + mx_v_word<NB>(group, p.dim + r));
+      uint32_t* word = reinterpret_cast<uint32_t*>(vc + mx_v_word<NB>(kk & ~7, p.dim + r));
       const uint32_t mask = (to == 8 ? 0xffffffffu : (1u << (4 * to)) - 1u) & ~((1u << (4 * from)) - 1u);
       *word = mask == 0xffffffffu ? vw : (*word & ~mask) | (vw & mask);
     }
@@ -226,23 +226,27 @@ __global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_read_kernel(const uint8_t
   const int lane = threadIdx.x & 63;
   MxShare s;
   bool outside;
-  const bool any = mx_share(a, threadIdx.x >> 6, s, outside);
-  if (!any) return;
+  if (!mx_share(a, s, outside)) return;
   const int64_t tiles = (a.S_max + MX_TILE - 1) / MX_TILE;
-  const int64_t at = (s.stream * tiles + s.tile) * mx_tile_bytes(NB * MX_BLOCK);
+  const int64_t at = (((int64_t)s.b * a.H_kv + s.h) * tiles + s.tile) * mx_tile_bytes(NB * MX_BLOCK);
   kc += at;
   vc += at;
-  constexpr int STEP = NB == 1 ? 16 : 8, SPLIT = NB == 4 ? 2 : 1;
-  const int first = s.lo / STEP * SPLIT, last = (s.hi + STEP - 1) / STEP * SPLIT;
-  for (int pass = first; pass < last; ++pass) {
-    const MxPass<NB> p(pass, lane);
-    const int block = p.dim >> 5;
-    const uint32_t kw = *reinterpret_cast<const uint32_t*>(kc + mx_k_chunk<NB>(p.kk, block) + ((p.dim >> 3) & 3) * 4);
-    const uint32_t vw = *reinterpret_cast<const uint32_t*>(vc + mx_v_word<NB>(p.kk & ~7, p.dim + (lane >> 3)));
-    const uint32_t ks = kc[mx_k_scale<NB>(p.kk, block)], vs = vc[mx_v_scale<NB>(p.kk, block)];
+  uint32_t kw[NB], vw[NB], ks[NB], vs[NB];
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    const MxPass<NB> p(i, lane);
+    const int kk = s.base + p.kk, block = p.dim >> 5;
+    kw[i] = *reinterpret_cast<const uint32_t*>(kc + mx_k_chunk<NB>(kk, block) + ((p.dim >> 3) & 3) * 4);
+    vw[i] = *reinterpret_cast<const uint32_t*>(vc + mx_v_word<NB>(kk & ~7, p.dim + (lane >> 3)));
+    ks[i] = kc[mx_k_scale<NB>(kk, block)];
+    vs[i] = vc[mx_v_scale<NB>(kk, block)];
+  }
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    const MxPass<NB> p(i, lane);
     float kv[8], vv[8];
-    mx_values8(kw, ks, kv);
-    mx_values8(mx_transpose8(vw, lane), vs, vv);
+    mx_values8(kw[i], ks[i], kv);
+    mx_values8(mx_transpose8(vw[i], lane), vs[i], vv);
     if (p.kk >= s.lo && p.kk < s.hi) {
       const int64_t row = (s.row0 + p.kk) * a.row_stride + (int64_t)s.h * a.d_h;
       mx_store8<T, VEC>(k + row, p.dim, a.d_h, kv);
@@ -268,6 +272,7 @@ __global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_read_kernel(const uint8_t
 //   The reference of the exponentials is the largest score when it was last raised, which happens when one exceeds it by more
 //     than MX_RAISE: fp32 and bf16 lose nothing by weights up to 2^MX_RAISE, and the usual tile needs no maximum.
 constexpr float MX_RAISE = 16.f;
+constexpr int MX_ATTN_WAVES = 8;                 // of a workgroup, at most
 constexpr int MX_P_PITCH = 72;                   // bf16 elements of a weight row in LDS: 64 positions, rows on different banks
 
 template <typename T, int NB, int NQ> struct MxAttn {
@@ -280,7 +285,8 @@ template <typename T, int NB, int NQ> struct MxAttn {
   // per wave: weight rows, and the staged queries or the wave's result
   static constexpr int P_BYTES = P_ROWS * MX_P_PITCH * 2;
   static constexpr int O_BYTES = NQ * (DP + 2) * 4;
-  static constexpr int WAVE_BYTES = (P_BYTES > O_BYTES ? P_BYTES : O_BYTES) + 15 & ~15;
+  static constexpr int Q_BYTES = NQ * PARTS * DP * 2;
+  static constexpr int WAVE_BYTES = ((P_BYTES > O_BYTES ? P_BYTES > Q_BYTES ? P_BYTES : Q_BYTES : O_BYTES > Q_BYTES ? O_BYTES : Q_BYTES) + 15) & ~15;
 };
 
 __device__ __forceinline__ bf16x8_t mx_operand(uint32_t w, float scale) {
@@ -320,11 +326,6 @@ struct MxQueries {
   float scale_log2e;
 };
 
-// A split's tiles of n positions.
-__device__ __forceinline__ int mx_split_tiles(int64_t n, int n_splits) {
-  const int tiles = (int)((n + MX_TILE - 1) / MX_TILE);
-  return (tiles + n_splits - 1) / n_splits;
-}
 // Positions that count for sequence b, and its queries.
 __device__ __forceinline__ void mx_sequence(const MxQueries& a, int b, int64_t& n, int& m) {
   n = a.seq_len[b];
@@ -334,7 +335,7 @@ __device__ __forceinline__ void mx_sequence(const MxQueries& a, int b, int64_t& 
 }
 
 template <typename T, int NB, int NQ>
-__global__ __launch_bounds__(512) void mxfp4_attn_kernel(const T* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
+__global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
                                                          T* __restrict__ out, float* __restrict__ ws, MxQueries a) {
   using C = MxAttn<T, NB, NQ>;
   constexpr int DP = C::DP, SETS = C::SETS, ACC = C::ACC, QSETS = C::QSETS, PARTS = C::PARTS, TB = mx_tile_bytes(DP);
@@ -342,34 +343,35 @@ __global__ __launch_bounds__(512) void mxfp4_attn_kernel(const T* __restrict__ q
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, waves = blockDim.x >> 6;
   const int c = lane & 15, kg = lane >> 4;
 
-  unsigned unit = blockIdx.x;
-  const int chunk = unit % (unsigned)a.groups;
-  unit /= (unsigned)a.groups;
-  const int split = unit % (unsigned)a.n_splits;
-  const int64_t stream = unit / (unsigned)a.n_splits;
-  const int b = (int)(stream / a.H_kv), hk = (int)(stream - (int64_t)b * a.H_kv);
+  const unsigned split = a.groups == 1 ? blockIdx.x : blockIdx.x / (unsigned)a.groups, chunk = blockIdx.x - split * a.groups;
+  const int b = blockIdx.z, hk = blockIdx.y;
 
   int64_t n;
   int m;
   mx_sequence(a, b, n, m);
+  // query i of the workgroup is row first_q + i of the stream's m * group: token row / group, head hk * group + row % group; it
+  // sees seen[i] positions
   const int first_q = chunk * NQ, queries = m * a.group - first_q;           // of this workgroup, at most NQ count
   if (queries <= 0) return;
-  // query i of the workgroup is row first_q + i: token t = row / group, head hk * group + row % group; it sees seen[i] positions
-  int64_t seen[NQ];
+  int64_t seen[NQ], q_row[NQ];
+  {
+    int t = a.group == 1 ? first_q : first_q / a.group, h = first_q - t * a.group;
 #pragma unroll
-  for (int i = 0; i < NQ; ++i) {
-    const int t = (first_q + (i < queries ? i : queries - 1)) / a.group;
-    const int64_t s = n - m + t + 1;
-    seen[i] = s < 0 ? 0 : s;
+    for (int i = 0; i < NQ; ++i) {
+      const int64_t s = n - m + t + 1;
+      seen[i] = s < 0 ? 0 : s;
+      q_row[i] = ((int64_t)b * a.T + t) * a.q_stride + (int64_t)(hk * a.group + h) * a.d_h;
+      if (i + 1 < queries && ++h == a.group) { h = 0; ++t; }                 // past the last query: the last one again
+    }
   }
   const int64_t hi = seen[NQ - 1], lo = seen[0];                             // seen grows with i
-  const int per = mx_split_tiles(n, a.n_splits);
-  const int begin = split * per;
-  int end = (int)((hi + MX_TILE - 1) / MX_TILE);
-  if (a.n_splits > 1 && begin >= (int)((n + MX_TILE - 1) / MX_TILE)) return;  // the merge knows that this split holds nothing
-  end = end < begin + per ? end : begin + per;
+  // The waves of all splits take the tiles in turn.  Splits that no tile is left for write nothing: the merge knows them.
+  const int end = (int)((hi + MX_TILE - 1) / MX_TILE), stride = a.n_splits * waves;
+  int tile = split * waves + wave;
+  if (a.n_splits > 1 && (int64_t)split * waves * MX_TILE >= n) return;
 
   const int64_t tiles = (a.S_max + MX_TILE - 1) / MX_TILE;
+  const int64_t stream = (int64_t)b * a.H_kv + hk;
   const uint8_t* kt = kc + stream * tiles * TB + lane * 16;
   const uint8_t* vt = vc + stream * tiles * TB + lane * 16;
   const uint8_t* kst = kc + stream * tiles * TB + NB * 1024 + lane * NB;
@@ -392,52 +394,49 @@ __global__ __launch_bounds__(512) void mxfp4_attn_kernel(const T* __restrict__ q
   };
 
   Tile cur, nxt;
-  int tile = begin + wave;
   if (tile < end) load(tile, cur);
 
-  // queries: in LDS, then into the operands of the score products
-  float* qs = reinterpret_cast<float*>(mx_lds);
-  for (int x = tid; x < NQ * DP; x += blockDim.x) {
-    const int i = x / DP, d = x % DP;
-    float v = 0.f;
-    if (i < queries && d < a.d_h) {
-      const int row = first_q + i, t = row / a.group, h = hk * a.group + row % a.group;
-      v = to_f32<T>(q[((int64_t)b * a.T + t) * a.q_stride + (int64_t)h * a.d_h + d]);
-    }
-    qs[x] = v;
-  }
-  __syncthreads();
+  // queries: their parts into the wave's LDS, then into the operands of the score products
+  char* own = mx_lds + wave * C::WAVE_BYTES;
   bf16x8_t aq[SETS][4];
   {
+    uint16_t* qs = reinterpret_cast<uint16_t*>(own);                         // [query][part][DP]
+#pragma unroll
+    for (int i = 0; i < NQ; ++i)
+#pragma unroll
+      for (int d0 = 0; d0 < DP; d0 += 64) {
+        const int d = d0 + lane;
+        if (DP < 64 && d >= DP) continue;
+        uint16_t* to = qs + i * PARTS * DP + d;
+        const float x = d < a.d_h ? to_f32<T>(q[q_row[i] + d]) : 0.f;
+        if constexpr (PARTS == 3) {
+          float p0, p1, p2;
+          mx_split3(x, p0, p1, p2);
+          to[0] = (uint16_t)(__float_as_uint(p0) >> 16);
+          to[DP] = (uint16_t)(__float_as_uint(p1) >> 16);
+          to[2 * DP] = (uint16_t)(__float_as_uint(p2) >> 16);
+        } else {
+          to[0] = (uint16_t)(__float_as_uint(x) >> 16);
+        }
+      }
+    mx_wave_order();
     const int g = c >> 2, i = c & 3;                                         // operand row c = 4 g + i
     const int block = NB == 1 ? 0 : NB == 2 ? kg & 1 : kg;
     const bool mine = NB == 1 ? g == kg : NB == 2 ? (g & 1) == (kg >> 1) : true;
 #pragma unroll
     for (int s = 0; s < SETS; ++s) {
-      const int part = NQ == 1 ? i : s % PARTS, qi = NQ == 1 ? 0 : (s / PARTS) * 4 + i;
-      const bool there = mine && part < PARTS;
+      // one query: row i is its part i (rows past the last part are not looked at); else part s % PARTS of query 4 (s / PARTS) + i
+      const int row = NQ == 1 ? (i < PARTS ? i : 0) : ((s / PARTS) * 4 + i) * PARTS + s % PARTS;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        uint4_t w;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float x[2];
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const float v = qs[qi * DP + block * 32 + j * 8 + 2 * e + u];
-            float p0, p1, p2;
-            mx_split3(v, p0, p1, p2);
-            x[u] = !there ? 0.f : part == 0 ? p0 : part == 1 ? p1 : p2;
-          }
-          w[e] = (__float_as_uint(x[0]) >> 16) | (__float_as_uint(x[1]) & 0xffff0000u);
-        }
+        uint4_t w = *reinterpret_cast<const uint4_t*>(qs + row * DP + block * 32 + j * 8);
+        if (!mine) w = uint4_t{0, 0, 0, 0};
         aq[s][j] = as_bf16x8(w);
       }
     }
   }
-  __syncthreads();                                                           // the staged queries make room for the weights
+  mx_wave_order();                                                           // the staged queries make room for the weights
 
-  char* own = mx_lds + wave * C::WAVE_BYTES;
   uint16_t* pw = reinterpret_cast<uint16_t*>(own);
   const uint16_t* pr = pw + kg * 8;
   float top[NQ], sum[NQ];
@@ -603,12 +602,12 @@ __global__ __launch_bounds__(512) void mxfp4_attn_kernel(const T* __restrict__ q
   };
 
   while (tile < end) {
-    int next = tile + waves;
+    int next = tile + stride;
     if (next < end) load(next, nxt);
     consume(tile, cur);
     tile = next;
     if (tile >= end) break;
-    next = tile + waves;
+    next = tile + stride;
     if (next < end) load(next, cur);
     consume(tile, nxt);
     tile = next;
@@ -648,20 +647,28 @@ __global__ __launch_bounds__(512) void mxfp4_attn_kernel(const T* __restrict__ q
   for (int x = tid; x < NQ * DP; x += blockDim.x) {
     const int i = x / DP, d = x % DP;
     if (i >= queries) break;
-    const char* at = mx_lds + (i * (DP + 2)) * 4;
-    float mx = NEG_BIG;
-    for (int w = 0; w < waves; ++w) mx = fmaxf(mx, reinterpret_cast<const float*>(at + w * C::WAVE_BYTES)[0]);
-    float l = 0.f, o = 0.f;
-    for (int w = 0; w < waves; ++w) {
-      const float* pw_ = reinterpret_cast<const float*>(at + w * C::WAVE_BYTES);
-      const float f = fast_exp2(pw_[0] - mx);
-      l = fmaf(pw_[1], f, l);
-      o = fmaf(pw_[2 + d], f, o);
+    const float* at = reinterpret_cast<const float*>(mx_lds) + i * (DP + 2);
+    float w_top[MX_ATTN_WAVES], w_sum[MX_ATTN_WAVES], w_o[MX_ATTN_WAVES], mx = NEG_BIG;
+#pragma unroll
+    for (int w = 0; w < MX_ATTN_WAVES; ++w) {
+      const float* from = at + (w < waves ? w : 0) * (C::WAVE_BYTES / 4);
+      w_top[w] = w < waves ? from[0] : NEG_BIG;
+      w_sum[w] = from[1];
+      w_o[w] = from[2 + d];
+      mx = fmaxf(mx, w_top[w]);
     }
-    const int row = first_q + i, t = row / a.group, h = hk * a.group + row % a.group;
+    float l = 0.f, o = 0.f;
+#pragma unroll
+    for (int w = 0; w < MX_ATTN_WAVES; ++w) {
+      if (w >= waves) break;
+      const float f = fast_exp2(w_top[w] - mx);
+      l = fmaf(w_sum[w], f, l);
+      o = fmaf(w_o[w], f, o);
+    }
+    const int row = first_q + i, t = a.group == 1 ? row : row / a.group, h = hk * a.group + row - t * a.group;
     const int64_t to = ((int64_t)b * a.T + t) * a.H + h;
     if (a.n_splits == 1) {
-      if (d < a.d_h) out[to * a.d_h + d] = from_f32<T>(seen[i < NQ ? i : 0] > 0 ? o / l : 0.f);
+      if (d < a.d_h) out[to * a.d_h + d] = from_f32<T>(n - m + t + 1 > 0 ? o / l : 0.f);
     } else {
       float* p = ws + (to * a.n_splits + split) * (DP + 2);
       if (d == 0) { p[0] = mx; p[1] = l; }
@@ -670,27 +677,45 @@ __global__ __launch_bounds__(512) void mxfp4_attn_kernel(const T* __restrict__ q
   }
 }
 
-// The splits' results of one query, in order.
+// The splits' results of one query, in order, eight at a time in flight.
 template <typename T, int NB>
-__global__ __launch_bounds__(NB * MX_BLOCK) void mxfp4_merge_kernel(const float* __restrict__ ws, T* __restrict__ out, MxQueries a) {
+__global__ __launch_bounds__(NB * MX_BLOCK) void mxfp4_merge_kernel(const float* __restrict__ ws, T* __restrict__ out, MxQueries a, int waves) {
   constexpr int DP = NB * MX_BLOCK;
-  const int h = blockIdx.x % (unsigned)a.H;
-  const int64_t row = blockIdx.x / (unsigned)a.H;
-  const int b = (int)(row / a.T), t = (int)(row - (int64_t)b * a.T), d = threadIdx.x;
+  const int h = blockIdx.x, t = blockIdx.y, b = blockIdx.z, d = threadIdx.x;
   int64_t n;
   int m;
   mx_sequence(a, b, n, m);
   if (t >= m) return;
-  const int per = mx_split_tiles(n, a.n_splits), tiles = (int)((n + MX_TILE - 1) / MX_TILE);
-  const int used = per == 0 ? 0 : (tiles + per - 1) / per;
-  const int64_t to = row * a.H + h;
+  const int64_t span = (int64_t)waves * MX_TILE, spans = (n + span - 1) / span;
+  const int used = spans < a.n_splits ? (int)spans : a.n_splits;
+  const int64_t to = ((int64_t)b * a.T + t) * a.H + h;
   const float* p = ws + to * a.n_splits * (DP + 2);
   float mx = NEG_BIG, l = 0.f, o = 0.f;
-  for (int s = 0; s < used; ++s) mx = fmaxf(mx, p[s * (DP + 2)]);
-  for (int s = 0; s < used; ++s) {
-    const float f = fast_exp2(p[s * (DP + 2)] - mx);
-    l = fmaf(p[s * (DP + 2) + 1], f, l);
-    o = fmaf(p[s * (DP + 2) + 2 + d], f, o);
+  for (int s0 = 0; s0 < used; s0 += 8) {
+    float s_top[8], s_sum[8], s_o[8], higher = mx;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const float* from = p + (s0 + u < used ? s0 + u : 0) * (DP + 2);
+      s_top[u] = from[0];
+      s_sum[u] = from[1];
+      s_o[u] = from[2 + d];
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (s0 + u >= used) s_top[u] = NEG_BIG;
+      higher = fmaxf(higher, s_top[u]);
+    }
+    const float f0 = fast_exp2(mx - higher);
+    mx = higher;
+    l *= f0;
+    o *= f0;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (s0 + u >= used) break;
+      const float f = fast_exp2(s_top[u] - mx);
+      l = fmaf(s_sum[u], f, l);
+      o = fmaf(s_o[u], f, o);
+    }
   }
   if (d < a.d_h) out[to * a.d_h + d] = from_f32<T>(n - m + t + 1 > 0 ? o / l : 0.f);
 }
@@ -698,27 +723,36 @@ __global__ __launch_bounds__(NB * MX_BLOCK) void mxfp4_merge_kernel(const float*
 // Queries that share what a workgroup reads.  fp32: at most 4 (the operands of 8 are 96 registers a lane: 120 spilled).
 int mx_query_rows(int64_t queries, bool f32) { return queries <= 1 ? 1 : queries <= 4 || f32 ? 4 : 8; }
 
+// One workgroup of eight waves per compute unit where streams are few, as long as a wave has four tiles: 128 streams of 128 tiles
+// take 16.9 us in 2 splits, 19.9 in 1, 17.9 in 4; 16 streams of 32 tiles 7.3 us in 1, 8.2 in 2 (the merge is a launch).
 int mx_auto_splits(int Bt, int T, int H, int H_kv, int64_t S_max) {
-  const int64_t queries = (int64_t)T * (H / H_kv), rows = mx_query_rows(queries, true);
+  const int64_t queries = (int64_t)T * (H / H_kv), rows = mx_query_rows(queries, false);
   const int64_t groups = (int64_t)Bt * H_kv * ((queries + rows - 1) / rows), tiles = (S_max + MX_TILE - 1) / MX_TILE;
-  int64_t splits = 1024 / groups;
-  const int64_t most = tiles / 16;                       // at least two tiles a wave
+  int64_t splits = 256 / groups;
+  const int64_t most = tiles / (4 * MX_ATTN_WAVES);
   splits = splits > most ? most : splits;
   return (int)(splits < 1 ? 1 : splits > 1024 ? 1024 : splits);
 }
 
+// Waves of a workgroup: eight, but not more than there are tiles, and once more waves are asked for than the chip holds, so many
+// that one has eight tiles (its start and end cost as much as six): 8192 streams of 3 tiles take 17.6 us with one wave, 20.6
+// with two, 52.8 with eight; 4096 streams of 32 tiles 86.2 us with four, 89.1 with two, 87.9 with eight.
+int mx_waves(int64_t streams, int64_t S_max, int n_splits) {
+  const int64_t tiles = (S_max + MX_TILE - 1) / MX_TILE;
+  int waves = MX_ATTN_WAVES;
+  while (waves > 1 && ((streams * n_splits * waves > 4096 && tiles < (int64_t)8 * waves * n_splits) || tiles <= (int64_t)waves / 2 * n_splits)) waves /= 2;
+  return waves;
+}
+
 template <typename T, int NB, int NQ>
 int32_t mx_launch_attn(const void* q, const void* kc, const void* vc, void* out, void* ws, const MxQueries& a, int Bt, hipStream_t st) {
-  const int64_t tiles = (a.S_max + MX_TILE - 1) / MX_TILE, per = (tiles + a.n_splits - 1) / a.n_splits;
-  const int64_t workgroups = (int64_t)Bt * a.H_kv * a.n_splits * a.groups;
-  PHOTON_REQUIRE(workgroups <= 0x7fffffff, PHOTON_ERR_UNSUPPORTED, "photon_mxfp4_decode_attn: %lld workgroups", (long long)workgroups);
-  const int waves = per >= 8 ? 8 : per > 2 ? 4 : per > 1 ? 2 : 1;
-  const int lds = waves * MxAttn<T, NB, NQ>::WAVE_BYTES, staged = NQ * NB * MX_BLOCK * 4;
-  PHOTON_LAUNCH(KC_COARSE_ATTN, st, (mxfp4_attn_kernel<T, NB, NQ>), dim3((unsigned)workgroups), dim3(waves * 64),
-                lds > staged ? lds : staged, st, (const T*)q, (const uint8_t*)kc, (const uint8_t*)vc, (T*)out, (float*)ws, a);
+  const int waves = mx_waves((int64_t)Bt * a.H_kv * a.groups, a.S_max, a.n_splits);
+  const unsigned lds = waves * (MxAttn<T, NB, NQ>::WAVE_BYTES);
+  PHOTON_LAUNCH(KC_COARSE_ATTN, st, (mxfp4_attn_kernel<T, NB, NQ>), dim3((unsigned)(a.n_splits * a.groups), a.H_kv, Bt),
+                dim3(waves * 64), lds, st, (const T*)q, (const uint8_t*)kc, (const uint8_t*)vc, (T*)out, (float*)ws, a);
   const int32_t rc = check_launch("mxfp4_attn_kernel");
   if (rc != PHOTON_OK || a.n_splits == 1) return rc;
-  PHOTON_LAUNCH(KC_COARSE_MERGE, st, (mxfp4_merge_kernel<T, NB>), dim3((unsigned)(Bt * a.T * a.H)), dim3(NB * MX_BLOCK), 0, st, (const float*)ws, (T*)out, a);
+  PHOTON_LAUNCH(KC_COARSE_MERGE, st, (mxfp4_merge_kernel<T, NB>), dim3(a.H, a.T, Bt), dim3(NB * MX_BLOCK), 0, st, (const float*)ws, (T*)out, a, waves);
   return check_launch("mxfp4_merge_kernel");
 }
 
@@ -756,7 +790,7 @@ int32_t check_shape(const char* who, int32_t Bt, int32_t T, int32_t H_kv, int32_
                  H_kv, (long long)S_max);
   PHOTON_REQUIRE(d_h >= 1 && d_h <= 128, PHOTON_ERR_UNSUPPORTED, "%s: d_h=%d not in [1, 128]", who, d_h);
   PHOTON_REQUIRE(S_max <= 0x7fffffff, PHOTON_ERR_UNSUPPORTED, "%s: S_max=%lld exceeds what an int32 position counts", who, (long long)S_max);
-  PHOTON_REQUIRE((int64_t)Bt * H_kv <= 0x7fffffff, PHOTON_ERR_UNSUPPORTED, "%s: Bt*H_kv=%lld streams", who, (long long)Bt * H_kv);
+  PHOTON_REQUIRE(Bt <= 65535 && H_kv <= 65535, PHOTON_ERR_UNSUPPORTED, "%s: Bt=%d, H_kv=%d streams: at most 65535 each", who, Bt, H_kv);
   return PHOTON_OK;
 }
 
@@ -771,37 +805,41 @@ int row_vec(const void* a, const void* b, int64_t stride, int d_h, size_t esz) {
   return 1;
 }
 
+// Steps of 16 positions that T rows can touch; waves of a workgroup; workgroups of a stream.
+int64_t mx_row_steps(int T) { return ((int64_t)T + MX_STEP - 2) / MX_STEP + 1; }
+int mx_row_waves(int T) { const int64_t n = mx_row_steps(T); return n < MX_WAVES ? (int)n : MX_WAVES; }
+int64_t mx_row_groups(int T) { return (mx_row_steps(T) + mx_row_waves(T) - 1) / mx_row_waves(T); }
+
 int32_t rows_args(const char* who, const void* k, const void* v, const void* kc, const void* vc, int64_t row_stride, const MxRows& a, photon_dtype dt) {
   const size_t esz = dtype_size(dt);
   PHOTON_REQUIRE(k && v && aligned(k, esz) && aligned(v, esz), PHOTON_ERR_INVALID_ARG, "%s: k and v must be non-null device pointers to whole elements", who);
   PHOTON_REQUIRE(kc && vc && aligned16(kc) && aligned16(vc), PHOTON_ERR_INVALID_ARG, "%s: the caches must be non-null, 16-byte aligned device pointers", who);
   PHOTON_REQUIRE(row_stride >= (int64_t)a.H_kv * a.d_h, PHOTON_ERR_INVALID_ARG, "%s: row_stride=%lld is less than a row of %d heads of %d", who,
                  (long long)row_stride, a.H_kv, a.d_h);
-  const int64_t groups = (a.streams * a.slots + MX_WAVES - 1) / MX_WAVES;
-  PHOTON_REQUIRE(groups <= 0x7fffffff, PHOTON_ERR_UNSUPPORTED, "%s: %lld workgroups", who, (long long)groups);
+  PHOTON_REQUIRE((int64_t)mx_row_groups(a.T) * a.H_kv <= 0x7fffffff, PHOTON_ERR_UNSUPPORTED, "%s: T=%d rows of %d heads are too many", who, a.T, a.H_kv);
   return PHOTON_OK;
 }
 
-MxRows mx_rows(const int32_t* start, const int32_t* n_new, int64_t row_stride, int32_t Bt, int32_t T, int32_t H_kv, int32_t d_h, int64_t S_max) {
+MxRows mx_rows(const int32_t* start, const int32_t* n_new, int64_t row_stride, int32_t T, int32_t H_kv, int32_t d_h, int64_t S_max) {
   MxRows a;
   a.start = start; a.n_new = n_new; a.row_stride = row_stride; a.S_max = S_max;
-  a.T = T; a.H_kv = H_kv; a.d_h = d_h; a.slots = (int)(((int64_t)T + 62) / 64 + 1); a.streams = (int64_t)Bt * H_kv;
+  a.T = T; a.H_kv = H_kv; a.d_h = d_h;
   return a;
 }
 
-#define MX_ROWS_CASE(kernel, T, NB, VEC, ...)                                                                      \
-  PHOTON_LAUNCH(KC_MXFP4_CACHE, st, (kernel<T, NB, VEC>), dim3((unsigned)((a.streams * a.slots + MX_WAVES - 1) / MX_WAVES)), dim3(MX_WAVES * 64), 0, st, __VA_ARGS__)
-#define MX_ROWS_VEC(kernel, T, NB, ...)                                                                            \
+#define MX_ROWS_CASE(kernel, T_, NB, VEC, ...)                                                                      \
+  PHOTON_LAUNCH(KC_MXFP4_CACHE, st, (kernel<T_, NB, VEC>), dim3((unsigned)mx_row_groups(T) * H_kv, Bt), dim3(mx_row_waves(T) * 64), 0, st, __VA_ARGS__)
+#define MX_ROWS_VEC(kernel, T_, NB, ...)                                                                            \
   do {                                                                                                             \
-    if (vec == 8) MX_ROWS_CASE(kernel, T, NB, 8, __VA_ARGS__);                                                     \
-    else if (vec == 4) MX_ROWS_CASE(kernel, T, NB, 4, __VA_ARGS__);                                                \
-    else MX_ROWS_CASE(kernel, T, NB, 1, __VA_ARGS__);                                                              \
+    if (vec == 8) MX_ROWS_CASE(kernel, T_, NB, 8, __VA_ARGS__);                                                     \
+    else if (vec == 4) MX_ROWS_CASE(kernel, T_, NB, 4, __VA_ARGS__);                                                \
+    else MX_ROWS_CASE(kernel, T_, NB, 1, __VA_ARGS__);                                                              \
   } while (0)
-#define MX_ROWS(kernel, T, ...)                                                                                    \
+#define MX_ROWS(kernel, T_, ...)                                                                                    \
   do {                                                                                                             \
-    if (d_p == 32) MX_ROWS_VEC(kernel, T, 1, __VA_ARGS__);                                                         \
-    else if (d_p == 64) MX_ROWS_VEC(kernel, T, 2, __VA_ARGS__);                                                    \
-    else MX_ROWS_VEC(kernel, T, 4, __VA_ARGS__);                                                                   \
+    if (d_p == 32) MX_ROWS_VEC(kernel, T_, 1, __VA_ARGS__);                                                         \
+    else if (d_p == 64) MX_ROWS_VEC(kernel, T_, 2, __VA_ARGS__);                                                    \
+    else MX_ROWS_VEC(kernel, T_, 4, __VA_ARGS__);                                                                   \
   } while (0)
 
 }  // namespace
@@ -822,7 +860,7 @@ extern "C" int32_t photon_mxfp4_cache_write(const void* k, const void* v, int64_
   clear_error();
   PHOTON_TRY(check_shape(__func__, Bt, T, H_kv, d_h, S_max, dt));
   if (Bt == 0 || T == 0) return PHOTON_OK;
-  const MxRows a = mx_rows(start, n_new, row_stride, Bt, T, H_kv, d_h, S_max);
+  const MxRows a = mx_rows(start, n_new, row_stride, T, H_kv, d_h, S_max);
   PHOTON_TRY(rows_args(__func__, k, v, k_cache, v_cache, row_stride, a, dt));
   const int d_p = photon_kv_row_elems(d_h), vec = row_vec(k, v, row_stride, d_h, dtype_size(dt));
   hipStream_t st = (hipStream_t)stream;
@@ -837,7 +875,7 @@ extern "C" int32_t photon_mxfp4_cache_read(const void* k_cache, const void* v_ca
   clear_error();
   PHOTON_TRY(check_shape(__func__, Bt, T, H_kv, d_h, S_max, dt));
   if (Bt == 0 || T == 0) return PHOTON_OK;
-  const MxRows a = mx_rows(start, n_rows, row_stride, Bt, T, H_kv, d_h, S_max);
+  const MxRows a = mx_rows(start, n_rows, row_stride, T, H_kv, d_h, S_max);
   PHOTON_TRY(rows_args(__func__, k, v, k_cache, v_cache, row_stride, a, dt));
   const int d_p = photon_kv_row_elems(d_h), vec = row_vec(k, v, row_stride, d_h, dtype_size(dt));
   hipStream_t st = (hipStream_t)stream;
@@ -864,8 +902,7 @@ extern "C" int32_t photon_mxfp4_decode_attn(const void* q, int64_t q_stride, con
   PHOTON_TRY(check_shape(__func__, Bt, T, H_kv, d_h, S_max, dt));
   PHOTON_REQUIRE(H > 0 && H % H_kv == 0, PHOTON_ERR_INVALID_ARG, "%s: H=%d query heads do not share H_kv=%d evenly", __func__, H, H_kv);
   PHOTON_REQUIRE(n_splits >= 0 && n_splits <= 1024, PHOTON_ERR_INVALID_ARG, "%s: n_splits=%d out of [0, 1024]", __func__, n_splits);
-  PHOTON_REQUIRE((int64_t)Bt * H <= 0x7fffffff && (int64_t)Bt * H * (T > 0 ? T : 1) <= 0x7fffffff, PHOTON_ERR_UNSUPPORTED,
-                 "%s: Bt=%d T=%d H=%d are too many queries", __func__, Bt, T, H);
+  PHOTON_REQUIRE(Bt <= 65535 && T <= 65535 && H <= 65535, PHOTON_ERR_UNSUPPORTED, "%s: Bt=%d, T=%d, H=%d queries: at most 65535 each", __func__, Bt, T, H);
   if (Bt == 0 || T == 0) return PHOTON_OK;
   const size_t esz = dtype_size(dt);
   PHOTON_REQUIRE(q && out && aligned(q, esz) && aligned(out, esz), PHOTON_ERR_INVALID_ARG, "%s: q and out must be non-null device pointers to whole elements", __func__);
