@@ -363,6 +363,10 @@ def _mx_counts(t: Optional[torch.Tensor], Bt: int, name: str) -> Optional[int]:
     return t.data_ptr()
 
 
+# The handle of a device's current stream without a Stream object around it (0.1 instead of 2.6 us of a call's 7).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
 def _mx_call(fn, tensors, *args) -> None:
     """fn(*args, stream) on the current stream of the tensors' device, with that device current."""
     device = tensors[0].get_device()
@@ -370,10 +374,10 @@ def _mx_call(fn, tensors, *args) -> None:
         if t is not None and (device < 0 or t.get_device() != device):
             raise PhotonError(-1, "all tensors must live in the memory of one device")
     if device == torch.cuda.current_device():
-        rc = fn(*args, _stream())
+        rc = fn(*args, _raw_stream(device))
     else:
         with torch.cuda.device(device):
-            rc = fn(*args, _stream())
+            rc = fn(*args, _raw_stream(device))
     if rc != 0:
         _check(rc)
 

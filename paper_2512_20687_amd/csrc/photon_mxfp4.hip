@@ -15,22 +15,35 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
 // ------------------------------------------------------------------ rows in and out
 //
-// A wave takes 16 positions of one stream, 8 positions x 64 elements at a time ("a pass"), all loads first: lane 8 r + x holds 8
-// consecutive elements of position r, 4 neighbouring lanes a block.  K words go out as they are.  V words hold 8 positions of
-// one element: the 8 lanes of equal x exchange nibbles (an 8 x 8 transposition in three steps).
-//   d_p = 128: a pass takes half of the elements; d_p = 32: lanes x >= 4 take the next 8 positions.
-// Neighbouring workgroups take neighbouring heads, so that rows [H_kv, d_h] are read as a whole.
+// A wave takes 16 positions of one stream, 8 positions x 64 elements at a time ("a pass"), all loads first.  Lane 8 r + x works on
+// position r.  Of bf16 rows it loads 8 consecutive elements at once.  Of others it loads 4 elements of the pass's block 0 and 4
+// of its block 1, so that 8 lanes read a row's elements side by side (for 32 x 64 fp32 elements a row 8 bytes apart cost 130 us
+// where this takes MX_T1), and neighbours exchange 4 codes: then it holds 8 consecutive elements, too.  These go out as they are
+// for K.  V words hold 8 positions of one element: the 8 lanes of equal x exchange nibbles (an 8 x 8 transposition in three steps).
+//   d_p = 128: a pass takes half of the elements; d_p = 32: it takes 16 positions, blocks 0 and 1 being positions r and 8 + r.
+// Neighbouring workgroups take neighbouring heads of the same positions, those of one die (blocks are dealt to the eight dies
+// in turn) heads that lie side by side, since heads of 52 to 60 elements share lines (4 x 8192 rows of 32 x 60 elements: bf16
+// written in 190 us and read back in 148 us without, in 118 and 114 with).
 
 constexpr int MX_WAVES = 4;      // waves of a workgroup, at most: 64 positions
 constexpr int MX_STEP = 16;      // positions of a wave
 
-template <int NB> struct MxPass {
-  int kk, dim;                                             // position among the wave's 16 and first of the lane's 8 elements
+template <typename T, int NB, int VEC> struct MxPass {
+  static constexpr bool SPLIT = sizeof(T) == 4 || VEC < 8;
+  static constexpr int LOADS = SPLIT ? 2 : 1, N = 8 / LOADS;           // loads of a pass, elements of each
+  int kk, dim;                                                         // position among the wave's 16 and first element of the lane's word
+  int load_kk[LOADS], load_dim[LOADS];                                 // the same of what it loads
   __device__ __forceinline__ MxPass(int pass, int lane) {
     const int r = lane >> 3, x = lane & 7;
-    if (NB == 1) { kk = (x >> 2) * 8 + r; dim = (x & 3) * 8; }
-    else if (NB == 2) { kk = pass * 8 + r; dim = x * 8; }
-    else { kk = (pass >> 1) * 8 + r; dim = (pass & 1) * 64 + x * 8; }
+    const int base_kk = (NB == 1 ? 0 : NB == 2 ? pass : pass >> 1) * 8 + r, base_dim = NB == 4 ? (pass & 1) * 64 : 0;
+    const int block = SPLIT ? x & 1 : x >> 2, in = (SPLIT ? x >> 1 : x & 3) * 8;
+    kk = base_kk + (NB == 1 ? block * 8 : 0);
+    dim = base_dim + (NB == 1 ? 0 : block * 32) + in;
+#pragma unroll
+    for (int u = 0; u < LOADS; ++u) {
+      load_kk[u] = SPLIT ? base_kk + (NB == 1 ? u * 8 : 0) : kk;
+      load_dim[u] = SPLIT ? base_dim + (NB == 1 ? 0 : u * 32) + x * 4 : dim;
+    }
   }
 };
 
@@ -44,77 +57,66 @@ __device__ __forceinline__ uint32_t mx_transpose8(uint32_t w, int lane) {
   return mx_swap_nibbles<1>(mx_swap_nibbles<2>(mx_swap_nibbles<4>(w, lane), lane), lane);
 }
 
-// The 8 elements of a row from `dim` on, zeros past d_h.  VEC elements per access: 8 or 4 where pointer, stride and d_h are whole
-// multiples of it, else 1.
-template <typename T, int VEC> __device__ __forceinline__ void mx_load8(const T* row, int dim, int d_h, float (&v)[8]) {
-  if constexpr (VEC == 8) {
-    if (dim < d_h) {
-      if constexpr (sizeof(T) == 2) Vec16<bf16_t>::load(reinterpret_cast<const bf16_t*>(row + dim), v);
-      else {
-        const float4_t a = *reinterpret_cast<const float4_t*>(row + dim), b = *reinterpret_cast<const float4_t*>(row + dim + 4);
+// N elements of a row from `dim` on, as loaded: at once where pointer, stride and d_h are whole multiples of 4 (8) elements, else
+// one by one (VEC = 1).  Loads are never skipped, so that all of them are in flight: past d_h the row's last elements are loaded.
+template <typename T, int N, int VEC> struct MxRaw {
+  static constexpr int WORDS = N * sizeof(T) / 4;
+  uint32_t w[WORDS];
+  __device__ __forceinline__ void load(const T* row, int dim, int d_h) {
+    if constexpr (VEC == 1) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+      for (int i = 0; i < N; ++i) {
+        const T x = row[dim + i < d_h ? dim + i : d_h - 1];
+        if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(x);
+        else w[i / 2] = i % 2 ? w[i / 2] | (uint32_t)x << 16 : (uint32_t)x;
       }
     } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = 0.f;
-    }
-  } else if constexpr (VEC == 4) {
-#pragma unroll
-    for (int u = 0; u < 8; u += 4) {
-      if (dim + u < d_h) {
-        if constexpr (sizeof(T) == 2) {
-          const uint2 r = *reinterpret_cast<const uint2*>(row + dim + u);
-          v[u] = bf16_lo(r.x); v[u + 1] = bf16_hi(r.x); v[u + 2] = bf16_lo(r.y); v[u + 3] = bf16_hi(r.y);
-        } else {
-          const float4_t a = *reinterpret_cast<const float4_t*>(row + dim + u);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[u + i] = a[i];
-        }
+      const T* from = row + (dim < d_h ? dim : d_h - N);
+      if constexpr (WORDS == 4) {
+        const uint4_t r = load16_stream(from);
+        w[0] = r.x; w[1] = r.y; w[2] = r.z; w[3] = r.w;
       } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[u + i] = 0.f;
+        const uint64_t r = __builtin_nontemporal_load(reinterpret_cast<const uint64_t*>(from));
+        w[0] = (uint32_t)r; w[1] = (uint32_t)(r >> 32);
       }
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = dim + i < d_h ? to_f32<T>(row[dim + i]) : 0.f;
   }
-}
-template <typename T, int VEC> __device__ __forceinline__ void mx_store8(T* row, int dim, int d_h, const float (&v)[8]) {
-  if constexpr (VEC == 8) {
-    if (dim < d_h) {
-      if constexpr (sizeof(T) == 2) Vec16<bf16_t>::store(reinterpret_cast<bf16_t*>(row + dim), v);
-      else {
-        *reinterpret_cast<float4_t*>(row + dim) = float4_t{v[0], v[1], v[2], v[3]};
-        *reinterpret_cast<float4_t*>(row + dim + 4) = float4_t{v[4], v[5], v[6], v[7]};
-      }
-    }
-  } else if constexpr (VEC == 4) {
+  __device__ __forceinline__ void values(int dim, int d_h, float (&v)[N]) const {      // zeros past d_h
 #pragma unroll
-    for (int u = 0; u < 8; u += 4) {
-      if (dim + u < d_h) {
-        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(row + dim + u) = make_uint2(pack_bf16x2(v[u], v[u + 1]), pack_bf16x2(v[u + 2], v[u + 3]));
-        else *reinterpret_cast<float4_t*>(row + dim + u) = float4_t{v[u], v[u + 1], v[u + 2], v[u + 3]};
-      }
+    for (int i = 0; i < N; ++i) {
+      const float x = sizeof(T) == 4 ? __uint_as_float(w[i % WORDS]) : i % 2 ? bf16_hi(w[i / 2 % WORDS]) : bf16_lo(w[i / 2 % WORDS]);
+      v[i] = dim + i < d_h ? x : 0.f;
     }
-  } else {
+  }
+};
+template <typename T, int N, int VEC> __device__ __forceinline__ void mx_store(T* row, int dim, int d_h, const float (&v)[N]) {
+  if constexpr (VEC == 1) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < N; ++i)
       if (dim + i < d_h) row[dim + i] = from_f32<T>(v[i]);
+  } else if (dim < d_h) {
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4_t*>(row + dim) = float4_t{v[0], v[1], v[2], v[3]};
+    else if constexpr (N == 8) Vec16<bf16_t>::store(reinterpret_cast<bf16_t*>(row + dim), v);
+    else *reinterpret_cast<uint2*>(row + dim) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
   }
 }
 
-// A block of 32 elements in 4 neighbouring lanes -> the lane's 8 codes and the block's scale byte.  The largest magnitude is taken
-// of the bits, so that a NaN or an infinity is the largest: such a block gets the scale byte 255 and reads back as NaN.
-__device__ __forceinline__ uint32_t mx_quantise8(const float (&v)[8], uint32_t& scale_byte) {
+template <int CTRL> __device__ __forceinline__ uint32_t mx_dpp(uint32_t x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xf, 0xf, false); }
+
+// A block of 32 elements in 32 / N neighbouring lanes -> the lane's N codes and the block's scale byte.  The largest magnitude is
+// taken of the bits, so that a NaN or an infinity is the largest: such a block gets the scale byte 255 and reads back as NaN.
+template <int N> __device__ __forceinline__ uint32_t mx_quantise(const float (&v)[N], uint32_t& scale_byte) {
   uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) { const uint32_t m = __float_as_uint(v[i]) & 0x7fffffffu; top = m > top ? m : top; }
-  uint32_t o = __builtin_amdgcn_update_dpp(0, top, DPP_XOR1, 0xf, 0xf, false);
+  for (int i = 0; i < N; ++i) { const uint32_t m = __float_as_uint(v[i]) & 0x7fffffffu; top = m > top ? m : top; }
+  uint32_t o = mx_dpp<DPP_XOR1>(top);
   top = o > top ? o : top;
-  o = __builtin_amdgcn_update_dpp(0, top, DPP_XOR2, 0xf, 0xf, false);
+  o = mx_dpp<DPP_XOR2>(top);
   top = o > top ? o : top;
+  if constexpr (N == 4) {
+    o = mx_dpp<DPP_HALF_MIRROR>(top);
+    top = o > top ? o : top;
+  }
   const uint32_t e = top >> 23;
   scale_byte = e == 255u ? 255u : (e > 2u ? e : 2u) - 2u;
   // The conversion takes x / X with X = 2^(exponent field - 127) of its scale operand, a field of 0 included.
@@ -122,20 +124,55 @@ __device__ __forceinline__ uint32_t mx_quantise8(const float (&v)[8], uint32_t& 
   uint32_t w = 0;
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0], v[1], scale, 0);
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], scale, 1);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], scale, 2);
-  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], scale, 3);
+  if constexpr (N == 8) {
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], scale, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], scale, 3);
+  }
   return w;
 }
 
-// 8 codes under one scale byte -> values.
-__device__ __forceinline__ void mx_values8(uint32_t w, uint32_t scale_byte, float (&v)[8]) {
+// What a pass loaded -> the lane's word and its block's scale byte.
+template <typename P, typename R> __device__ __forceinline__ uint32_t mx_word(const P& p, const R (&raw)[P::LOADS], int lane, int d_h, uint32_t& scale_byte) {
+  float v[P::N];
+  raw[0].values(p.load_dim[0], d_h, v);
+  const uint32_t w0 = mx_quantise(v, scale_byte);
+  if constexpr (!P::SPLIT) return w0;
+  else {
+    uint32_t s1;
+    raw[1].values(p.load_dim[1], d_h, v);
+    const uint32_t w1 = mx_quantise(v, s1);
+    const bool odd = lane & 1;
+    const uint32_t other = mx_dpp<DPP_XOR1>(odd ? w0 : w1);
+    scale_byte = odd ? s1 : scale_byte;
+    return odd ? other | w1 << 16 : w0 | other << 16;
+  }
+}
+
+// N codes under one scale byte -> values.
+template <int N> __device__ __forceinline__ void mx_values(uint32_t w, uint32_t scale_byte, float (&v)[N]) {
   const float scale = __uint_as_float(scale_byte << 23);
   const f32x2_native a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1);
-  const f32x2_native c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3);
-  v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y; v[4] = c.x; v[5] = c.y; v[6] = d.x; v[7] = d.y;
+  v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+  if constexpr (N == 8) {
+    const f32x2_native c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3);
+    v[4] = c.x; v[5] = c.y; v[6] = d.x; v[7] = d.y;
+  }
   if (scale_byte > (uint32_t)MX_LAST_SCALE)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(0x7fc00000u);
+    for (int i = 0; i < N; ++i) v[i] = __uint_as_float(0x7fc00000u);
+}
+
+// The lane's word and scale byte -> the codes and scales of what its row accesses hold: mx_word's exchange backwards.
+template <typename P> __device__ __forceinline__ void mx_parts(uint32_t w, uint32_t scale_byte, int lane, uint32_t (&code)[P::LOADS], uint32_t (&scale)[P::LOADS]) {
+  if constexpr (!P::SPLIT) { code[0] = w; scale[0] = scale_byte; }
+  else {
+    const bool odd = lane & 1;
+    const uint32_t other = mx_dpp<DPP_XOR1>(odd ? w & 0xffffu : w >> 16), other_scale = mx_dpp<DPP_XOR1>(scale_byte);
+    code[0] = odd ? other : w & 0xffffu;
+    code[1] = odd ? w >> 16 : other;
+    scale[0] = odd ? other_scale : scale_byte;
+    scale[1] = odd ? scale_byte : other_scale;
+  }
 }
 
 struct MxRows {                  // a stretch of rows and the positions it belongs to
@@ -152,9 +189,9 @@ struct MxShare {
 };
 // false: nothing to do.  outside: rows of this sequence have no place in the cache.
 __device__ __forceinline__ bool mx_share(const MxRows& a, MxShare& s, bool& outside) {
-  const unsigned group = blockIdx.x / (unsigned)a.H_kv;
+  const unsigned group = blockIdx.x / (unsigned)a.H_kv, h = blockIdx.x - group * a.H_kv;
   s.b = blockIdx.y;
-  s.h = blockIdx.x - group * a.H_kv;
+  s.h = a.H_kv % 8 == 0 ? h % 8 * (a.H_kv / 8) + h / 8 : h;
   int64_t n = a.n_new ? a.n_new[s.b] : a.T;
   n = n < 0 ? 0 : n > a.T ? a.T : n;
   const int64_t first = a.start ? a.start[s.b] : 0;
@@ -179,43 +216,46 @@ __global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_write_kernel(const T* __r
   const bool any = mx_share(a, s, outside);
   if (outside && status != nullptr && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(status, (int)PHOTON_STATUS_CACHE_FULL);
   if (!any) return;
-  float kv[NB][8], vv[NB][8];
-#pragma unroll
-  for (int i = 0; i < NB; ++i) {
-    const MxPass<NB> p(i, lane);
-    if (p.kk >= s.lo && p.kk < s.hi) {
-      const int64_t row = (s.row0 + p.kk) * a.row_stride + (int64_t)s.h * a.d_h;
-      mx_load8<T, VEC>(k + row, p.dim, a.d_h, kv[i]);
-      mx_load8<T, VEC>(v + row, p.dim, a.d_h, vv[i]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) kv[i][e] = vv[i][e] = 0.f;
-    }
-  }
   const int64_t tiles = (a.S_max + MX_TILE - 1) / MX_TILE;
   const int64_t at = (((int64_t)s.b * a.H_kv + s.h) * tiles + s.tile) * mx_tile_bytes(NB * MX_BLOCK);
   kc += at;
   vc += at;
+  using P = MxPass<T, NB, VEC>;
+  MxRaw<T, P::N, VEC> kr[NB][P::LOADS], vr[NB][P::LOADS];
+  uint32_t held[NB];
 #pragma unroll
   for (int i = 0; i < NB; ++i) {
-    const MxPass<NB> p(i, lane);
-    const int kk = s.base + p.kk, block = p.dim >> 5;
+    const P p(i, lane);
+#pragma unroll
+    for (int u = 0; u < P::LOADS; ++u) {
+      const int kk = p.load_kk[u] < s.lo ? s.lo : p.load_kk[u] < s.hi ? p.load_kk[u] : s.hi - 1;   // what other positions give is not stored
+      const int64_t row = (s.row0 + kk) * a.row_stride + (int64_t)s.h * a.d_h;
+      kr[i][u].load(k + row, p.load_dim[u], a.d_h);
+      vr[i][u].load(v + row, p.load_dim[u], a.d_h);
+    }
+    // the lane's V word, element dim + r of the 8 positions around p.kk: those outside [lo, hi) keep what they held
+    const int group = p.kk & ~7;
+    held[i] = 0;
+    if ((s.lo > group || s.hi < group + 8) && s.lo < group + 8 && s.hi > group)
+      held[i] = *reinterpret_cast<const uint32_t*>(vc + mx_v_word<NB>(s.base + group, p.dim + (lane >> 3)));
+  }
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    const P p(i, lane);
+    const int kk = s.base + p.kk, block = p.dim >> 5, group = p.kk & ~7;
     uint32_t ks, vs;
-    const uint32_t kw = mx_quantise8(kv[i], ks), vw = mx_transpose8(mx_quantise8(vv[i], vs), lane);
+    const uint32_t kw = mx_word(p, kr[i], lane, a.d_h, ks), vw = mx_transpose8(mx_word(p, vr[i], lane, a.d_h, vs), lane);
     if (p.kk >= s.lo && p.kk < s.hi) {
       *reinterpret_cast<uint32_t*>(kc + mx_k_chunk<NB>(kk, block) + ((p.dim >> 3) & 3) * 4) = kw;
-      if ((lane & 3) == 0) {
+      if ((p.dim & 31) == 0) {
         kc[mx_k_scale<NB>(kk, block)] = (uint8_t)ks;
         vc[mx_v_scale<NB>(kk, block)] = (uint8_t)vs;
       }
     }
-    // the lane's V word: element dim + r, the 8 positions around p.kk; those outside [lo, hi) keep what they held
-    const int group = p.kk & ~7, r = lane >> 3;
-    const int from = s.lo - group < 0 ? 0 : s.lo - group, to = s.hi - group > 8 ? 8 : s.hi - group;
+    const int from = s.lo > group ? s.lo - group : 0, to = s.hi < group + 8 ? s.hi - group : 8;
     if (from < to) {
-      uint32_t* word = reinterpret_cast<uint32_t*>(vc + mx_v_word<NB>(kk & ~7, p.dim + r));
       const uint32_t mask = (to == 8 ? 0xffffffffu : (1u << (4 * to)) - 1u) & ~((1u << (4 * from)) - 1u);
-      *word = mask == 0xffffffffu ? vw : (*word & ~mask) | (vw & mask);
+      *reinterpret_cast<uint32_t*>(vc + mx_v_word<NB>(s.base + group, p.dim + (lane >> 3))) = (held[i] & ~mask) | (vw & mask);
     }
   }
 }
@@ -231,10 +271,11 @@ __global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_read_kernel(const uint8_t
   const int64_t at = (((int64_t)s.b * a.H_kv + s.h) * tiles + s.tile) * mx_tile_bytes(NB * MX_BLOCK);
   kc += at;
   vc += at;
+  using P = MxPass<T, NB, VEC>;
   uint32_t kw[NB], vw[NB], ks[NB], vs[NB];
 #pragma unroll
   for (int i = 0; i < NB; ++i) {
-    const MxPass<NB> p(i, lane);
+    const P p(i, lane);
     const int kk = s.base + p.kk, block = p.dim >> 5;
     kw[i] = *reinterpret_cast<const uint32_t*>(kc + mx_k_chunk<NB>(kk, block) + ((p.dim >> 3) & 3) * 4);
     vw[i] = *reinterpret_cast<const uint32_t*>(vc + mx_v_word<NB>(kk & ~7, p.dim + (lane >> 3)));
@@ -243,14 +284,20 @@ __global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_read_kernel(const uint8_t
   }
 #pragma unroll
   for (int i = 0; i < NB; ++i) {
-    const MxPass<NB> p(i, lane);
-    float kv[8], vv[8];
-    mx_values8(kw[i], ks[i], kv);
-    mx_values8(mx_transpose8(vw[i], lane), vs[i], vv);
-    if (p.kk >= s.lo && p.kk < s.hi) {
-      const int64_t row = (s.row0 + p.kk) * a.row_stride + (int64_t)s.h * a.d_h;
-      mx_store8<T, VEC>(k + row, p.dim, a.d_h, kv);
-      mx_store8<T, VEC>(v + row, p.dim, a.d_h, vv);
+    const P p(i, lane);
+    uint32_t kc_[P::LOADS], ks_[P::LOADS], vc_[P::LOADS], vs_[P::LOADS];
+    mx_parts<P>(kw[i], ks[i], lane, kc_, ks_);
+    mx_parts<P>(mx_transpose8(vw[i], lane), vs[i], lane, vc_, vs_);
+#pragma unroll
+    for (int u = 0; u < P::LOADS; ++u) {
+      float kv[P::N], vv[P::N];
+      mx_values(kc_[u], ks_[u], kv);
+      mx_values(vc_[u], vs_[u], vv);
+      if (p.load_kk[u] >= s.lo && p.load_kk[u] < s.hi) {
+        const int64_t row = (s.row0 + p.load_kk[u]) * a.row_stride + (int64_t)s.h * a.d_h;
+        mx_store<T, P::N, VEC>(k + row, p.load_dim[u], a.d_h, kv);
+        mx_store<T, P::N, VEC>(v + row, p.load_dim[u], a.d_h, vv);
+      }
     }
   }
 }
@@ -796,13 +843,10 @@ int32_t check_shape(const char* who, int32_t Bt, int32_t T, int32_t H_kv, int32_
 
 bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
-// Elements per access of rows: what pointers, stride and head size are whole multiples of.
+// Elements per access of rows: 8 (bf16) or 4 where pointers, stride and head size are whole multiples of it, else 1.
 int row_vec(const void* a, const void* b, int64_t stride, int d_h, size_t esz) {
-  for (int vec = 8; vec > 1; vec -= 4) {
-    const size_t bytes = vec * esz < 16 ? vec * esz : 16;
-    if (d_h % vec == 0 && stride * esz % bytes == 0 && aligned(a, bytes) && aligned(b, bytes)) return vec;
-  }
-  return 1;
+  const auto whole = [&](int vec) { return d_h % vec == 0 && stride % vec == 0 && aligned(a, vec * esz) && aligned(b, vec * esz); };
+  return esz == 2 && whole(8) ? 8 : whole(4) ? 4 : 1;
 }
 
 // Steps of 16 positions that T rows can touch; waves of a workgroup; workgroups of a stream.
@@ -816,7 +860,7 @@ int32_t rows_args(const char* who, const void* k, const void* v, const void* kc,
   PHOTON_REQUIRE(kc && vc && aligned16(kc) && aligned16(vc), PHOTON_ERR_INVALID_ARG, "%s: the caches must be non-null, 16-byte aligned device pointers", who);
   PHOTON_REQUIRE(row_stride >= (int64_t)a.H_kv * a.d_h, PHOTON_ERR_INVALID_ARG, "%s: row_stride=%lld is less than a row of %d heads of %d", who,
                  (long long)row_stride, a.H_kv, a.d_h);
-  PHOTON_REQUIRE((int64_t)mx_row_groups(a.T) * a.H_kv <= 0x7fffffff, PHOTON_ERR_UNSUPPORTED, "%s: T=%d rows of %d heads are too many", who, a.T, a.H_kv);
+  PHOTON_REQUIRE(mx_row_groups(a.T) * a.H_kv <= 0x7fffffff, PHOTON_ERR_UNSUPPORTED, "%s: T=%d rows of %d heads are too many", who, a.T, a.H_kv);
   return PHOTON_OK;
 }
 
@@ -827,20 +871,31 @@ MxRows mx_rows(const int32_t* start, const int32_t* n_new, int64_t row_stride, i
   return a;
 }
 
-#define MX_ROWS_CASE(kernel, T_, NB, VEC, ...)                                                                      \
-  PHOTON_LAUNCH(KC_MXFP4_CACHE, st, (kernel<T_, NB, VEC>), dim3((unsigned)mx_row_groups(T) * H_kv, Bt), dim3(mx_row_waves(T) * 64), 0, st, __VA_ARGS__)
-#define MX_ROWS_VEC(kernel, T_, NB, ...)                                                                            \
-  do {                                                                                                             \
-    if (vec == 8) MX_ROWS_CASE(kernel, T_, NB, 8, __VA_ARGS__);                                                     \
-    else if (vec == 4) MX_ROWS_CASE(kernel, T_, NB, 4, __VA_ARGS__);                                                \
-    else MX_ROWS_CASE(kernel, T_, NB, 1, __VA_ARGS__);                                                              \
-  } while (0)
-#define MX_ROWS(kernel, T_, ...)                                                                                    \
-  do {                                                                                                             \
-    if (d_p == 32) MX_ROWS_VEC(kernel, T_, 1, __VA_ARGS__);                                                         \
-    else if (d_p == 64) MX_ROWS_VEC(kernel, T_, 2, __VA_ARGS__);                                                    \
-    else MX_ROWS_VEC(kernel, T_, 4, __VA_ARGS__);                                                                   \
-  } while (0)
+template <typename T, int NB, int VEC>
+void launch_rows(bool write, const void* k, const void* v, const void* kc, const void* vc, int32_t* status, const MxRows& a, int Bt, hipStream_t st) {
+  const dim3 grid((unsigned)(mx_row_groups(a.T) * a.H_kv), Bt), block(mx_row_waves(a.T) * 64);
+  if (write)
+    PHOTON_LAUNCH(KC_MXFP4_CACHE, st, (mxfp4_write_kernel<T, NB, VEC>), grid, block, 0, st, (const T*)k, (const T*)v, (uint8_t*)kc, (uint8_t*)vc, status, a);
+  else
+    PHOTON_LAUNCH(KC_MXFP4_CACHE, st, (mxfp4_read_kernel<T, NB, VEC>), grid, block, 0, st, (const uint8_t*)kc, (const uint8_t*)vc, (T*)k, (T*)v, a);
+}
+template <typename T, int NB>
+void launch_rows_vec(bool write, const void* k, const void* v, const void* kc, const void* vc, int32_t* status, const MxRows& a, int Bt, hipStream_t st) {
+  const int vec = row_vec(k, v, a.row_stride, a.d_h, sizeof(T));
+  if constexpr (sizeof(T) == 2)
+    if (vec == 8) return launch_rows<T, NB, 8>(write, k, v, kc, vc, status, a, Bt, st);
+  if (vec == 4) return launch_rows<T, NB, 4>(write, k, v, kc, vc, status, a, Bt, st);
+  launch_rows<T, NB, 1>(write, k, v, kc, vc, status, a, Bt, st);
+}
+template <typename T>
+int32_t launch_rows_t(bool write, const void* k, const void* v, const void* kc, const void* vc, int32_t* status, const MxRows& a, int Bt, hipStream_t st) {
+  switch (kv_row_elems(a.d_h)) {
+    case 32: launch_rows_vec<T, 1>(write, k, v, kc, vc, status, a, Bt, st); break;
+    case 64: launch_rows_vec<T, 2>(write, k, v, kc, vc, status, a, Bt, st); break;
+    default: launch_rows_vec<T, 4>(write, k, v, kc, vc, status, a, Bt, st); break;
+  }
+  return check_launch(write ? "mxfp4_write_kernel" : "mxfp4_read_kernel");
+}
 
 }  // namespace
 
@@ -862,11 +917,7 @@ extern "C" int32_t photon_mxfp4_cache_write(const void* k, const void* v, int64_
   if (Bt == 0 || T == 0) return PHOTON_OK;
   const MxRows a = mx_rows(start, n_new, row_stride, T, H_kv, d_h, S_max);
   PHOTON_TRY(rows_args(__func__, k, v, k_cache, v_cache, row_stride, a, dt));
-  const int d_p = photon_kv_row_elems(d_h), vec = row_vec(k, v, row_stride, d_h, dtype_size(dt));
-  hipStream_t st = (hipStream_t)stream;
-  if (dt == PHOTON_F32) MX_ROWS(mxfp4_write_kernel, float, (const float*)k, (const float*)v, (uint8_t*)k_cache, (uint8_t*)v_cache, status, a);
-  else MX_ROWS(mxfp4_write_kernel, bf16_t, (const bf16_t*)k, (const bf16_t*)v, (uint8_t*)k_cache, (uint8_t*)v_cache, status, a);
-  return check_launch("mxfp4_write_kernel");
+  return (dt == PHOTON_F32 ? launch_rows_t<float> : launch_rows_t<bf16_t>)(true, k, v, k_cache, v_cache, status, a, Bt, (hipStream_t)stream);
 }
 
 extern "C" int32_t photon_mxfp4_cache_read(const void* k_cache, const void* v_cache, const int32_t* start, const int32_t* n_rows, void* k, void* v,
@@ -877,11 +928,7 @@ extern "C" int32_t photon_mxfp4_cache_read(const void* k_cache, const void* v_ca
   if (Bt == 0 || T == 0) return PHOTON_OK;
   const MxRows a = mx_rows(start, n_rows, row_stride, T, H_kv, d_h, S_max);
   PHOTON_TRY(rows_args(__func__, k, v, k_cache, v_cache, row_stride, a, dt));
-  const int d_p = photon_kv_row_elems(d_h), vec = row_vec(k, v, row_stride, d_h, dtype_size(dt));
-  hipStream_t st = (hipStream_t)stream;
-  if (dt == PHOTON_F32) MX_ROWS(mxfp4_read_kernel, float, (const uint8_t*)k_cache, (const uint8_t*)v_cache, (float*)k, (float*)v, a);
-  else MX_ROWS(mxfp4_read_kernel, bf16_t, (const uint8_t*)k_cache, (const uint8_t*)v_cache, (bf16_t*)k, (bf16_t*)v, a);
-  return check_launch("mxfp4_read_kernel");
+  return (dt == PHOTON_F32 ? launch_rows_t<float> : launch_rows_t<bf16_t>)(false, k, v, k_cache, v_cache, nullptr, a, Bt, (hipStream_t)stream);
 }
 
 extern "C" size_t photon_mxfp4_decode_attn_workspace_bytes(int32_t Bt, int32_t T, int32_t H, int32_t d_h, int32_t n_splits) {
