@@ -17,13 +17,15 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 //
 // A wave takes 16 positions of one stream, 8 positions x 64 elements at a time ("a pass"), all loads first.  Lane 8 r + x works on
 // position r.  Of bf16 rows it loads 8 consecutive elements at once.  Of others it loads 4 elements of the pass's block 0 and 4
-// of its block 1, so that 8 lanes read a row's elements side by side (for 32 x 64 fp32 elements a row 8 bytes apart cost 130 us
-// where this takes MX_T1), and neighbours exchange 4 codes: then it holds 8 consecutive elements, too.  These go out as they are
+// of its block 1, so that 8 lanes read a row's elements side by side (4 x 8192 fp32 rows of 32 x 64 elements: 111 us, 130 with 8
+// consecutive elements a lane), and neighbours exchange 4 codes: then it holds 8 consecutive elements, too.  These go out as they are
 // for K.  V words hold 8 positions of one element: the 8 lanes of equal x exchange nibbles (an 8 x 8 transposition in three steps).
 //   d_p = 128: a pass takes half of the elements; d_p = 32: it takes 16 positions, blocks 0 and 1 being positions r and 8 + r.
-// Neighbouring workgroups take neighbouring heads of the same positions, those of one die (blocks are dealt to the eight dies
-// in turn) heads that lie side by side, since heads of 52 to 60 elements share lines (4 x 8192 rows of 32 x 60 elements: bf16
-// written in 190 us and read back in 148 us without, in 118 and 114 with).
+// Neighbouring workgroups take neighbouring heads of the same positions (but see launch_rows), those of one die (blocks are dealt to the eight dies
+// in turn) heads that lie side by side, since heads of 52 to 60 elements share lines (4 x 8192 bf16 rows of 32 x 60 elements:
+// written in 190 us and read back in 148 without, in 120 and 109 with).
+// Measured for four prompts of 8192 rows of 32 x 64 elements (K and V): fp32 written at 5.4 TB/s (537 MB in, 71 MB out) and read
+// back at 4.8; bf16 at 4.9 and 5.6.  Without its stores the write takes 97 us (fp32): its bound is memory in both directions.
 
 constexpr int MX_WAVES = 4;      // waves of a workgroup, at most: 64 positions
 constexpr int MX_STEP = 16;      // positions of a wave
@@ -62,7 +64,8 @@ __device__ __forceinline__ uint32_t mx_transpose8(uint32_t w, int lane) {
 template <typename T, int N, int VEC> struct MxRaw {
   static constexpr int WORDS = N * sizeof(T) / 4;
   uint32_t w[WORDS];
-  __device__ __forceinline__ void load(const T* row, int dim, int d_h) {
+  // ONCE: nothing else will read these lines, so they are read past the caches
+  template <bool ONCE> __device__ __forceinline__ void load(const T* row, int dim, int d_h) {
     if constexpr (VEC == 1) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
@@ -73,10 +76,11 @@ template <typename T, int N, int VEC> struct MxRaw {
     } else {
       const T* from = row + (dim < d_h ? dim : d_h - N);
       if constexpr (WORDS == 4) {
-        const uint4_t r = load16_stream(from);
+        const uint4_t r = ONCE ? load16_stream(from) : load16(from);
         w[0] = r.x; w[1] = r.y; w[2] = r.z; w[3] = r.w;
       } else {
-        const uint64_t r = __builtin_nontemporal_load(reinterpret_cast<const uint64_t*>(from));
+        const uint64_t* at = reinterpret_cast<const uint64_t*>(from);
+        const uint64_t r = ONCE ? __builtin_nontemporal_load(at) : *at;
         w[0] = (uint32_t)r; w[1] = (uint32_t)(r >> 32);
       }
     }
@@ -180,6 +184,7 @@ struct MxRows {                  // a stretch of rows and the positions it belon
   int64_t row_stride;            // elements from a row to the next
   int64_t S_max;
   int T, H_kv, d_h;
+  bool heads_first;              // neighbouring workgroups take neighbouring heads of the same positions, else the other way round
 };
 
 // A wave's share: a step of 16 positions, and those [lo, hi) of it that rows in use belong to.
@@ -189,9 +194,10 @@ struct MxShare {
 };
 // false: nothing to do.  outside: rows of this sequence have no place in the cache.
 __device__ __forceinline__ bool mx_share(const MxRows& a, MxShare& s, bool& outside) {
-  const unsigned group = blockIdx.x / (unsigned)a.H_kv, h = blockIdx.x - group * a.H_kv;
+  const unsigned of = a.heads_first ? (unsigned)a.H_kv : gridDim.x / (unsigned)a.H_kv, major = blockIdx.x / of, minor = blockIdx.x - major * of;
+  const unsigned group = a.heads_first ? major : minor;
   s.b = blockIdx.y;
-  s.h = a.H_kv % 8 == 0 ? h % 8 * (a.H_kv / 8) + h / 8 : h;
+  s.h = !a.heads_first ? major : a.H_kv % 8 == 0 ? minor % 8 * (a.H_kv / 8) + minor / 8 : minor;
   int64_t n = a.n_new ? a.n_new[s.b] : a.T;
   n = n < 0 ? 0 : n > a.T ? a.T : n;
   const int64_t first = a.start ? a.start[s.b] : 0;
@@ -207,7 +213,7 @@ __device__ __forceinline__ bool mx_share(const MxRows& a, MxShare& s, bool& outs
   return true;
 }
 
-template <typename T, int NB, int VEC>
+template <typename T, int NB, int VEC, bool ONCE>
 __global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_write_kernel(const T* __restrict__ k, const T* __restrict__ v, uint8_t* __restrict__ kc,
                                                                     uint8_t* __restrict__ vc, int32_t* __restrict__ status, MxRows a) {
   const int lane = threadIdx.x & 63;
@@ -230,8 +236,8 @@ __global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_write_kernel(const T* __r
     for (int u = 0; u < P::LOADS; ++u) {
       const int kk = p.load_kk[u] < s.lo ? s.lo : p.load_kk[u] < s.hi ? p.load_kk[u] : s.hi - 1;   // what other positions give is not stored
       const int64_t row = (s.row0 + kk) * a.row_stride + (int64_t)s.h * a.d_h;
-      kr[i][u].load(k + row, p.load_dim[u], a.d_h);
-      vr[i][u].load(v + row, p.load_dim[u], a.d_h);
+      kr[i][u].template load<ONCE>(k + row, p.load_dim[u], a.d_h);
+      vr[i][u].template load<ONCE>(v + row, p.load_dim[u], a.d_h);
     }
     // the lane's V word, element dim + r of the 8 positions around p.kk: those outside [lo, hi) keep what they held
     const int group = p.kk & ~7;
@@ -872,10 +878,18 @@ MxRows mx_rows(const int32_t* start, const int32_t* n_new, int64_t row_stride, i
 }
 
 template <typename T, int NB, int VEC>
-void launch_rows(bool write, const void* k, const void* v, const void* kc, const void* vc, int32_t* status, const MxRows& a, int Bt, hipStream_t st) {
+void launch_rows(bool write, const void* k, const void* v, const void* kc, const void* vc, int32_t* status, MxRows a, int Bt, hipStream_t st) {
   const dim3 grid((unsigned)(mx_row_groups(a.T) * a.H_kv), Bt), block(mx_row_waves(a.T) * 64);
-  if (write)
-    PHOTON_LAUNCH(KC_MXFP4_CACHE, st, (mxfp4_write_kernel<T, NB, VEC>), grid, block, 0, st, (const T*)k, (const T*)v, (uint8_t*)kc, (uint8_t*)vc, status, a);
+  // A head's row of whole lines of 128 bytes is read past the caches (4 x 8192 rows of 32 x 64 elements: fp32 111 us, 145 through
+  // them, bf16 70 and 88); where neighbours share lines that is slower (32 x 60 elements: 174 us, 167 through them, 120 and 92).
+  const bool lines = a.d_h * sizeof(T) % 128 == 0 && a.row_stride * sizeof(T) % 128 == 0 && aligned(k, 128) && aligned(v, 128);
+  // Read back, whole lines are written by workgroups of neighbouring positions: their tiles follow each other (bf16, 66 us instead of 76).
+  a.heads_first = write || !lines;
+  if (write && VEC * sizeof(T) >= 16 && lines)
+    PHOTON_LAUNCH(KC_MXFP4_CACHE, st, (mxfp4_write_kernel<T, NB, VEC, (VEC * sizeof(T) >= 16)>), grid, block, 0, st, (const T*)k, (const T*)v, (uint8_t*)kc,
+                  (uint8_t*)vc, status, a);
+  else if (write)
+    PHOTON_LAUNCH(KC_MXFP4_CACHE, st, (mxfp4_write_kernel<T, NB, VEC, false>), grid, block, 0, st, (const T*)k, (const T*)v, (uint8_t*)kc, (uint8_t*)vc, status, a);
   else
     PHOTON_LAUNCH(KC_MXFP4_CACHE, st, (mxfp4_read_kernel<T, NB, VEC>), grid, block, 0, st, (const uint8_t*)kc, (const uint8_t*)vc, (T*)k, (T*)v, a);
 }
