@@ -33,6 +33,11 @@ constexpr int MX_STEP = 16;      // positions of a wave
 template <typename T, int NB, int VEC> struct MxPass {
   static constexpr bool SPLIT = sizeof(T) == 4 || VEC < 8;
   static constexpr int LOADS = SPLIT ? 2 : 1, N = 8 / LOADS;           // loads of a pass, elements of each
+  // Whether any of the positions [lo, hi) is the pass's.
+  static __device__ __forceinline__ bool live(int pass, int lo, int hi) {
+    const int from = NB == 1 ? 0 : NB == 2 ? 8 * pass : 8 * (pass >> 1);
+    return lo < from + (NB == 1 ? 16 : 8) && hi > from;
+  }
   int kk, dim;                                                         // position among the wave's 16 and first element of the lane's word
   int load_kk[LOADS], load_dim[LOADS];                                 // the same of what it loads
   __device__ __forceinline__ MxPass(int pass, int lane) {
@@ -203,7 +208,8 @@ __device__ __forceinline__ bool mx_share(const MxRows& a, MxShare& s, bool& outs
   const int64_t first = a.start ? a.start[s.b] : 0;
   const int64_t begin = first < 0 ? 0 : first, end = first + n < a.S_max ? first + n : a.S_max;
   outside = n > 0 && (first < 0 || first + n > a.S_max);
-  const int64_t at = (begin / MX_STEP + (int64_t)group * (blockDim.x >> 6) + (threadIdx.x >> 6)) * MX_STEP;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);           // the same in the wave: what follows is scalar
+  const int64_t at = (begin / MX_STEP + (int64_t)group * (blockDim.x >> 6) + wave) * MX_STEP;
   if (at >= end) return false;
   s.tile = at / MX_TILE;
   s.base = (int)(at % MX_TILE);
@@ -231,6 +237,7 @@ __global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_write_kernel(const T* __r
   uint32_t held[NB];
 #pragma unroll
   for (int i = 0; i < NB; ++i) {
+    if (!P::live(i, s.lo, s.hi)) continue;
     const P p(i, lane);
 #pragma unroll
     for (int u = 0; u < P::LOADS; ++u) {
@@ -247,6 +254,7 @@ __global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_write_kernel(const T* __r
   }
 #pragma unroll
   for (int i = 0; i < NB; ++i) {
+    if (!P::live(i, s.lo, s.hi)) continue;
     const P p(i, lane);
     const int kk = s.base + p.kk, block = p.dim >> 5, group = p.kk & ~7;
     uint32_t ks, vs;
@@ -281,6 +289,7 @@ __global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_read_kernel(const uint8_t
   uint32_t kw[NB], vw[NB], ks[NB], vs[NB];
 #pragma unroll
   for (int i = 0; i < NB; ++i) {
+    if (!P::live(i, s.lo, s.hi)) continue;
     const P p(i, lane);
     const int kk = s.base + p.kk, block = p.dim >> 5;
     kw[i] = *reinterpret_cast<const uint32_t*>(kc + mx_k_chunk<NB>(kk, block) + ((p.dim >> 3) & 3) * 4);
@@ -290,6 +299,7 @@ __global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_read_kernel(const uint8_t
   }
 #pragma unroll
   for (int i = 0; i < NB; ++i) {
+    if (!P::live(i, s.lo, s.hi)) continue;
     const P p(i, lane);
     uint32_t kc_[P::LOADS], ks_[P::LOADS], vc_[P::LOADS], vs_[P::LOADS];
     mx_parts<P>(kw[i], ks[i], lane, kc_, ks_);
@@ -393,7 +403,7 @@ __global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T*
   using C = MxAttn<T, NB, NQ>;
   constexpr int DP = C::DP, SETS = C::SETS, ACC = C::ACC, QSETS = C::QSETS, PARTS = C::PARTS, TB = mx_tile_bytes(DP);
   extern __shared__ __align__(16) char mx_lds[];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, waves = blockDim.x >> 6;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, waves = blockDim.x >> 6;
   const int c = lane & 15, kg = lane >> 4;
 
   const unsigned split = a.groups == 1 ? blockIdx.x : blockIdx.x / (unsigned)a.groups, chunk = blockIdx.x - split * a.groups;
