@@ -42,7 +42,9 @@ extern "C" {
 
 /* PHOTON_FP8_E4M3: 8-bit floating point (OCP E4M3: bias 7, no infinities, largest finite value 448), accepted only
  * as the storage type of a coarse K/V cache (photon_config.kv_dt, photon_coarse_decode_attn). */
-typedef enum { PHOTON_F32 = 0, PHOTON_BF16 = 1, PHOTON_FP8_E4M3 = 2 } photon_dtype;
+/* PHOTON_MXFP4: 4-bit floating point in blocks of 32 under a scale (see photon_mxfp4_cache_write), accepted only as
+ * photon_config.kv_dt. */
+typedef enum { PHOTON_F32 = 0, PHOTON_BF16 = 1, PHOTON_FP8_E4M3 = 2, PHOTON_MXFP4 = 3 } photon_dtype;
 
 typedef enum {
   PHOTON_OK = 0,
@@ -311,7 +313,10 @@ typedef struct photon_config {
   photon_dtype dt;               /* storage of matrices and tables */
   photon_dtype kv_dt;            /* storage of the coarse K/V caches (state and hierarchical state): equal to dt, or
                                     PHOTON_FP8_E4M3 with dt == PHOTON_BF16: entries are rounded to nearest even from their
-                                    fp32 values and saturate at +-448; no scale factor (a variant beyond the paper) */
+                                    fp32 values and saturate at +-448; no scale factor (a variant beyond the paper), or
+                                    PHOTON_MXFP4 with dt == PHOTON_BF16: entries in 4 bits with a scale per 32 elements, every
+                                    layer's cache as photon_mxfp4_cache_write lays it out (photon_mxfp4_cache_bytes(Bt, H,
+                                    d_h, S_max) bytes of K and of V; a variant beyond the paper as well) */
   float rms_eps;
   float rope_theta;              /* 0 disables the rotary encoding */
 } photon_config;
@@ -342,7 +347,7 @@ typedef struct photon_weights {
 } photon_weights;
 
 typedef struct photon_state {
-  void* k_cache;        /* [n_layers, Bt, H, S_max, photon_kv_row_elems(d_h)] kv_dt : KV^(L) */
+  void* k_cache;        /* [n_layers, Bt, H, S_max, photon_kv_row_elems(d_h)] kv_dt : KV^(L); kv_dt PHOTON_MXFP4: n_layers caches */
   void* v_cache;
   int32_t* seq_len;     /* [Bt] entries cached per sequence; the step adds 1.  Must be < S_max on entry (else see status). */
   float* x_top;         /* [Bt, D]       X^(L)_g, replaced by X^(L)_{g+1} */

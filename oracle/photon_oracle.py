@@ -153,9 +153,11 @@ def mxfp4_decode_attn(q, k, v, seq_len, n_new, scale):
 
 
 def kv_store(cfg, x):
-    """What the coarse K/V cache holds for the value x: x itself, or its E4M3
-    rounding when the configuration stores the cache in 8 bits (reading G19)."""
-    return e4m3_round(x) if getattr(cfg, "kv_dtype", "") == "fp8" else f64(x)
+    """What the coarse K/V cache holds for rows x [..., d_h]: x itself, or its E4M3
+    (MXFP4) rounding when the configuration stores the cache in 8 (4) bits
+    (reading G19)."""
+    kv = getattr(cfg, "kv_dtype", "")
+    return e4m3_round(x) if kv == "fp8" else mxfp4_round(x) if kv == "mxfp4" else f64(x)
 
 
 def rmsnorm(x, g, eps):

@@ -11,7 +11,7 @@ import torch  # imported before the library so both share one HIP runtime
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB: Optional[C.CDLL] = None
 
-PHOTON_F32, PHOTON_BF16, PHOTON_FP8_E4M3 = 0, 1, 2
+PHOTON_F32, PHOTON_BF16, PHOTON_FP8_E4M3, PHOTON_MXFP4 = 0, 1, 2, 3
 
 
 class PhotonError(RuntimeError):
@@ -517,7 +517,7 @@ def _c_config(cfg) -> _Config:
         c.C[i], c.R[i] = cfg.C[i], cfg.R[i]
     c.D, c.H, c.d_h, c.n_layers, c.d_ff, c.vocab = cfg.D, cfg.H, cfg.d_h, cfg.n_layers, cfg.d_ff, cfg.vocab
     c.dt = PHOTON_BF16 if cfg.dtype == "bf16" else PHOTON_F32
-    c.kv_dt = PHOTON_FP8_E4M3 if getattr(cfg, "kv_dtype", "") == "fp8" else c.dt
+    c.kv_dt = {"fp8": PHOTON_FP8_E4M3, "mxfp4": PHOTON_MXFP4}.get(getattr(cfg, "kv_dtype", ""), c.dt)
     c.rms_eps, c.rope_theta = cfg.rms_eps, cfg.rope_theta
     return c
 
@@ -532,7 +532,7 @@ class PhotonModel:
         self.device = torch.device(device)
         self.mat_dtype = torch.bfloat16 if cfg.dtype == "bf16" else torch.float32
         # coarse K/V caches: the matrices' type, or E4M3 bit patterns held as uint8
-        self.kv_dtype = torch.uint8 if getattr(cfg, "kv_dtype", "") == "fp8" else self.mat_dtype
+        self.kv_dtype = torch.uint8 if getattr(cfg, "kv_dtype", "") in ("fp8", "mxfp4") else self.mat_dtype
         self._keep = []
         self.c_cfg = _c_config(cfg)
         w = _Weights()
@@ -595,6 +595,13 @@ class PhotonModel:
         m.g_final = self._vec(mod["g_final"])
 
 
+def _kv_shape(cfg, Bt: int, S_max: int):
+    """Shape of the K (or V) caches of all layers: rows of a type, or the tiles of a 4-bit cache."""
+    if getattr(cfg, "kv_dtype", "") == "mxfp4":
+        return (cfg.n_layers, Bt, cfg.H, (S_max + MXFP4_TILE - 1) // MXFP4_TILE, photon_mxfp4_tile_bytes(cfg.d_h))
+    return (cfg.n_layers, Bt, cfg.H, S_max, photon_kv_row_elems(cfg.d_h))
+
+
 class PhotonState:
     """Decode state on the device: coarse K/V cache, per-sequence lengths, top
     state, carries, and the step's workspace."""
@@ -609,16 +616,16 @@ class PhotonState:
         _register_step(lib)
         self.model, self.Bt, self.S_max = model, Bt, S_max
         # cache rows hold photon_kv_row_elems(d_h) elements; a cache given with rows of d_h is zero-padded
-        shape = (cfg.n_layers, Bt, cfg.H, S_max, photon_kv_row_elems(cfg.d_h))
+        shape = _kv_shape(cfg, Bt, S_max)
 
         def put(a, dtype, shp):
             if a is None:
                 return torch.zeros(shp, dtype=dtype, device=dev)
             t = a if isinstance(a, torch.Tensor) else torch.from_numpy(np_contig(a))
             if dtype == torch.uint8 and t.dtype != torch.uint8:
-                raise PhotonError(-1, "an 8-bit cache is given as E4M3 bit patterns (uint8)")
+                raise PhotonError(-1, "an 8-bit cache is given as E4M3 bit patterns, a 4-bit cache as its tiles (uint8)")
             t = t.to(device=dev, dtype=dtype)
-            if len(shp) == 5:
+            if len(shp) == 5 and getattr(cfg, "kv_dtype", "") != "mxfp4":
                 t = pad_kv_rows(t, cfg.d_h)
             t = t.contiguous()
             assert tuple(t.shape) == tuple(shp), (t.shape, shp)
@@ -681,16 +688,16 @@ class PhotonHierState:
             caps[l] = cap
             cap *= cfg.C[l - 1]
         for l in range(1, cfg.L):
-            shape = (cfg.n_layers, Bt, cfg.H, caps[l], photon_kv_row_elems(cfg.d_h))
+            shape = _kv_shape(cfg, Bt, caps[l])
 
             def put(a, dtype, shp):
                 if a is None:
                     return torch.zeros(shp, dtype=dtype, device=dev)
                 t = a if isinstance(a, torch.Tensor) else torch.from_numpy(np_contig(a))
                 if dtype == torch.uint8 and t.dtype != torch.uint8:
-                    raise PhotonError(-1, "an 8-bit cache is given as E4M3 bit patterns (uint8)")
+                    raise PhotonError(-1, "an 8-bit cache is given as E4M3 bit patterns, a 4-bit cache as its tiles (uint8)")
                 t = t.to(device=dev, dtype=dtype)
-                if len(shp) == 5:
+                if len(shp) == 5 and getattr(cfg, "kv_dtype", "") != "mxfp4":
                     t = pad_kv_rows(t, cfg.d_h)
                 t = t.contiguous()
                 assert tuple(t.shape) == tuple(shp), (t.shape, shp)

@@ -36,4 +36,14 @@ template <int NB> __device__ __forceinline__ int mx_v_word(int kk, int dim) {
 }
 template <int NB> __device__ __forceinline__ int mx_v_scale(int kk, int block) { return NB * MX_TILE * 16 + kk * NB + block; }
 
+// Launches for the decode step and the prefill: fp32 rows, H_kv = H.
+size_t mx_cache_bytes(int Bt, int H_kv, int d_h, int64_t S_max);
+// photon_mxfp4_cache_write of rows at positions start[b] + add + t (start NULL: add + t).
+int32_t launch_mx_write(const float* k, const float* v, int64_t row_stride, void* kc, void* vc, const int32_t* start, int add, int Bt, int T, int H,
+                        int d_h, int64_t S_max, hipStream_t st);
+// photon_mxfp4_decode_attn with seq_len[b] + add entries; out_bf16: the fp32 results rounded to bf16.
+int32_t launch_mx_attn(const float* q, const void* kc, const void* vc, const int32_t* seq_len, int add, void* out, bool out_bf16, int Bt, int T, int H,
+                       int d_h, int64_t S_max, float scale, int n_splits, void* ws, hipStream_t st);
+int mx_auto_splits(int Bt, int T, int H, int H_kv, int64_t S_max);
+
 }  // namespace photon

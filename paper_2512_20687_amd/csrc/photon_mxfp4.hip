@@ -190,7 +190,7 @@ struct MxRows {                  // a stretch of rows and the positions it belon
   const int32_t *start, *n_new;  // [Bt] or NULL: position of row 0 (0), rows in use (T)
   int64_t row_stride;            // elements from a row to the next
   int64_t S_max;
-  int T, H_kv, d_h;
+  int T, H_kv, d_h, add;         // add: to start
   bool heads_first;              // neighbouring workgroups take neighbouring heads of the same positions, else the other way round
 };
 
@@ -207,7 +207,7 @@ __device__ __forceinline__ bool mx_share(const MxRows& a, MxShare& s, bool& outs
   s.h = !a.heads_first ? major : a.H_kv % 8 == 0 ? minor % 8 * (a.H_kv / 8) + minor / 8 : minor;
   int64_t n = a.n_new ? a.n_new[s.b] : a.T;
   n = n < 0 ? 0 : n > a.T ? a.T : n;
-  const int64_t first = a.start ? a.start[s.b] : 0;
+  const int64_t first = (a.start ? (int64_t)a.start[s.b] : 0) + a.add;
   const int64_t begin = first < 0 ? 0 : first, end = first + n < a.S_max ? first + n : a.S_max;
   outside = n > 0 && (first < 0 || first + n > a.S_max);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);           // the same in the wave: what follows is scalar
@@ -405,13 +405,20 @@ struct MxQueries {
   const int32_t *seq_len, *n_new;
   int64_t q_stride, S_max;
   int T, H, H_kv, d_h, group, groups, n_splits;    // group: query heads of a K/V head; groups: workgroups that share its T * group queries
+  int add;                                         // to seq_len
+  bool out_bf16;                                   // fp32 queries with bf16 results
   float scale_log2e;
 };
 
+template <typename T> __device__ __forceinline__ void mx_put(T* out, int64_t at, float y, bool bf16) {
+  if (sizeof(T) == 4 && bf16) reinterpret_cast<bf16_t*>(out)[at] = from_f32<bf16_t>(y);
+  else out[at] = from_f32<T>(y);
+}
+
 // Positions that count for sequence b, and its queries.
 __device__ __forceinline__ void mx_sequence(const MxQueries& a, int b, int& n, int& m) {
-  n = a.seq_len[b];
-  n = n < 0 ? 0 : n > (int)a.S_max ? (int)a.S_max : n;                       // S_max < 2^31
+  const int64_t all = (int64_t)a.seq_len[b] + a.add;
+  n = all < 0 ? 0 : all > a.S_max ? (int)a.S_max : (int)all;                // S_max < 2^31
   m = a.n_new ? a.n_new[b] : a.T;
   m = m < 0 ? 0 : m > a.T ? a.T : m;
 }
@@ -739,7 +746,7 @@ __global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T*
     const int row = first_q + i, t = a.group == 1 ? row : row / a.group, h = hk * a.group + row - t * a.group;
     const int64_t to = ((int64_t)b * a.T + t) * a.H + h;
     if (a.n_splits == 1) {
-      if (d < a.d_h) out[to * a.d_h + d] = from_f32<T>(n - m + t + 1 > 0 ? o / l : 0.f);
+      if (d < a.d_h) mx_put(out, to * a.d_h + d, n - m + t + 1 > 0 ? o / l : 0.f, a.out_bf16);
     } else {
       float* p = ws + (to * a.n_splits + split) * (DP + 2);
       if (d == 0) { p[0] = mx; p[1] = l; }
@@ -787,7 +794,7 @@ __global__ __launch_bounds__(NB * MX_BLOCK) void mxfp4_merge_kernel(const float*
       o = fmaf(s_o[u], f, o);
     }
   }
-  if (d < a.d_h) out[to * a.d_h + d] = from_f32<T>(n - m + t + 1 > 0 ? o / l : 0.f);
+  if (d < a.d_h) mx_put(out, to * a.d_h + d, n - m + t + 1 > 0 ? o / l : 0.f, a.out_bf16);
 }
 
 // Queries that share what a workgroup reads.  fp32: at most 4 (the operands of 8 are 96 registers a lane: 120 spilled).
@@ -890,7 +897,7 @@ int32_t rows_args(const char* who, const void* k, const void* v, const void* kc,
 MxRows mx_rows(const int32_t* start, const int32_t* n_new, int64_t row_stride, int32_t T, int32_t H_kv, int32_t d_h, int64_t S_max) {
   MxRows a;
   a.start = start; a.n_new = n_new; a.row_stride = row_stride; a.S_max = S_max;
-  a.T = T; a.H_kv = H_kv; a.d_h = d_h;
+  a.T = T; a.H_kv = H_kv; a.d_h = d_h; a.add = 0; a.heads_first = true;
   return a;
 }
 
@@ -935,9 +942,33 @@ extern "C" int32_t photon_mxfp4_tile_bytes(int32_t d_h) {
   return d_p == 0 ? 0 : mx_tile_bytes(d_p);
 }
 
+namespace photon {
+
+size_t mx_cache_bytes(int Bt, int H_kv, int d_h, int64_t S_max) {
+  return (size_t)Bt * H_kv * (size_t)((S_max + MX_TILE - 1) / MX_TILE) * photon_mxfp4_tile_bytes(d_h);
+}
+
+int32_t launch_mx_write(const float* k, const float* v, int64_t row_stride, void* kc, void* vc, const int32_t* start, int add, int Bt, int T, int H,
+                        int d_h, int64_t S_max, hipStream_t st) {
+  MxRows a = mx_rows(start, nullptr, row_stride, T, H, d_h, S_max);
+  a.add = add;
+  return launch_rows_t<float>(true, k, v, kc, vc, nullptr, a, Bt, st);
+}
+
+int32_t launch_mx_attn(const float* q, const void* kc, const void* vc, const int32_t* seq_len, int add, void* out, bool out_bf16, int Bt, int T, int H,
+                       int d_h, int64_t S_max, float scale, int n_splits, void* ws, hipStream_t st) {
+  MxQueries a;
+  a.seq_len = seq_len; a.n_new = nullptr; a.q_stride = (int64_t)H * d_h; a.S_max = S_max;
+  a.T = T; a.H = H; a.H_kv = H; a.d_h = d_h; a.group = 1; a.groups = 1; a.n_splits = n_splits; a.add = add; a.out_bf16 = out_bf16;
+  a.scale_log2e = scale * LOG2E;
+  return mx_launch_attn_t<float>(q, kc, vc, out, ws, a, Bt, st);
+}
+
+}  // namespace photon
+
 extern "C" size_t photon_mxfp4_cache_bytes(int32_t Bt, int32_t H_kv, int32_t d_h, int64_t S_max) {
   if (Bt <= 0 || H_kv <= 0 || S_max <= 0) return 0;
-  return (size_t)Bt * H_kv * (size_t)((S_max + MX_TILE - 1) / MX_TILE) * photon_mxfp4_tile_bytes(d_h);
+  return mx_cache_bytes(Bt, H_kv, d_h, S_max);
 }
 
 extern "C" int32_t photon_mxfp4_cache_write(const void* k, const void* v, int64_t row_stride, void* k_cache, void* v_cache, const int32_t* start,
@@ -997,7 +1028,7 @@ extern "C" int32_t photon_mxfp4_decode_attn(const void* q, int64_t q_stride, con
   }
   MxQueries a;
   a.seq_len = seq_len; a.n_new = n_new; a.q_stride = q_stride; a.S_max = S_max;
-  a.T = T; a.H = H; a.H_kv = H_kv; a.d_h = d_h; a.group = H / H_kv; a.groups = 1; a.n_splits = n_splits;
+  a.T = T; a.H = H; a.H_kv = H_kv; a.d_h = d_h; a.group = H / H_kv; a.groups = 1; a.n_splits = n_splits; a.add = 0; a.out_bf16 = false;
   a.scale_log2e = scale * LOG2E;
   if (dt == PHOTON_F32) return mx_launch_attn_t<float>(q, k_cache, v_cache, out, workspace, a, Bt, (hipStream_t)stream);
   return mx_launch_attn_t<bf16_t>(q, k_cache, v_cache, out, workspace, a, Bt, (hipStream_t)stream);

@@ -4,10 +4,14 @@
 // sequence lengths and tokens stay in device memory, so the enqueue pattern does
 // not depend on data and the whole step can be captured in a HIP graph.
 #include "photon_attn.h"
+
+#include <algorithm>
+
 #include "photon_encoder_attn.h"
 #include "photon_device.h"
 #include "photon_host.h"
 #include "photon_linear.h"
+#include "photon_mxfp4.h"
 #include "photon_persistent.h"
 #include "photon_small.h"
 
@@ -140,6 +144,37 @@ __global__ __launch_bounds__(256) void rope_append_coarse_kernel(const float* __
   vc[slot + i] = from_f32<TKV>(va);
   vc[slot + i + half] = from_f32<TKV>(vb);
   for (int p = d_h + i; p < pitch; p += half) { kc[slot + p] = TKV{}; vc[slot + p] = TKV{}; }
+}
+
+// The same for a cache in 4 bits, whose entries a pass over whole blocks writes: k rotated and v summed up go back to the first
+// part's rows.  seq_len == nullptr: positions 0 .. n_new - 1 of every sequence (a prompt); qrot == nullptr: no queries.
+__global__ __launch_bounds__(256) void rope_rows_kernel(float* __restrict__ qkv, int n_parts, int64_t part_stride, float* __restrict__ qrot,
+                                                        const int32_t* __restrict__ seq_len, int64_t rows, int64_t n_new, int first, int H, int d_h,
+                                                        float theta) {
+  const int half = d_h >> 1, D = H * d_h;
+  const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (idx >= rows * H * half) return;
+  const int i = (int)(idx % half);
+  const int h = (int)((idx / half) % H);
+  const int64_t row = idx / ((int64_t)half * H), b = row / n_new;
+  const int pos = (seq_len != nullptr ? seq_len[b] + first : 0) + (int)(row - b * n_new);
+  float* src = qkv + row * 3 * D + h * d_h;
+  float ka = src[D + i], kb = src[D + i + half];
+  float c, s;
+  rope_angle(pos, i, d_h, theta, c, s);
+  if (qrot != nullptr) {
+    float qa = src[i], qb = src[i + half], va = src[2 * D + i], vb = src[2 * D + i + half];
+    for (int p = 1; p < n_parts; ++p) {
+      const float* more = src + p * part_stride;
+      qa += more[i]; qb += more[i + half]; ka += more[D + i]; kb += more[D + i + half]; va += more[2 * D + i]; vb += more[2 * D + i + half];
+    }
+    float* qd = qrot + row * D + h * d_h;
+    qd[i] = fmaf(qa, c, -(qb * s));
+    qd[i + half] = fmaf(qa, s, qb * c);
+    if (n_parts > 1) { src[2 * D + i] = va; src[2 * D + i + half] = vb; }
+  }
+  src[D + i] = fmaf(ka, c, -(kb * s));
+  src[D + i + half] = fmaf(ka, s, kb * c);
 }
 
 // Token choice for one row of logits (greedy, lowest index on ties, or the forced token), then the
@@ -327,8 +362,9 @@ static Plan make_plan(const photon_config& c, int Bt, int64_t S_max) {
 static int32_t validate_config(const photon_config* c, int Bt, int64_t S_max) {
   PHOTON_REQUIRE(c != nullptr, PHOTON_ERR_INVALID_ARG, "config is null");
   PHOTON_REQUIRE(valid_dtype(c->dt), PHOTON_ERR_UNSUPPORTED, "unknown dtype %d", (int)c->dt);
-  PHOTON_REQUIRE(c->kv_dt == c->dt || (c->dt == PHOTON_BF16 && c->kv_dt == PHOTON_FP8_E4M3), PHOTON_ERR_UNSUPPORTED,
-                 "kv_dt=%d must equal dt=%d, or be 8-bit with bf16 matrices", (int)c->kv_dt, (int)c->dt);
+  PHOTON_REQUIRE(c->kv_dt == c->dt || (c->dt == PHOTON_BF16 && (c->kv_dt == PHOTON_FP8_E4M3 || c->kv_dt == PHOTON_MXFP4)), PHOTON_ERR_UNSUPPORTED,
+                 "kv_dt=%d must equal dt=%d, or be 8-bit or 4-bit with bf16 matrices", (int)c->kv_dt, (int)c->dt);
+  PHOTON_REQUIRE(c->kv_dt != PHOTON_MXFP4 || S_max <= 0x7fffffff, PHOTON_ERR_UNSUPPORTED, "S_max=%lld exceeds what a 4-bit cache counts", (long long)S_max);
   PHOTON_REQUIRE(c->L >= 1 && c->L <= PHOTON_MAX_LEVELS, PHOTON_ERR_INVALID_ARG, "L=%d not in [1, %d]", c->L, (int)PHOTON_MAX_LEVELS);
   PHOTON_REQUIRE(Bt > 0 && S_max > 0, PHOTON_ERR_INVALID_ARG, "Bt=%d and S_max=%lld must be positive", Bt, (long long)S_max);
   PHOTON_REQUIRE(c->D > 0 && c->H > 0 && c->d_h > 0 && c->H * c->d_h == c->D, PHOTON_ERR_INVALID_ARG,
@@ -356,6 +392,12 @@ static int32_t validate_config(const photon_config* c, int Bt, int64_t S_max) {
 }
 
 // ------------------------------------------------------------------ composition
+
+// Bytes of one layer's K (or V) cache of capacity S.
+static size_t layer_cache_bytes(const photon_config& c, int Bt, int64_t S) {
+  if (c.kv_dt == PHOTON_MXFP4) return mx_cache_bytes(Bt, c.H, c.d_h, S);
+  return (size_t)Bt * c.H * S * kv_row_elems(c.d_h) * dtype_size(c.kv_dt);
+}
 
 struct Ctx {
   const photon_config* c;
@@ -578,9 +620,10 @@ static int32_t stream_step(const Ctx& x, const photon_module_weights& mod, void*
   }
   const bool many = many_rows(x, rows);
   float *qrot = x.f(x.o_qrot), *attn = x.f(x.o_attn);
-  const size_t esz = dtype_size(c.kv_dt);
   const int pitch = kv_row_elems(c.d_h);
-  const size_t layer_cache = (size_t)x.Bt * c.H * S_cap * pitch * esz;
+  const size_t layer_cache = layer_cache_bytes(c, x.Bt, S_cap);
+  const bool mx = c.kv_dt == PHOTON_MXFP4;
+  if (mx) n_splits = std::min(n_splits, mx_auto_splits(x.Bt, units, c.H, c.H, S_cap));   // partial results of the same size
   const float scale = 1.0f / sqrtf((float)c.d_h);
   for (int i = 0; i < c.n_layers; ++i) {
     const photon_layer_weights& lw = mod.layers[i];
@@ -591,6 +634,17 @@ static int32_t stream_step(const Ctx& x, const photon_module_weights& mod, void*
     const float* qkv0 = qkv.n_parts ? qkv.parts : qkv.x;
     const int qkv_parts = qkv.n_parts ? qkv.n_parts : 1;
     const int64_t n_el = (int64_t)rows * c.H * (c.d_h / 2);
+    if (mx) {
+      float* rows_at = const_cast<float*>(qkv0);             // dead once the attention has run
+      PHOTON_LAUNCH(KC_ROPE_APPEND, x.st, rope_rows_kernel, dim3(blocks_for(n_el)), dim3(256), 0, x.st, rows_at, qkv_parts, qkv.part_stride, qrot, seq_len,
+                    (int64_t)rows, (int64_t)units, first, c.H, c.d_h, c.rope_theta);
+      PHOTON_TRY(check_launch("rope_rows_kernel"));
+      PHOTON_TRY(launch_mx_write(rows_at + c.D, rows_at + 2 * c.D, 3 * (int64_t)c.D, kc, vc, seq_len, first, x.Bt, units, c.H, c.d_h, S_cap, x.st));
+      PHOTON_TRY(launch_mx_attn(qrot, kc, vc, seq_len, first + units, attn, many, x.Bt, units, c.H, c.d_h, S_cap, scale, n_splits,
+                                n_new > 0 ? ws : x.base + x.p.coarse_ws, x.st));
+      PHOTON_TRY(block_tail(x, lw, in, rows, many, &in));
+      continue;
+    }
     if (c.kv_dt == PHOTON_FP8_E4M3)
       PHOTON_LAUNCH(KC_ROPE_APPEND, x.st, rope_append_coarse_kernel<fp8_t>, dim3(blocks_for(n_el)), dim3(256), 0, x.st, qkv0, qkv_parts, qkv.part_stride, qrot,
                     (fp8_t*)kc, (fp8_t*)vc, seq_len, rows, units, first, c.H, c.d_h, pitch, S_cap, c.rope_theta);
@@ -948,7 +1002,7 @@ static int32_t prefill_impl(const Ctx& x, Ctx e, const PrefillPlan& pp, const ph
   const photon_config& c = *x.c;
   const int D = c.D, L = c.L, Bt = x.Bt;
   const float scale = 1.0f / sqrtf((float)c.d_h);
-  const size_t esz = dtype_size(c.kv_dt);
+  const bool mx = c.kv_dt == PHOTON_MXFP4;
 
   float *A = e.f(pp.A), *qkv = e.f(pp.qkv), *attn = e.f(pp.attn);
   float* before_last = e.f(pp.before_last);                // X^(L) in front of the last one, one row per sequence
@@ -972,10 +1026,12 @@ static int32_t prefill_impl(const Ctx& x, Ctx e, const PrefillPlan& pp, const ph
     else if (l > 1)
       PHOTON_TRY(linear(e, RowSource{e.f(pp.X[l - 1]), (int64_t)C * D}, ew.chunker_w[l - 1], nullptr, ew.chunker_b[l - 1], A, D, rows, D, C * D));
     RowSource in{A, D};
-    const size_t layer_cache = (size_t)Bt * c.H * x.s->S_max * kv_row_elems(c.d_h) * esz;
+    const size_t layer_cache = layer_cache_bytes(c, Bt, x.s->S_max);
     // Where it pays, the projection writes the attention's operands itself; a separate pass over it takes the angles'
     // cosines and sines from the same table.
-    const bool fused = many_rows(e, rows) && qkv_rope_pays(rows, D, c.d_h);
+    // A cache in 4 bits takes its entries from the fp32 rows, rounded once: no fused projection where one is filled.
+    const bool fills = l == L || x.hs != nullptr;
+    const bool fused = many_rows(e, rows) && qkv_rope_pays(rows, D, c.d_h) && !(mx && fills);
     QkvOperands ops;
     float* table = e.f(pp.table);
     if (x.bf16) PHOTON_TRY(encoder_operands_begin(Bt, M, c.H, c.d_h, c.rope_theta, scale, fused, e.base + pp.ea, table, &ops, x.st));
@@ -988,7 +1044,7 @@ static int32_t prefill_impl(const Ctx& x, Ctx e, const PrefillPlan& pp, const ph
         vc = reinterpret_cast<char*>(x.s->v_cache) + (size_t)i * layer_cache;
       } else if (x.hs != nullptr) {                        // hierarchical generation keeps every level's stream
         cap = x.hs->S_cap[l - 1];
-        const size_t lc = (size_t)Bt * c.H * cap * kv_row_elems(c.d_h) * esz;
+        const size_t lc = layer_cache_bytes(c, Bt, cap);
         kc = reinterpret_cast<char*>(x.hs->k_cache[l - 1]) + (size_t)i * lc;
         vc = reinterpret_cast<char*>(x.hs->v_cache[l - 1]) + (size_t)i * lc;
       }
@@ -1001,7 +1057,13 @@ static int32_t prefill_impl(const Ctx& x, Ctx e, const PrefillPlan& pp, const ph
       } else {
         RowSource qkv_rows;
         PHOTON_TRY(block_qkv(e, lw, &in, rows, false, &qkv_rows));
-        PHOTON_TRY(launch_encoder_attn(qkv, attn, Bt, M, c.H, c.d_h, c.rope_theta, scale, kc, vc, cap, e.base + pp.ea, x.bf16, c.kv_dt == PHOTON_FP8_E4M3, x.bf16, x.st, table));
+        PHOTON_TRY(launch_encoder_attn(qkv, attn, Bt, M, c.H, c.d_h, c.rope_theta, scale, mx ? nullptr : kc, mx ? nullptr : vc, cap, e.base + pp.ea, x.bf16, c.kv_dt == PHOTON_FP8_E4M3, x.bf16, x.st, table));
+        if (mx && kc != nullptr) {
+          PHOTON_LAUNCH(KC_ROPE_APPEND, x.st, rope_rows_kernel, dim3(blocks_for((int64_t)rows * c.H * (c.d_h / 2))), dim3(256), 0, x.st, qkv, 1,
+                        (int64_t)0, (float*)nullptr, (const int32_t*)nullptr, (int64_t)rows, M, 0, c.H, c.d_h, c.rope_theta);
+          PHOTON_TRY(check_launch("rope_rows_kernel"));
+          PHOTON_TRY(launch_mx_write(qkv + D, qkv + 2 * D, 3 * (int64_t)D, kc, vc, nullptr, 0, Bt, (int)M, c.H, c.d_h, cap, x.st));
+        }
       }
       PHOTON_TRY(block_tail(e, lw, in, rows, x.bf16, &in));
     }
