@@ -336,7 +336,7 @@ __global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_read_kernel(const uint8_t
 //     elements of V as columns.  The weights change from a lane per position to operand order through LDS.
 //   The reference of the exponentials is the largest score when it was last raised, which happens when one exceeds it by more
 //     than MX_RAISE: fp32 and bf16 lose nothing by weights up to 2^MX_RAISE, and the usual tile needs no maximum.
-constexpr float MX_RAISE = 16.f;
+constexpr float MX_RAISE = 8.f;
 constexpr int MX_ATTN_WAVES = 8;                 // of a workgroup, at most
 constexpr int MX_P_PITCH = 72;                   // bf16 elements of a weight row in LDS: 64 positions, rows on different banks
 
@@ -825,7 +825,7 @@ template <typename T, int NB, int NQ>
 int32_t mx_launch_attn(const void* q, const void* kc, const void* vc, void* out, void* ws, const MxQueries& a, int Bt, hipStream_t st) {
   const int waves = mx_waves((int64_t)Bt * a.H_kv * a.groups, a.S_max, a.n_splits);
   const unsigned lds = waves * (MxAttn<T, NB, NQ>::WAVE_BYTES);
-  PHOTON_LAUNCH(KC_COARSE_ATTN, st, (mxfp4_attn_kernel<T, NB, NQ>), dim3((unsigned)(a.n_splits * a.groups), a.H_kv, Bt),
+  PHOTON_LAUNCH(KC_COARSE_ATTN, st, (mxfp4_attn_kernel<T, NB, NQ>), dim3((unsigned)a.n_splits * (unsigned)a.groups, a.H_kv, Bt),
                 dim3(waves * 64), lds, st, (const T*)q, (const uint8_t*)kc, (const uint8_t*)vc, (T*)out, (float*)ws, a);
   const int32_t rc = check_launch("mxfp4_attn_kernel");
   if (rc != PHOTON_OK || a.n_splits == 1) return rc;
@@ -890,7 +890,8 @@ int32_t rows_args(const char* who, const void* k, const void* v, const void* kc,
   PHOTON_REQUIRE(kc && vc && aligned16(kc) && aligned16(vc), PHOTON_ERR_INVALID_ARG, "%s: the caches must be non-null, 16-byte aligned device pointers", who);
   PHOTON_REQUIRE(row_stride >= (int64_t)a.H_kv * a.d_h, PHOTON_ERR_INVALID_ARG, "%s: row_stride=%lld is less than a row of %d heads of %d", who,
                  (long long)row_stride, a.H_kv, a.d_h);
-  PHOTON_REQUIRE(mx_row_groups(a.T) * a.H_kv <= 0x7fffffff, PHOTON_ERR_UNSUPPORTED, "%s: T=%d rows of %d heads are too many", who, a.T, a.H_kv);
+  PHOTON_REQUIRE(kc != vc, PHOTON_ERR_INVALID_ARG, "%s: K and V need a cache each", who);
+  PHOTON_REQUIRE(mx_row_groups(a.T) * a.H_kv <= (int64_t)0xffffffff / (MX_WAVES * 64), PHOTON_ERR_UNSUPPORTED, "%s: T=%d rows of %d heads are too many", who, a.T, a.H_kv);
   return PHOTON_OK;
 }
 
@@ -1018,6 +1019,9 @@ extern "C" int32_t photon_mxfp4_decode_attn(const void* q, int64_t q_stride, con
   PHOTON_REQUIRE_PTR(k_cache);
   PHOTON_REQUIRE_PTR(v_cache);
   PHOTON_REQUIRE(seq_len != nullptr, PHOTON_ERR_INVALID_ARG, "%s: seq_len is null", __func__);
+  PHOTON_REQUIRE(k_cache != v_cache, PHOTON_ERR_INVALID_ARG, "%s: K and V need a cache each", __func__);
+  PHOTON_REQUIRE(((int64_t)T * (H / H_kv) / 4 + 1) * (n_splits > 1 ? n_splits : 1) <= (int64_t)0xffffffff / (MX_ATTN_WAVES * 64) && n_splits <= 1024,
+                 PHOTON_ERR_UNSUPPORTED, "%s: T=%d queries of %d heads a K/V head are too many", __func__, T, H / H_kv);
   PHOTON_REQUIRE(q_stride >= (int64_t)H * d_h, PHOTON_ERR_INVALID_ARG, "%s: q_stride=%lld is less than a row of %d heads of %d", __func__,
                  (long long)q_stride, H, d_h);
   if (n_splits == 0) n_splits = photon_mxfp4_decode_attn_auto_splits(Bt, T, H, H_kv, S_max);

@@ -294,6 +294,52 @@ def test_attention_of_flat_and_sharp_scores(ph, dtype, spread):
     check_attention(ph, np.random.default_rng(2), 2, 2, 4, 2, 64, [3000, 777], dtype, spread=spread)
 
 
+@pytest.mark.parametrize("T", [1, 4])
+@pytest.mark.parametrize("order", [1, -1])
+def test_scores_that_rise_or_fall_along_the_cache(ph, order, T):
+    """Every tile's scores lie far above (below) those of the one before: the reference of the exponentials is raised in each."""
+    d_h, n = 64, 1000
+    rng = np.random.default_rng(14)
+    k = rng.standard_normal((1, n, 1, d_h)) * 0.05
+    k[0, ::order, 0, :32] += (np.arange(n) // 64 * 1.5)[:, None] / 32
+    v = rng.standard_normal((1, n, 1, d_h))
+    kc, vc = ph.mxfp4_cache(1, 1, d_h, n), ph.mxfp4_cache(1, 1, d_h, n)
+    k, v = (torch.from_numpy(a.astype(np.float32)).cuda() for a in (k, v))
+    ph.photon_mxfp4_cache_write(k, v, kc, vc)
+    kq, vq = (po.mxfp4_round(a.cpu().numpy()).transpose(0, 2, 1, 3) for a in (k, v))
+    for dtype in (torch.float32, torch.bfloat16):
+        q = torch.full((1, T, 1, d_h), 8.0, dtype=dtype, device="cuda")
+        out = torch.empty_like(q)
+        ph.photon_mxfp4_decode_attn(q, kc, vc, torch.tensor([n], dtype=torch.int32, device="cuda"), out, n_splits=1)
+        ref = po.mxfp4_decode_attn(q.float().cpu().numpy(), kq, vq, [n], [T], 0.125)
+        weight = po.mxfp4_decode_attn(q.float().cpu().numpy(), kq, np.abs(vq), [n], [T], 0.125)
+        # fp32 scores of up to 30: known to 30 * 2^-23, which is what the weights are off by; bf16 as above
+        bound = 1e-5 * weight if dtype == torch.float32 else 2.0 ** -8 * (np.abs(ref) + weight) + 1e-5 * weight
+        assert np.all(np.abs(out.float().cpu().numpy() - ref) <= bound)
+
+
+def test_two_streams_at_once(ph):
+    """Calls on two streams with caches and workspaces of their own do not meet."""
+    rng = np.random.default_rng(15)
+    sides = []
+    for i in range(2):
+        _, (kc, vc) = filled(rng, 2, 4, 64, [3000, 1500], 3000)
+        q = torch.from_numpy(rng.standard_normal((2, 1, 4, 64)).astype(np.float32)).cuda()
+        ws = torch.empty(ph.photon_mxfp4_decode_attn_workspace_bytes(2, 1, 4, 64, 8), dtype=torch.uint8, device="cuda")
+        lens = torch.tensor([3000, 1500], dtype=torch.int32, device="cuda")
+        want = torch.empty_like(q)
+        ph.photon_mxfp4_decode_attn(q, kc, vc, lens, want, n_splits=8, workspace=ws)
+        sides.append((torch.cuda.Stream(), q, kc, vc, lens, torch.empty_like(q), ws, want))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for stream, q, kc, vc, lens, out, ws, _ in sides:
+            with torch.cuda.stream(stream):
+                ph.photon_mxfp4_decode_attn(q, kc, vc, lens, out, n_splits=8, workspace=ws)
+    torch.cuda.synchronize()
+    for *_, out, _, want in sides:
+        assert torch.equal(out, want)
+
+
 def test_attention_over_a_long_cache(ph):
     check_attention(ph, np.random.default_rng(4), 1, 1, 1, 1, 64, [100003], torch.float32)
     check_attention(ph, np.random.default_rng(4), 1, 3, 4, 1, 128, [40001], torch.bfloat16)

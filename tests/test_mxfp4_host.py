@@ -92,17 +92,19 @@ def test_sizes(lib):
 
 
 P, ODD = ctypes.c_void_p(1 << 20), ctypes.c_void_p((1 << 20) + 2)        # never dereferenced: validation fails first
-WRITE = dict(k=P, v=P, stride=128, kc=P, vc=P, start=P, n=None, status=None, Bt=1, T=3, H=2, d=64, S=100, dt=0)
-READ = dict(kc=P, vc=P, start=P, n=None, k=P, v=P, stride=128, Bt=1, T=3, H=2, d=64, S=100, dt=0)
-ATTN = dict(q=P, stride=256, kc=P, vc=P, seq=P, n=None, out=P, Bt=1, T=3, H=4, H_kv=2, d=64, S=100, scale=0.1, splits=1, ws=None, ws_bytes=0, dt=0)
+Q = ctypes.c_void_p(1 << 21)
+WRITE = dict(k=P, v=P, stride=128, kc=P, vc=Q, start=P, n=None, status=None, Bt=1, T=3, H=2, d=64, S=100, dt=0)
+READ = dict(kc=P, vc=Q, start=P, n=None, k=P, v=P, stride=128, Bt=1, T=3, H=2, d=64, S=100, dt=0)
+ATTN = dict(q=P, stride=256, kc=P, vc=Q, seq=P, n=None, out=P, Bt=1, T=3, H=4, H_kv=2, d=64, S=100, scale=0.1, splits=1, ws=None, ws_bytes=0, dt=0)
 
 
 @pytest.mark.parametrize("change,code,text", [
     (dict(dt=2), -2, b"dtype 2"), (dict(dt=9), -2, b"dtype 9"), (dict(d=129, stride=999), -2, b"d_h=129"), (dict(d=0), -2, b"d_h=0"),
     (dict(Bt=-1), -1, b"Bt=-1"), (dict(T=-1), -1, b"T=-1"), (dict(H=0), -1, b"H_kv=0"), (dict(S=0), -1, b"S_max=0"),
     (dict(S=1 << 31), -2, b"S_max=2147483648"), (dict(k=None), -1, b"k and v"), (dict(v=None), -1, b"k and v"), (dict(k=ODD), -1, b"k and v"),
-    (dict(kc=None), -1, b"caches"), (dict(vc=ODD), -1, b"caches"), (dict(stride=127), -1, b"row_stride=127"), (dict(stride=0), -1, b"row_stride=0"),
+    (dict(vc=P), -1, b"a cache each"), (dict(kc=None), -1, b"caches"), (dict(vc=ODD), -1, b"caches"), (dict(stride=127), -1, b"row_stride=127"), (dict(stride=0), -1, b"row_stride=0"),
     (dict(Bt=1 << 16), -2, b"Bt=65536"), (dict(H=1 << 16, stride=1 << 30), -2, b"H_kv=65536"), (dict(H=60000, T=1 << 30, stride=1 << 30), -2, b"T=1073741824"),
+    (dict(T=1 << 30), -2, b"T=1073741824"),
 ])
 def test_write_and_read_refuse(lib, change, code, text):
     for fn, args in ((lib.photon_mxfp4_cache_write, WRITE), (lib.photon_mxfp4_cache_read, READ)):
@@ -116,7 +118,8 @@ def test_write_and_read_refuse(lib, change, code, text):
     (dict(q=None), -1, b"q and out"), (dict(out=ODD), -1, b"q and out"), (dict(kc=ODD), -1, b"k_cache"), (dict(vc=None), -1, b"v_cache"),
     (dict(seq=None), -1, b"seq_len"), (dict(stride=255), -1, b"q_stride=255"), (dict(splits=4), -3, b"workspace"),
     (dict(splits=4, ws=P, ws_bytes=4 * 3 * 4 * 66 * 4 - 1), -3, b"workspace"), (dict(splits=4, ws=ODD, ws_bytes=1 << 20), -3, b"workspace"),
-    (dict(Bt=1 << 16), -2, b"Bt=65536"), (dict(T=1 << 16), -2, b"T=65536"), (dict(H=1 << 16, stride=1 << 30), -2, b"H=65536"),
+    (dict(Bt=1 << 16), -2, b"Bt=65536"), (dict(T=1 << 16), -2, b"T=65536"), (dict(H=1 << 16, stride=1 << 30), -2, b"H=65536"), (dict(vc=P), -1, b"a cache each"),
+    (dict(T=65535, H=60000, H_kv=1, stride=1 << 30), -2, b"T=65535"),
 ])
 def test_attention_refuses(lib, change, code, text):
     assert lib.photon_mxfp4_decode_attn(*{**ATTN, **change}.values(), None) == code, lib.photon_last_error()
