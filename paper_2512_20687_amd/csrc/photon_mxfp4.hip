@@ -320,6 +320,178 @@ __global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_read_kernel(const uint8_t
   }
 }
 
+// ------------------------------------------------------------------ few rows
+//
+// A wave of the kernels above uses one lane in eight where a sequence has one new row, and the instructions that it issues are
+// what bounds a step's append.  Up to MX_FEW rows per sequence are taken with a lane per 8 elements of a head instead, all rows
+// of 64 / (4 NB) heads by one wave: 256 sequences append one bf16 row of 32 x 52 elements in 4.4 us (7.9 with the kernel above),
+// three in 5.3 (9.8), four in 6.1 (9.9) and read them back in 3.5 (5.8), 4.5 (7.6) and 5.0 (7.8); four sequences of 32 x 64 fp32
+// elements one in 2.9 (3.5), four in 4.0 (3.5).  V words are put together nibble by nibble, 8 of them a lane, in the one or two
+// groups of 8 positions that the rows are in.
+constexpr int MX_FEW = 4;        // rows of a sequence, at most
+
+struct MxFew {
+  int b, h, n;                   // sequence, head, rows in use that have a place
+  int dim;                       // first of the lane's 8 elements
+  int64_t begin, row0;           // position of the first of them, and its row
+  int64_t stream;
+};
+template <int NB> __device__ __forceinline__ bool mx_few(const MxRows& a, MxFew& s, bool& outside) {
+  constexpr int LANES = 4 * NB;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  s.b = blockIdx.y;
+  s.h = (blockIdx.x * (blockDim.x >> 6) + wave) * (64 / LANES) + lane / LANES;
+  s.dim = lane % LANES * 8;
+  int64_t n = a.n_new ? a.n_new[s.b] : a.T;
+  n = n < 0 ? 0 : n > a.T ? a.T : n;
+  const int64_t first = (a.start ? (int64_t)a.start[s.b] : 0) + a.add;
+  s.begin = first < 0 ? 0 : first;
+  const int64_t end = first + n < a.S_max ? first + n : a.S_max;
+  outside = n > 0 && (first < 0 || first + n > a.S_max);
+  s.n = end > s.begin ? (int)(end - s.begin) : 0;
+  s.row0 = (int64_t)s.b * a.T + s.begin - first;
+  s.stream = (int64_t)s.b * a.H_kv + s.h;
+  return s.n > 0;
+}
+// The byte of position pos's 8-position group in the stream's tiles.
+template <int NB> __device__ __forceinline__ int64_t mx_few_tile(const MxRows& a, const MxFew& s, int64_t pos) {
+  return (s.stream * ((a.S_max + MX_TILE - 1) / MX_TILE) + pos / MX_TILE) * mx_tile_bytes(NB * MX_BLOCK);
+}
+
+template <typename T, int NB, int VEC>
+__global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_write_few_kernel(const T* __restrict__ k, const T* __restrict__ v, uint8_t* __restrict__ kc,
+                                                                        uint8_t* __restrict__ vc, int32_t* __restrict__ status, MxRows a) {
+  MxFew s;
+  bool outside;
+  const bool any = mx_few<NB>(a, s, outside);
+  if (outside && status != nullptr && blockIdx.x == 0 && threadIdx.x == 0) atomicOr(status, (int)PHOTON_STATUS_CACHE_FULL);
+  if (!any) return;
+  const bool mine = s.h < a.H_kv;                          // a wave's heads past the last one load what the last one loads, and store nothing
+  if (!mine) { s.stream -= s.h - (a.H_kv - 1); s.h = a.H_kv - 1; }
+  MxRaw<T, 4, VEC> kr[MX_FEW][2], vr[MX_FEW][2];
+#pragma unroll
+  for (int t = 0; t < MX_FEW; ++t) {
+    if (t >= s.n) break;
+    const int64_t row = (s.row0 + t) * a.row_stride + (int64_t)s.h * a.d_h;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      kr[t][u].template load<false>(k + row, s.dim + 4 * u, a.d_h);
+      vr[t][u].template load<false>(v + row, s.dim + 4 * u, a.d_h);
+    }
+  }
+  const int in = (int)(s.begin & 7);                       // of the first group; rows from 8 - in on are in the second
+  const int groups = in + s.n > 8 ? 2 : 1, block = s.dim >> 5;
+  uint32_t held[2][8], word[2][8];
+#pragma unroll
+  for (int g = 0; g < 2; ++g)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) word[g][e] = held[g][e] = 0;
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    if (g >= groups) break;
+    const int64_t pos = s.begin + 8 * g;
+    const uint8_t* tile = vc + mx_few_tile<NB>(a, s, pos);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) held[g][e] = *reinterpret_cast<const uint32_t*>(tile + mx_v_word<NB>((int)(pos % MX_TILE) & ~7, s.dim + e));
+  }
+#pragma unroll
+  for (int t = 0; t < MX_FEW; ++t) {
+    if (t >= s.n) break;
+    const int64_t pos = s.begin + t;
+    const int kk = (int)(pos % MX_TILE), at = in + t;
+    uint32_t ks, vs, kw, vw;
+    float x[8];
+    auto values = [&](const MxRaw<T, 4, VEC> (&raw)[2]) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float y[4];
+        raw[u].values(s.dim + 4 * u, a.d_h, y);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[4 * u + e] = y[e];
+      }
+    };
+    values(kr[t]);
+    kw = mx_quantise(x, ks);
+    values(vr[t]);
+    vw = mx_quantise(x, vs);
+    const int64_t tile = mx_few_tile<NB>(a, s, pos);
+    if (mine) {
+      *reinterpret_cast<uint32_t*>(kc + tile + mx_k_chunk<NB>(kk, block) + ((s.dim >> 3) & 3) * 4) = kw;
+      if ((s.dim & 31) == 0) {
+        kc[tile + mx_k_scale<NB>(kk, block)] = (uint8_t)ks;
+        vc[tile + mx_v_scale<NB>(kk, block)] = (uint8_t)vs;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t nibble = ((vw >> (4 * e)) & 15u) << (4 * (at & 7));
+      if (at < 8) word[0][e] |= nibble;
+      else word[1][e] |= nibble;
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    if (g >= groups) break;
+    const int from = g == 0 ? in : 0, to = in + s.n - 8 * g < 8 ? in + s.n - 8 * g : 8;     // of the group, never all of it
+    const uint32_t mask = (to == 8 ? 0xffffffffu : (1u << (4 * to)) - 1u) & ~((1u << (4 * from)) - 1u);
+    const int64_t pos = s.begin + 8 * g;
+    uint8_t* tile = vc + mx_few_tile<NB>(a, s, pos);
+    if (mine)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        *reinterpret_cast<uint32_t*>(tile + mx_v_word<NB>((int)(pos % MX_TILE) & ~7, s.dim + e)) = (held[g][e] & ~mask) | word[g][e];
+  }
+}
+
+template <typename T, int NB, int VEC>
+__global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_read_few_kernel(const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc, T* __restrict__ k,
+                                                                       T* __restrict__ v, MxRows a) {
+  MxFew s;
+  bool outside;
+  if (!mx_few<NB>(a, s, outside) || s.h >= a.H_kv) return;
+  const int in = (int)(s.begin & 7), groups = in + s.n > 8 ? 2 : 1, block = s.dim >> 5;
+  uint32_t kw[MX_FEW], ks[MX_FEW], vs[MX_FEW], word[2][8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) word[1][e] = 0;
+#pragma unroll
+  for (int t = 0; t < MX_FEW; ++t) {
+    if (t >= s.n) break;
+    const int64_t pos = s.begin + t, tile = mx_few_tile<NB>(a, s, pos);
+    const int kk = (int)(pos % MX_TILE);
+    kw[t] = *reinterpret_cast<const uint32_t*>(kc + tile + mx_k_chunk<NB>(kk, block) + ((s.dim >> 3) & 3) * 4);
+    ks[t] = kc[tile + mx_k_scale<NB>(kk, block)];
+    vs[t] = vc[tile + mx_v_scale<NB>(kk, block)];
+  }
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    if (g >= groups) break;
+    const int64_t pos = s.begin + 8 * g;
+    const uint8_t* tile = vc + mx_few_tile<NB>(a, s, pos);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) word[g][e] = *reinterpret_cast<const uint32_t*>(tile + mx_v_word<NB>((int)(pos % MX_TILE) & ~7, s.dim + e));
+  }
+#pragma unroll
+  for (int t = 0; t < MX_FEW; ++t) {
+    if (t >= s.n) break;
+    const int at = in + t;
+    uint32_t vw = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t w0 = word[0][e], w1 = word[1][e];
+      vw |= (((at < 8 ? w0 : w1) >> (4 * (at & 7))) & 15u) << (4 * e);
+    }
+    const int64_t row = (s.row0 + t) * a.row_stride + (int64_t)s.h * a.d_h;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      float kv[4], vv[4];
+      mx_values(kw[t] >> (16 * u), ks[t], kv);
+      mx_values(vw >> (16 * u), vs[t], vv);
+      mx_store<T, 4, VEC>(k + row, s.dim + 4 * u, a.d_h, kv);
+      mx_store<T, 4, VEC>(v + row, s.dim + 4 * u, a.d_h, vv);
+    }
+  }
+}
+
 // ------------------------------------------------------------------ attention
 //
 // Score and value products run on the matrix cores in bf16, in which every stored value is exact; fp32 operands (the query, a
@@ -918,9 +1090,19 @@ void launch_rows(bool write, const void* k, const void* v, const void* kc, const
   else
     PHOTON_LAUNCH(KC_MXFP4_CACHE, st, (mxfp4_read_kernel<T, NB, VEC>), grid, block, 0, st, (const uint8_t*)kc, (const uint8_t*)vc, (T*)k, (T*)v, a);
 }
+template <typename T, int NB, int VEC>
+void launch_few(bool write, const void* k, const void* v, const void* kc, const void* vc, int32_t* status, const MxRows& a, int Bt, hipStream_t st) {
+  const int groups = (a.H_kv + 64 / (4 * NB) - 1) / (64 / (4 * NB)), waves = groups < MX_WAVES ? groups : MX_WAVES;   // of heads
+  const dim3 grid((groups + waves - 1) / waves, Bt), block(waves * 64);
+  if (write)
+    PHOTON_LAUNCH(KC_MXFP4_CACHE, st, (mxfp4_write_few_kernel<T, NB, VEC>), grid, block, 0, st, (const T*)k, (const T*)v, (uint8_t*)kc, (uint8_t*)vc, status, a);
+  else
+    PHOTON_LAUNCH(KC_MXFP4_CACHE, st, (mxfp4_read_few_kernel<T, NB, VEC>), grid, block, 0, st, (const uint8_t*)kc, (const uint8_t*)vc, (T*)k, (T*)v, a);
+}
 template <typename T, int NB>
 void launch_rows_vec(bool write, const void* k, const void* v, const void* kc, const void* vc, int32_t* status, const MxRows& a, int Bt, hipStream_t st) {
   const int vec = row_vec(k, v, a.row_stride, a.d_h, sizeof(T));
+  if (a.T <= MX_FEW) return vec > 1 ? launch_few<T, NB, 4>(write, k, v, kc, vc, status, a, Bt, st) : launch_few<T, NB, 1>(write, k, v, kc, vc, status, a, Bt, st);
   if constexpr (sizeof(T) == 2)
     if (vec == 8) return launch_rows<T, NB, 8>(write, k, v, kc, vc, status, a, Bt, st);
   if (vec == 4) return launch_rows<T, NB, 4>(write, k, v, kc, vc, status, a, Bt, st);

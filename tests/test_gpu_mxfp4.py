@@ -110,7 +110,8 @@ def test_all_bytes_read_back(ph, d_h):
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("Bt,T,H,d_h,start,n_new", [
     (1, 1, 1, 64, [0], None), (1, 1, 2, 52, [63], None), (2, 1, 3, 64, [64, 7], None), (3, 2, 2, 60, [63, 5, 62], [2, 0, 1]),
-    (2, 64, 2, 64, [0, 64], None), (2, 65, 2, 64, [63, 1], None), (2, 66, 1, 128, [63, 0], None), (2, 130, 2, 128, [3, 61], [130, 77]),
+    (4, 4, 5, 64, [61, 6, 0, 4], None), (3, 4, 3, 128, [5, 126, 60], [4, 3, 4]), (3, 3, 20, 20, [62, 63, 7], None), (2, 4, 17, 100, [7, 64], [1, 4]),
+    (5, 2, 9, 52, [63, 7, 8, 0, 70], [2, 2, 2, 0, 1]), (2, 4, 33, 33, [61, 5], None), (2, 5, 3, 64, [60, 4], None), (2, 64, 2, 64, [0, 64], None), (2, 65, 2, 64, [63, 1], None), (2, 66, 1, 128, [63, 0], None), (2, 130, 2, 128, [3, 61], [130, 77]),
     (2, 200, 2, 32, [0, 17], [200, 1]), (2, 77, 3, 20, [55, 100], None), (1, 100, 5, 100, [31], None), (2, 33, 2, 1, [8, 15], None),
     (2, 40, 2, 33, [9, 14], [40, 39]), (1, 300, 2, 56, None, None), (2, 9, 2, 65, [0, 60], [4, 9]), (2, 17, 1, 127, [2, 120], None),
 ])
@@ -148,11 +149,12 @@ def test_write_places_rows_and_leaves_the_rest(ph, dtype, Bt, T, H, d_h, start, 
         np.testing.assert_array_equal(got.float().cpu().numpy(), ref.astype(np.float32))
 
 
+@pytest.mark.parametrize("T", [37, 3])
 @pytest.mark.parametrize("dtype,H,d_h,offset", [(torch.float32, 2, 64, 0), (torch.bfloat16, 2, 64, 0), (torch.float32, 3, 52, 0), (torch.bfloat16, 1, 52, 0),
                                                 (torch.bfloat16, 2, 60, 3), (torch.float32, 2, 64, 1), (torch.bfloat16, 3, 33, 5)])
-def test_rows_may_be_parts_of_a_wider_matrix(ph, dtype, H, d_h, offset):
+def test_rows_may_be_parts_of_a_wider_matrix(ph, dtype, H, d_h, offset, T):
     """k and v as columns of a [Bt * T, q | k | v] projection, at any alignment; the columns beside them are not touched."""
-    Bt, T = 2, 37
+    Bt = 2
     rng = np.random.default_rng(5)
     D = H * d_h
     wide, base = rows(rng, (Bt, T, offset + 3 * D + 1), dtype)
@@ -168,12 +170,13 @@ def test_rows_may_be_parts_of_a_wider_matrix(ph, dtype, H, d_h, offset):
     np.testing.assert_array_equal(out.float().cpu().numpy(), ref.astype(np.float32))
 
 
-def test_rows_without_a_place(ph):
+@pytest.mark.parametrize("T", [10, 4])
+def test_rows_without_a_place(ph, T):
     """Entries outside the cache are dropped and reported, the others kept; reading leaves such rows alone."""
-    Bt, T, H, d_h, S = 4, 10, 2, 64, 128
+    Bt, H, d_h, S = 4, 2, 64, 128
     rng = np.random.default_rng(8)
     kx, k = rows(rng, (Bt, T, H, d_h), torch.float32)
-    first = [S - 4, -3, S, 2 ** 31 - 5]
+    first = [S - 2, -3, S, 2 ** 31 - 5]
     start = torch.tensor(first, dtype=torch.int32, device="cuda")
     kc, vc = ph.mxfp4_cache(Bt, H, d_h, S), ph.mxfp4_cache(Bt, H, d_h, S)
     status = torch.tensor([8], dtype=torch.int32, device="cuda")
@@ -200,16 +203,17 @@ def test_rows_without_a_place(ph):
     np.testing.assert_array_equal(out.cpu().numpy(), ref)
 
 
-def test_counts_outside_their_range(ph):
+@pytest.mark.parametrize("T", [5, 2])
+def test_counts_outside_their_range(ph, T):
     """n_new below 0 and above T count as 0 and T."""
     rng = np.random.default_rng(9)
-    kx, k = rows(rng, (2, 5, 1, 64), torch.float32)
+    kx, k = rows(rng, (2, T, 1, 64), torch.float32)
     kc, vc = ph.mxfp4_cache(2, 1, 64, 64), ph.mxfp4_cache(2, 1, 64, 64)
     ph.photon_mxfp4_cache_write(k, k, kc, vc, n_new=torch.tensor([-2, 99], dtype=torch.int32, device="cuda"))
     codes, _ = lay.unpack(kc.cpu().numpy(), 64, False)
     assert not codes[0].any()
-    np.testing.assert_array_equal(codes[1, 0, :5], stored(kx)[0][1, :, 0])
-    assert not codes[1, 0, 5:].any()
+    np.testing.assert_array_equal(codes[1, 0, :T], stored(kx)[0][1, :, 0])
+    assert not codes[1, 0, T:].any()
 
 
 # ---------------------------------------------------------------- attention
