@@ -334,12 +334,18 @@ def mxfp4_cache(Bt: int, H_kv: int, d_h: int, S_max: int, device="cuda") -> torc
     return torch.zeros((Bt, H_kv, tiles, photon_mxfp4_tile_bytes(d_h)), dtype=torch.uint8, device=device)
 
 
+_mx_tile_bytes: dict = {}        # d_h -> bytes of a tile, as asked of the library before
+
+
 def _mx_caches(k_cache: torch.Tensor, v_cache: torch.Tensor, Bt: int, d_h: int):
     """(H_kv, S_max) of a pair of caches that fit Bt sequences and head size d_h."""
     shape = k_cache.shape
+    tile_bytes = _mx_tile_bytes.get(d_h)
+    if tile_bytes is None:
+        tile_bytes = _mx_tile_bytes[d_h] = photon_mxfp4_tile_bytes(d_h)
     if k_cache.dtype is not torch.uint8 or v_cache.dtype is not torch.uint8 or len(shape) != 4:
         raise PhotonError(-1, "an MXFP4 cache is a uint8 tensor [Bt, H_kv, tiles, tile bytes]")
-    if v_cache.shape != shape or shape[0] != Bt or shape[3] != load_library().photon_mxfp4_tile_bytes(d_h):
+    if v_cache.shape != shape or shape[0] != Bt or shape[3] != tile_bytes:
         raise PhotonError(-1, f"caches {tuple(shape)} and {tuple(v_cache.shape)} do not hold {Bt} sequences of head size {d_h}")
     if not (k_cache.is_contiguous() and v_cache.is_contiguous()):
         raise PhotonError(-1, "caches must be contiguous")
@@ -389,7 +395,7 @@ def _mx_rows(k, v, k_cache, v_cache):
         raise PhotonError(-1, "k and v must be fp32 or bf16 tensors [Bt, T, H_kv, d_h] of one shape and dtype")
     Bt, T, H_kv, d_h = shape
     stride = _mx_row_stride(k)
-    if _mx_row_stride(v) != stride:
+    if v.stride() != k.stride() and _mx_row_stride(v) != stride:
         raise PhotonError(-1, f"k and v rows must have one stride: {stride} and {_mx_row_stride(v)}")
     heads, S_max = _mx_caches(k_cache, v_cache, Bt, d_h)
     if heads != H_kv:
