@@ -26,8 +26,9 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 // Neighbouring workgroups take neighbouring heads of the same positions (but see launch_rows), those of one die (blocks are dealt to the eight dies
 // in turn) heads that lie side by side, since heads of 52 to 60 elements share lines (4 x 8192 bf16 rows of 32 x 60 elements:
 // written in 190 us and read back in 148 without, in 120 and 109 with).
-// Measured for four prompts of 8192 rows of 32 x 64 elements (K and V): fp32 written at 5.4 TB/s (537 MB in, 71 MB out) and read
-// back at 4.8; bf16 at 4.9 and 5.6.  Without its stores the write takes 97 us (fp32): its bound is memory in both directions.
+// Measured for four prompts of 8192 rows of 32 x 64 elements (K and V): fp32 written in 113 us = 5.4 TB/s (537 MB in, 71 MB out) and
+// read back in 118 = 5.1; bf16 in 70 us = 4.9 and 67 = 5.1.  Without its stores the write takes 97 us (fp32): memory is the bound,
+// in both directions.
 
 constexpr int MX_WAVES = 4;      // waves of a workgroup, at most: 64 positions
 constexpr int MX_STEP = 16;      // positions of a wave
@@ -508,6 +509,10 @@ __global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_read_few_kernel(const uin
 //     elements of V as columns.  The weights change from a lane per position to operand order through LDS.
 //   The reference of the exponentials is the largest score when it was last raised, which happens when one exceeds it by more
 //     than MX_RAISE: fp32 and bf16 lose nothing by weights up to 2^MX_RAISE, and the usual tile needs no maximum.
+// Bound by HBM where streams are many (256 x 16 streams of 2048 positions: 573 MB in 84.5 us = 6.8 TB/s; 183 vector instructions a
+// tile of 64 x 64, 16 of them MFMAs, of about 380 that the bytes leave time for), by the start and the end of a wave where they are
+// few or short (4 x 32 streams of 8192 positions: 71 MB in 15.6 us with the merge), by the weights' instructions and two waves a
+// SIMD with eight queries of 128 elements (560 a tile: 143 MB in 38.3 us, one query 29.8).
 constexpr float MX_RAISE = 8.f;
 constexpr int MX_ATTN_WAVES = 8;                 // of a workgroup, at most
 constexpr int MX_P_PITCH = 72;                   // bf16 elements of a weight row in LDS: 64 positions, rows on different banks

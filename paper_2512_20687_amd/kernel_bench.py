@@ -1,12 +1,12 @@
 """Per-kernel throughput of the hot path's entry points at the shapes of the
 benchmark configurations, each against the roofline that bounds it.
 
-    python -m paper_2512_20687_amd.kernel_bench [--only copy,module,probe,a1,a2,a3,encoder,prefill,schedules,linear]
+    python -m paper_2512_20687_amd.kernel_bench [--only copy,module,probe,a1,a2,mx,a3,encoder,prefill,schedules,linear]
 
 Prints one JSON object per line: a streaming-read ceiling (a trivial read-only
 kernel over 2 GiB), the chunker GEMM (bf16 MFMA peak), the coarse decode
 attention at the configuration-3 shape and over a flat 131072-key cache (HBM
-peak), chunk-local attention in tile mode (HBM peak), the encoders' whole-sequence causal
+peak), the 4-bit cache written, read back and attended over (HBM peak), chunk-local attention in tile mode (HBM peak), the encoders' whole-sequence causal
 attention (bf16 MFMA peak on the causal half's flops) and the few-row linear
 maps of one block (HBM peak on weight bytes).  Inputs are seeded and synthetic,
 drawn on the GPU; buffers below 1 GiB are rotated so that no cache can serve a
@@ -129,6 +129,39 @@ def bench_a2():
     _emit("coarse_attn_kernel + coarse_merge_kernel", f"cfg3 with an 8-bit cache: Bt={Bt} H={H} S={S} d_h={d_h} splits={ns}", us,
           bytes_=2 * Bt * H * S * d_h)
     del k, v
+
+
+def bench_mx():
+    """The 4-bit cache: rows of a prompt in and out, and attention of one query per sequence (grouped heads as well)."""
+    def make(Bt, H, d_h, S):
+        k, v = ph.mxfp4_cache(Bt, H, d_h, S), ph.mxfp4_cache(Bt, H, d_h, S)
+        for b in range(Bt):
+            rows = [torch.randn((1, S, H, d_h), device="cuda").to(torch.bfloat16) for _ in range(2)]
+            ph.photon_mxfp4_cache_write(*rows, k[b : b + 1], v[b : b + 1])
+        return k, v
+
+    for Bt, T, H, d_h, dtype, what in ((4, 8192, 32, 64, torch.float32, "cfg3 prompt"), (4, 8192, 32, 64, torch.bfloat16, "cfg3 prompt"),
+                                       (256, 1, 16, 64, torch.float32, "cfg4 append"), (256, 1, 32, 52, torch.float32, "600M append")):
+        k, v = (torch.randn((Bt, T, H, d_h), device="cuda").to(dtype) for _ in range(2))
+        kc, vc = ph.mxfp4_cache(Bt, H, d_h, T), ph.mxfp4_cache(Bt, H, d_h, T)
+        nbytes = 2 * k.numel() * k.element_size() + kc.numel() * 2 if T > 1 else 2 * k.numel() * k.element_size()
+        shape = f"{what}: Bt={Bt} T={T} H={H} d_h={d_h} {str(dtype)[6:]}"
+        iters = 20 if T > 1 else 200
+        _emit("mxfp4_write_kernel", shape, _time_us(lambda i: ph.photon_mxfp4_cache_write(k, v, kc, vc), iters), bytes_=nbytes)
+        _emit("mxfp4_read_kernel", shape, _time_us(lambda i: ph.photon_mxfp4_cache_read(kc, vc, k, v), iters), bytes_=nbytes)
+        del k, v, kc, vc
+    for Bt, H, H_kv, d_h, S, dtype, what in ((4, 32, 32, 64, 8320, torch.float32, "cfg3"), (256, 16, 16, 64, 2112, torch.float32, "cfg4"),
+                                             (4, 32, 32, 64, 131072, torch.float32, "flat comparison"), (8, 32, 4, 128, 32768, torch.bfloat16, "grouped heads")):
+        caches = [make(Bt, H_kv, d_h, S) for _ in range(1 if S > 100000 else 3)]
+        q = torch.randn((Bt, 1, H, d_h), device="cuda").to(dtype)
+        out, lens = torch.empty_like(q), torch.full((Bt,), S, dtype=torch.int32, device="cuda")
+        n = ph.photon_mxfp4_decode_attn_auto_splits(Bt, 1, H, H_kv, S)
+        ws = torch.empty(max(16, ph.photon_mxfp4_decode_attn_workspace_bytes(Bt, 1, H, d_h, n)), dtype=torch.uint8, device="cuda")
+        us = _time_us(lambda i: ph.photon_mxfp4_decode_attn(q, *caches[i % len(caches)], lens, out, workspace=ws), 60)
+        _emit("mxfp4_attn_kernel" + (" + mxfp4_merge_kernel" if n > 1 else ""), f"{what}: Bt={Bt} H={H} H_kv={H_kv} S={S} d_h={d_h} splits={n}", us,
+              bytes_=2 * Bt * H_kv * S * (d_h // 2 + d_h // 32))
+        del caches, q, out, ws
+        torch.cuda.empty_cache()
 
 
 def bench_a3():
@@ -375,7 +408,7 @@ def bench_linear():
             del ws
 
 
-ALL = {"copy": bench_copy, "module": bench_module, "probe": bench_probe, "a1": bench_a1, "a2": bench_a2, "a3": bench_a3, "encoder": bench_encoder_attn, "prefill": bench_prefill, "schedules": bench_schedules, "linear": bench_linear}
+ALL = {"copy": bench_copy, "module": bench_module, "probe": bench_probe, "a1": bench_a1, "a2": bench_a2, "mx": bench_mx, "a3": bench_a3, "encoder": bench_encoder_attn, "prefill": bench_prefill, "schedules": bench_schedules, "linear": bench_linear}
 
 
 def main(argv=None):
