@@ -158,7 +158,7 @@ PHOTON_API int32_t photon_coarse_decode_attn_static(const void* q, const void* k
  *
  * Caches must be 16-byte aligned.  Rows (q, k, v, out) need the alignment of
  * their elements only; whole multiples of 16 bytes (pointer, stride, d_h) are
- * read fastest.  d_h in [1, 128], S_max < 2^31, dt fp32 or bf16.
+ * read fastest.  d_h in [1, 128], S_max <= 2^31 - 64, dt fp32 or bf16.
  * Bt == 0 or T == 0 is a no-op.
  * -------------------------------------------------------------------------- */
 PHOTON_API int32_t photon_mxfp4_tile_bytes(int32_t d_h);   /* 0 when d_h is outside [1, 128] */

@@ -17,6 +17,7 @@
 namespace photon {
 
 constexpr int MX_TILE = 64;      // positions of a tile
+constexpr int64_t MX_MOST = (1ll << 31) - MX_TILE;   // positions of a stream: the end of its last tile is an int32, too
 constexpr int MX_BLOCK = 32;     // elements under one scale
 constexpr int MX_LAST_SCALE = 252;   // the writer's largest scale byte: 6 * 2^(252 - 127) is the largest power step that stays finite in fp32; bytes above it read as NaN
 

@@ -23,9 +23,9 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 // consecutive elements a lane), and neighbours exchange 4 codes: then it holds 8 consecutive elements, too.  These go out as they are
 // for K.  V words hold 8 positions of one element: the 8 lanes of equal x exchange nibbles (an 8 x 8 transposition in three steps).
 //   d_p = 128: a pass takes half of the elements; d_p = 32: it takes 16 positions, blocks 0 and 1 being positions r and 8 + r.
-// Neighbouring workgroups take neighbouring heads of the same positions (but see launch_rows), those of one die (blocks are dealt to the eight dies
-// in turn) heads that lie side by side, since heads of 52 to 60 elements share lines (4 x 8192 bf16 rows of 32 x 60 elements:
-// written in 190 us and read back in 148 without, in 120 and 109 with).
+// Neighbouring workgroups take neighbouring heads of the same positions (but see launch_rows), those of one die (blocks are dealt to
+// the eight dies in turn) heads that lie side by side, since heads of 52 to 60 elements share lines (4 x 8192 bf16 rows of 32 x 60
+// elements: written in 190 us and read back in 148 without, in 120 and 109 with).
 // Measured for four prompts of 8192 rows of 32 x 64 elements (K and V): fp32 written in 113 us = 5.4 TB/s (537 MB in, 71 MB out) and
 // read back in 118 = 5.1; bf16 in 70 us = 4.9 and 67 = 5.1.  Without its stores the write takes 97 us (fp32): memory is the bound,
 // in both directions.
@@ -595,7 +595,7 @@ template <typename T> __device__ __forceinline__ void mx_put(T* out, int64_t at,
 // Positions that count for sequence b, and its queries.
 __device__ __forceinline__ void mx_sequence(const MxQueries& a, int b, int& n, int& m) {
   const int64_t all = (int64_t)a.seq_len[b] + a.add;
-  n = all < 0 ? 0 : all > a.S_max ? (int)a.S_max : (int)all;                // S_max < 2^31
+  n = all < 0 ? 0 : all > a.S_max ? (int)a.S_max : (int)all;                // S_max <= MX_MOST
   m = a.n_new ? a.n_new[b] : a.T;
   m = m < 0 ? 0 : m > a.T ? a.T : m;
 }
@@ -1043,7 +1043,7 @@ int32_t check_shape(const char* who, int32_t Bt, int32_t T, int32_t H_kv, int32_
   PHOTON_REQUIRE(Bt >= 0 && T >= 0 && H_kv > 0 && S_max > 0, PHOTON_ERR_INVALID_ARG, "%s: Bt=%d T=%d H_kv=%d S_max=%lld invalid", who, Bt, T,
                  H_kv, (long long)S_max);
   PHOTON_REQUIRE(d_h >= 1 && d_h <= 128, PHOTON_ERR_UNSUPPORTED, "%s: d_h=%d not in [1, 128]", who, d_h);
-  PHOTON_REQUIRE(S_max <= 0x7fffffff, PHOTON_ERR_UNSUPPORTED, "%s: S_max=%lld exceeds what an int32 position counts", who, (long long)S_max);
+  PHOTON_REQUIRE(S_max <= MX_MOST, PHOTON_ERR_UNSUPPORTED, "%s: S_max=%lld exceeds 2^31 - 64", who, (long long)S_max);
   PHOTON_REQUIRE(Bt <= 65535 && H_kv <= 65535, PHOTON_ERR_UNSUPPORTED, "%s: Bt=%d, H_kv=%d streams: at most 65535 each", who, Bt, H_kv);
   return PHOTON_OK;
 }

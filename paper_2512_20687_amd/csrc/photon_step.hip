@@ -364,7 +364,7 @@ static int32_t validate_config(const photon_config* c, int Bt, int64_t S_max) {
   PHOTON_REQUIRE(valid_dtype(c->dt), PHOTON_ERR_UNSUPPORTED, "unknown dtype %d", (int)c->dt);
   PHOTON_REQUIRE(c->kv_dt == c->dt || (c->dt == PHOTON_BF16 && (c->kv_dt == PHOTON_FP8_E4M3 || c->kv_dt == PHOTON_MXFP4)), PHOTON_ERR_UNSUPPORTED,
                  "kv_dt=%d must equal dt=%d, or be 8-bit or 4-bit with bf16 matrices", (int)c->kv_dt, (int)c->dt);
-  PHOTON_REQUIRE(c->kv_dt != PHOTON_MXFP4 || S_max <= 0x7fffffff, PHOTON_ERR_UNSUPPORTED, "S_max=%lld exceeds what a 4-bit cache counts", (long long)S_max);
+  PHOTON_REQUIRE(c->kv_dt != PHOTON_MXFP4 || S_max <= MX_MOST, PHOTON_ERR_UNSUPPORTED, "S_max=%lld exceeds what a 4-bit cache counts", (long long)S_max);
   PHOTON_REQUIRE(c->L >= 1 && c->L <= PHOTON_MAX_LEVELS, PHOTON_ERR_INVALID_ARG, "L=%d not in [1, %d]", c->L, (int)PHOTON_MAX_LEVELS);
   PHOTON_REQUIRE(Bt > 0 && S_max > 0, PHOTON_ERR_INVALID_ARG, "Bt=%d and S_max=%lld must be positive", Bt, (long long)S_max);
   PHOTON_REQUIRE(c->D > 0 && c->H > 0 && c->d_h > 0 && c->H * c->d_h == c->D, PHOTON_ERR_INVALID_ARG,

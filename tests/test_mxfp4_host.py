@@ -158,3 +158,37 @@ def test_binding_refuses(lib):
                  (q, c, c, i32, q)):
         with pytest.raises(ph.PhotonError):
             ph.photon_mxfp4_decode_attn(*args)
+
+
+def test_the_storage_type_is_accepted_where_it_is_one(lib):
+    """Only a configuration's kv_dt with bf16 matrices; elsewhere it is no element type."""
+    import paper_2512_20687_amd as ph
+    import seeded_inputs as si
+    from paper_2512_20687_amd import binding as b
+    assert b.PHOTON_MXFP4 == 3
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "photon.h")).read()
+    assert "PHOTON_MXFP4 = 3" in text
+    assert lib.photon_coarse_decode_attn(P, P, P, P, P, 1, 2, 64, 16, 0.1, 1, None, 0, 3, None) == -2
+    assert lib.photon_chunk_local_attn(P, P, P, P, 4, 4, 4, 0, 2, 64, 0.1, 3, None) == -2
+    cfg = si.PhotonConfig(L=2, C=(4, 4), R=(1, 1), D=256, H=4, d_h=64, n_layers=2, d_ff=640, vocab=1024, dtype="bf16", kv_dtype="mxfp4")
+    assert ph.photon_decode_step_workspace_bytes(cfg, 2, 100) > 0
+    c = b._c_config(cfg)
+    assert (c.dt, c.kv_dt) == (1, 3)
+    c.dt = 0
+    assert lib.photon_decode_step_workspace_bytes(ctypes.byref(c), 2, 100) == 0 and b"kv_dt=3" in lib.photon_last_error()
+    c.dt = 1
+    assert lib.photon_decode_step_workspace_bytes(ctypes.byref(c), 2, 1 << 31) == 0 and b"4-bit" in lib.photon_last_error()
+
+
+def test_positions_past_the_last_whole_tile_of_31_bits_are_refused(lib):
+    """Tiles end at a position that an int32 holds: S_max is at most 2^31 - 64, for the cache's calls and a step's."""
+    import paper_2512_20687_amd as ph
+    import seeded_inputs as si
+    from paper_2512_20687_amd import binding as b
+    most = (1 << 31) - 64
+    c = b._c_config(si.PhotonConfig(L=2, C=(4, 4), R=(1, 1), D=256, H=4, d_h=64, n_layers=2, d_ff=640, vocab=1024, dtype="bf16", kv_dtype="mxfp4"))
+    for S, ok in ((most, True), (most + 1, False), ((1 << 31) - 1, False)):
+        for fn, args in ((lib.photon_mxfp4_cache_write, WRITE), (lib.photon_mxfp4_cache_read, READ), (lib.photon_mxfp4_decode_attn, ATTN)):
+            assert fn(*{**args, "S": S, "T": 0}.values(), None) == (0 if ok else -2)
+            assert ok or b"S_max=%d" % S in lib.photon_last_error()
+        assert (lib.photon_decode_step_workspace_bytes(ctypes.byref(c), 2, S) > 0) == ok
