@@ -475,7 +475,8 @@ typedef struct photon_encoder_weights {
 /* Encoder streams of the levels below the top, kept only by hierarchical
  * generation (Appendix A, Definition 1): index l-1 for level l = 1 .. L-1. */
 typedef struct photon_hier_state {
-  void* k_cache[PHOTON_MAX_LEVELS];     /* [n_layers, Bt, H, S_cap[l-1], photon_kv_row_elems(d_h)] kv_dt: K/V of the level-l encoder */
+  void* k_cache[PHOTON_MAX_LEVELS];     /* [n_layers, Bt, H, S_cap[l-1], photon_kv_row_elems(d_h)] kv_dt: K/V of the level-l encoder
+                                           (kv_dt PHOTON_MXFP4: n_layers caches, S_cap <= 2^31 - 64) */
   void* v_cache[PHOTON_MAX_LEVELS];
   int32_t* seq_len[PHOTON_MAX_LEVELS];  /* [Bt] units cached per sequence at level l */
   int64_t S_cap[PHOTON_MAX_LEVELS];     /* capacity per sequence; a step appends prod(C_{l+1..L}) units */

@@ -148,6 +148,7 @@ __global__ __launch_bounds__(256) void rope_append_coarse_kernel(const float* __
 
 // The same for a cache in 4 bits, whose entries a pass over whole blocks writes: k rotated and v summed up go back to the first
 // part's rows.  seq_len == nullptr: positions 0 .. n_new - 1 of every sequence (a prompt); qrot == nullptr: no queries.
+// Units past the last slot are not written.
 __global__ __launch_bounds__(256) void rope_rows_kernel(float* __restrict__ qkv, int n_parts, int64_t part_stride, float* __restrict__ qrot,
                                                         const int32_t* __restrict__ seq_len, int64_t rows, int64_t n_new, int first, int H, int d_h,
                                                         float theta) {
@@ -1173,6 +1174,8 @@ static int32_t require_hier_state(const photon_config& c, const photon_hier_stat
     PHOTON_REQUIRE(hst->k_cache[l - 1] && aligned16(hst->k_cache[l - 1]) && hst->v_cache[l - 1] && aligned16(hst->v_cache[l - 1]) &&
                        hst->seq_len[l - 1] && hst->S_cap[l - 1] > 0,
                    PHOTON_ERR_INVALID_ARG, "stream of level %d: cache, seq_len or capacity missing or misaligned", l);
+    PHOTON_REQUIRE(c.kv_dt != PHOTON_MXFP4 || hst->S_cap[l - 1] <= MX_MOST, PHOTON_ERR_UNSUPPORTED,
+                   "stream of level %d: capacity %lld exceeds what a 4-bit cache counts", l, (long long)hst->S_cap[l - 1]);
   }
   return PHOTON_OK;
 }

@@ -192,3 +192,22 @@ def test_positions_past_the_last_whole_tile_of_31_bits_are_refused(lib):
             assert fn(*{**args, "S": S, "T": 0}.values(), None) == (0 if ok else -2)
             assert ok or b"S_max=%d" % S in lib.photon_last_error()
         assert (lib.photon_decode_step_workspace_bytes(ctypes.byref(c), 2, S) > 0) == ok
+
+
+def test_capacity_of_the_lower_levels_is_refused_too(lib):
+    """A lower level's stream is a cache of its own: past 2^31 - 64 positions a hierarchical step and a prefill refuse it."""
+    import paper_2512_20687_amd as ph
+    import seeded_inputs as si
+    from paper_2512_20687_amd import binding as b
+    cfg = si.PhotonConfig(L=2, C=(4, 4), R=(1, 1), D=128, H=2, d_h=64, n_layers=1, d_ff=128, vocab=64, dtype="bf16", kv_dtype="mxfp4")
+    model = ph.PhotonModel(cfg, si.make_weights(cfg, 3), device="cpu")
+    at = P.value                                   # never dereferenced: there is no workspace, should the capacity pass
+    state, hier = b._State(k_cache=at, v_cache=at, seq_len=at, x_top=at, carry=at, S_max=8), b._HierState()
+    hier.k_cache[0] = hier.v_cache[0] = hier.seq_len[0] = at
+    hier.S_cap[0] = (1 << 31) - 63
+    b._register_step(lib)
+    args = [ctypes.byref(x) for x in (model.c_cfg, model.c_weights, model.c_encoder_weights, state, hier)]
+    assert lib.photon_hiergen_step(*args, 2, None, P, None, None) == -2, lib.photon_last_error()
+    assert b"level 1" in lib.photon_last_error()
+    assert lib.photon_prefill(*args, 2, P, 32, None, 0, None) == -2, lib.photon_last_error()
+    assert b"level 1" in lib.photon_last_error()
