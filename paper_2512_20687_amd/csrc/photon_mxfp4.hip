@@ -1178,6 +1178,7 @@ extern "C" int32_t photon_mxfp4_cache_read(const void* k_cache, const void* v_ca
   if (Bt == 0 || T == 0) return PHOTON_OK;
   const MxRows a = mx_rows(start, n_rows, row_stride, T, H_kv, d_h, S_max);
   PHOTON_TRY(rows_args(__func__, k, v, k_cache, v_cache, row_stride, a, dt));
+  PHOTON_REQUIRE(k != v, PHOTON_ERR_INVALID_ARG, "%s: k and v overlap", __func__);
   return (dt == PHOTON_F32 ? launch_rows_t<float> : launch_rows_t<bf16_t>)(false, k, v, k_cache, v_cache, nullptr, a, Bt, (hipStream_t)stream);
 }
 

@@ -211,3 +211,9 @@ def test_capacity_of_the_lower_levels_is_refused_too(lib):
     assert b"level 1" in lib.photon_last_error()
     assert lib.photon_prefill(*args, 2, P, 32, None, 0, None) == -2, lib.photon_last_error()
     assert b"level 1" in lib.photon_last_error()
+
+
+def test_reading_back_needs_a_place_each(lib):
+    """K and V read into the same rows would race."""
+    assert lib.photon_mxfp4_cache_read(*READ.values(), None) == -1                                 # k and v are one pointer there
+    assert b"k and v overlap" in lib.photon_last_error()
