@@ -1015,9 +1015,9 @@ int32_t mx_launch_attn_q(const void* q, const void* kc, const void* vc, void* ou
   const int64_t queries = (int64_t)a.T * a.group, rows = mx_query_rows(queries, sizeof(T) == 4);
   a.groups = (int)((queries + rows - 1) / rows);
   if (rows == 1) return mx_launch_attn<T, NB, 1>(q, kc, vc, out, ws, a, Bt, st);
-  if (rows == 4) return mx_launch_attn<T, NB, 4>(q, kc, vc, out, ws, a, Bt, st);
-  if constexpr (sizeof(T) == 2) return mx_launch_attn<T, NB, 8>(q, kc, vc, out, ws, a, Bt, st);
-  return fail(PHOTON_ERR_UNSUPPORTED, "attention: %d query rows", (int)rows);
+  if constexpr (sizeof(T) == 2)
+    if (rows == 8) return mx_launch_attn<T, NB, 8>(q, kc, vc, out, ws, a, Bt, st);
+  return mx_launch_attn<T, NB, 4>(q, kc, vc, out, ws, a, Bt, st);
 }
 
 template <typename T>
