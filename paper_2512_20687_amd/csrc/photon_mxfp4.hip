@@ -509,11 +509,12 @@ __global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_read_few_kernel(const uin
 //     elements of V as columns.  The weights change from a lane per position to operand order through LDS.
 //   The reference of the exponentials is the largest score when it was last raised, which happens when one exceeds it by more
 //     than MX_RAISE: fp32 and bf16 lose nothing by weights up to 2^MX_RAISE, and the usual tile needs no maximum.
-// Bound by HBM where streams are many (256 x 16 streams of 2048 positions: 573 MB in 84.5 us = 6.8 TB/s; 183 vector instructions a
+// Bound by HBM where streams are many (256 x 16 streams of 2048 positions: 573 MB in 83.8 us = 6.8 TB/s; 184 vector instructions a
 // tile of 64 x 64, 16 of them MFMAs, of about 380 that the bytes leave time for), by the start and the end of a wave where they are
-// few or short (4 x 32 streams of 8192 positions: 71 MB in 15.6 us with the merge), by the weights' instructions and two waves a
-// SIMD with eight queries of 128 elements (560 a tile: 143 MB in 38.3 us, one query 29.8).
+// few or short (4 x 32 streams of 8192 positions: 71 MB in 16.1 us with the merge), by the weights' instructions and two waves a
+// SIMD with eight queries of 128 elements (566 a tile: 143 MB in 39.1 us, one query 29.8).
 constexpr float MX_RAISE = 8.f;
+constexpr float MX_LOWEST = -3.402823466e38f;    // of fp32: no finite score is below it
 constexpr int MX_ATTN_WAVES = 8;                 // of a workgroup, at most
 constexpr int MX_P_PITCH = 72;                   // bf16 elements of a weight row in LDS: 64 positions, rows on different banks
 
@@ -590,6 +591,13 @@ struct MxQueries {
 template <typename T> __device__ __forceinline__ void mx_put(T* out, int64_t at, float y, bool bf16) {
   if (sizeof(T) == 4 && bf16) reinterpret_cast<bf16_t*>(out)[at] = from_f32<bf16_t>(y);
   else out[at] = from_f32<T>(y);
+}
+
+// x * y, not merged with what follows: the reference was rounded, too, and what a merged product keeps beyond it is an exponent of its
+// own once scores pass 2^24.
+__device__ __forceinline__ float mx_rounded_product(float x, float y) {
+#pragma clang fp contract(off)
+  return x * y;
 }
 
 // Positions that count for sequence b, and its queries.
@@ -699,7 +707,7 @@ __global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T*
   const uint16_t* pr = pw + kg * 8;
   float top[NQ], sum[NQ];
 #pragma unroll
-  for (int i = 0; i < NQ; ++i) { top[i] = NEG_BIG; sum[i] = 0.f; }
+  for (int i = 0; i < NQ; ++i) { top[i] = MX_LOWEST; sum[i] = 0.f; }
   f32x4_t acc[QSETS][ACC];
 #pragma unroll
   for (int s = 0; s < QSETS; ++s)
@@ -756,13 +764,14 @@ __global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T*
     }
     // e: what the exponential is taken of
     float e[NQ];
-    auto reduce = [&](int i) { e[i] = SLOW ? s[i] - top[i] : fmaf(s[i], a.scale_log2e, -top[i]); };
-    float highest = NEG_BIG;
+    auto reduce = [&](int i) { e[i] = s[i] - top[i]; };
+    float highest = MX_LOWEST;
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
+      s[i] = mx_rounded_product(s[i], a.scale_log2e);
       if constexpr (SLOW) {
-        s[i] = nan_here ? __uint_as_float(0x7fc00000u) : s[i] * a.scale_log2e;
-        if (base + lane >= seen[i]) s[i] = NEG_BIG;
+        if (nan_here) s[i] = __uint_as_float(0x7fc00000u);
+        if (base + lane >= seen[i]) s[i] = MX_LOWEST;
       }
       reduce(i);
       highest = fmaxf(highest, e[i]);
@@ -771,7 +780,7 @@ __global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T*
       float shrink[NQ];
 #pragma unroll
       for (int i = 0; i < NQ; ++i) {
-        const float higher = fmaxf(top[i], mx_wave_max(SLOW ? s[i] : s[i] * a.scale_log2e));
+        const float higher = fmaxf(top[i], mx_wave_max(s[i]));
         shrink[i] = fast_exp2(top[i] - higher);
         top[i] = higher;
         sum[i] *= shrink[i];
@@ -903,11 +912,11 @@ __global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T*
     const int i = x / DP, d = x % DP;
     if (i >= queries) break;
     const float* at = reinterpret_cast<const float*>(mx_lds) + i * (DP + 2);
-    float w_top[MX_ATTN_WAVES], w_sum[MX_ATTN_WAVES], w_o[MX_ATTN_WAVES], mx = NEG_BIG;
+    float w_top[MX_ATTN_WAVES], w_sum[MX_ATTN_WAVES], w_o[MX_ATTN_WAVES], mx = MX_LOWEST;
 #pragma unroll
     for (int w = 0; w < MX_ATTN_WAVES; ++w) {
       const float* from = at + (w < waves ? w : 0) * (C::WAVE_BYTES / 4);
-      w_top[w] = w < waves ? from[0] : NEG_BIG;
+      w_top[w] = w < waves ? from[0] : MX_LOWEST;
       w_sum[w] = from[1];
       w_o[w] = from[2 + d];
       mx = fmaxf(mx, w_top[w]);
@@ -944,7 +953,7 @@ __global__ __launch_bounds__(NB * MX_BLOCK) void mxfp4_merge_kernel(const float*
   const int used = spans < (unsigned)a.n_splits ? (int)spans : a.n_splits;
   const int64_t to = ((int64_t)b * a.T + t) * a.H + h;
   const float* p = ws + to * a.n_splits * (DP + 2);
-  float mx = NEG_BIG, l = 0.f, o = 0.f;
+  float mx = MX_LOWEST, l = 0.f, o = 0.f;
   for (int s0 = 0; s0 < used; s0 += 8) {
     float s_top[8], s_sum[8], s_o[8], higher = mx;
 #pragma unroll
@@ -956,7 +965,7 @@ __global__ __launch_bounds__(NB * MX_BLOCK) void mxfp4_merge_kernel(const float*
     }
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      if (s0 + u >= used) s_top[u] = NEG_BIG;
+      if (s0 + u >= used) s_top[u] = MX_LOWEST;
       higher = fmaxf(higher, s_top[u]);
     }
     const float f0 = fast_exp2(mx - higher);

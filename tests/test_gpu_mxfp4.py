@@ -552,3 +552,34 @@ def test_offsets_past_32_bits(ph):
     p = np.exp(0.25 * K[1] @ K[1, -1])
     ref = p @ V[1] / (p.sum() + first)
     assert np.abs(out[1, 0, 0].cpu().numpy() - ref).max() <= 1e-5 * np.abs(ref).max()
+
+
+@pytest.mark.parametrize("dtype,T,n_splits,n", [(torch.float32, 1, 1, 1), (torch.float32, 1, 3, 700), (torch.float32, 4, 1, 70), (torch.float32, 4, 2, 900),
+                                                (torch.bfloat16, 1, 1, 64), (torch.bfloat16, 4, 1, 70), (torch.bfloat16, 8, 2, 700), (torch.bfloat16, 8, 1, 8)])
+def test_scores_near_the_lowest_number(ph, dtype, T, n_splits, n):
+    """Every score about -1e37: equal keys weigh the same, and a key that is half as far away takes all of the weight."""
+    rng = np.random.default_rng(n)
+    H, d_h = 2, 64
+    K = np.full((2, 1, H, n, d_h), -(2.0 ** 60))
+    K[1, 0, :, 0] = -(2.0 ** 59)
+    V = rng.standard_normal((2, 1, H, n, d_h))
+    caches, values = [], []
+    for x, is_v in ((K, False), (V, True)):
+        x = np.concatenate([x.reshape(2, H, n, d_h), np.zeros((2, H, -n % 64, d_h))], 2)
+        codes, scales = po.mxfp4_encode(x)
+        values.append(po.mxfp4_decode(codes, scales))
+        caches.append(torch.from_numpy(lay.pack(codes, scales, is_v)).cuda())
+    q = torch.full((2, T, H, d_h), 2.0 ** 60, dtype=dtype, device="cuda")
+    lens = torch.full((2,), n, dtype=torch.int32, device="cuda")
+    out = torch.empty_like(q)
+    ws = torch.empty(max(ph.photon_mxfp4_decode_attn_workspace_bytes(2, T, H, d_h, n_splits), 16), dtype=torch.uint8, device="cuda")
+    ph.photon_mxfp4_decode_attn(q, *caches, lens, out, n_splits=n_splits, workspace=ws, scale=0.125)
+    got = out.double().cpu().numpy()
+    half = 2.0 ** -8 if dtype == torch.bfloat16 else 0.0                # a bf16 result's rounding; 2^-15: of a weight, as above
+    weight = 2.0 ** -15 if dtype == torch.bfloat16 else 0.0
+    for t in range(T):
+        seen = n - T + t + 1
+        v = values[1][:, :, :seen]
+        ref = np.stack([v[0].mean(1), v[1][:, 0]])
+        bound = half * np.abs(ref) + weight * np.stack([np.abs(v[0]).mean(1), np.abs(ref[1])]) + 1e-5 * np.abs(ref).max()
+        assert np.all(np.abs(got[:, t] - ref) <= bound), t
