@@ -495,8 +495,8 @@ __global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_read_few_kernel(const uin
 
 // ------------------------------------------------------------------ attention
 //
-// Score and value products run on the matrix cores in bf16, in which every stored value is exact; fp32 operands (the query, a
-// weight) enter as three bf16 parts of 8 bits each, which are exact too, so with fp32 rows nothing is rounded below fp32.
+// Score and value products run on the matrix cores in bf16, in which every stored value is exact; fp32 operands (an fp32 query, a
+// weight) enter as three bf16 parts of 8 bits each, which are exact too, so nothing is rounded below fp32 but a bf16 result.
 //
 // A wave takes 64 positions at a time: NB loads of 16 bytes a lane of K, as many of V, and the scale bytes.
 //   Scores: S^T = Q K^T with the queries (or the parts of one query) as the four rows i of every row group g = 0..3 of a
@@ -506,13 +506,15 @@ __global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_read_few_kernel(const uin
 //     (or could), zeros elsewhere, and picks the load that holds them.  Lane l ends up with the scores of position l: softmax
 //     costs one exponential per lane and query, and no lane repeats another's.
 //   Values: O = (P X) V with the weights times V's scale as rows (a scale per 32 elements: one such operand per block) and the
-//     elements of V as columns.  The weights change from a lane per position to operand order through LDS.
+//     elements of V as columns.  The weights change from a lane per position to operand order through LDS.  The three parts of
+//     four queries (or of one) fit the sixteen rows; of eight, two do, and the third goes into the second's sums as an operand of
+//     its own (sums of its own would not fit the registers: 59 spilled).
 //   The reference of the exponentials is the largest score when it was last raised, which happens when one exceeds it by more
 //     than MX_RAISE: fp32 and bf16 lose nothing by weights up to 2^MX_RAISE, and the usual tile needs no maximum.
 // Bound by HBM where streams are many (256 x 16 streams of 2048 positions: 573 MB in 83.8 us = 6.8 TB/s; 184 vector instructions a
 // tile of 64 x 64, 16 of them MFMAs, of about 380 that the bytes leave time for), by the start and the end of a wave where they are
 // few or short (4 x 32 streams of 8192 positions: 71 MB in 16.1 us with the merge), by the weights' instructions and two waves a
-// SIMD with eight queries of 128 elements (566 a tile: 143 MB in 39.1 us, one query 29.8).
+// SIMD with eight queries of 128 elements (143 MB in 43.7 us, one query 29.8).
 constexpr float MX_RAISE = 8.f;
 constexpr float MX_LOWEST = -3.402823466e38f;    // of fp32: no finite score is below it
 constexpr int MX_ATTN_WAVES = 8;                 // of a workgroup, at most
@@ -522,9 +524,7 @@ template <typename T, int NB, int NQ> struct MxAttn {
   static constexpr int DP = NB * MX_BLOCK;
   static constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
   static constexpr int SETS = NQ == 1 ? 1 : PARTS * (NQ / 4);       // score operands: parts (one query: its parts are rows of one)
-  static constexpr int W_PARTS = PARTS == 3 ? 3 : 2;                // of a weight: with bf16 rows 16 bits of it, which no result shows
-  static constexpr int QSETS = NQ == 1 || PARTS == 1 ? 1 : NQ / 4;  // weight operands of a block
-  static constexpr int B_ROWS = NQ == 1 ? 4 : PARTS == 1 ? 2 * NQ : 12 * QSETS;   // weight rows of a block
+  static constexpr int B_ROWS = NQ == 1 ? 4 : 3 * NQ;               // weight rows of a block: NQ part + query (one query: its parts, and one unused)
   static constexpr int P_ROWS = B_ROWS * NB;
   static constexpr int ACC = 2 * NB;                                // column tiles of 16 elements
   // per wave: weight rows, and the staged queries or the wave's result
@@ -612,7 +612,7 @@ template <typename T, int NB, int NQ>
 __global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
                                                          T* __restrict__ out, float* __restrict__ ws, MxQueries a) {
   using C = MxAttn<T, NB, NQ>;
-  constexpr int DP = C::DP, SETS = C::SETS, ACC = C::ACC, QSETS = C::QSETS, PARTS = C::PARTS, TB = mx_tile_bytes(DP);
+  constexpr int DP = C::DP, SETS = C::SETS, ACC = C::ACC, PARTS = C::PARTS, TB = mx_tile_bytes(DP);
   extern __shared__ __align__(16) char mx_lds[];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, waves = blockDim.x >> 6;
   const int c = lane & 15, kg = lane >> 4;
@@ -708,11 +708,9 @@ __global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T*
   float top[NQ], sum[NQ];
 #pragma unroll
   for (int i = 0; i < NQ; ++i) { top[i] = MX_LOWEST; sum[i] = 0.f; }
-  f32x4_t acc[QSETS][ACC];
+  f32x4_t acc[ACC];
 #pragma unroll
-  for (int s = 0; s < QSETS; ++s)
-#pragma unroll
-    for (int t = 0; t < ACC; ++t) acc[s][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  for (int t = 0; t < ACC; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
   // Scale bytes above MX_LAST_SCALE, four at a time: the top bit of every byte that is one.
   auto bad_bytes = [](uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x03030303u) & w & 0x80808080u; };
@@ -787,20 +785,13 @@ __global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T*
         reduce(i);
       }
 #pragma unroll
-      for (int u = 0; u < QSETS; ++u)
+      for (int r = 0; r < 4; ++r) {
+        // row 4 kg + r of the value products is of query (4 kg + r) % NQ
+        float f = shrink[r % NQ];
+        if constexpr (NQ == 8) f = (kg & 1) == 0 ? f : shrink[4 + r];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          // row 4 kg + r of the value products: the query it belongs to
-          float f;
-          if constexpr (NQ == 1) f = shrink[0];
-          else if constexpr (PARTS == 3 || NQ == 4) f = shrink[(4 * u + r) % NQ];
-          else {
-            const float f0 = shrink[r], f1 = shrink[(4 + r) % NQ];
-            f = (kg & 1) == 0 ? f0 : f1;
-          }
-#pragma unroll
-          for (int t = 0; t < ACC; ++t) acc[u][t][r] *= f;
-        }
+        for (int t = 0; t < ACC; ++t) acc[t][r] *= f;
+      }
     }
     float p[NQ];
 #pragma unroll
@@ -816,7 +807,7 @@ __global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T*
       for (int t = 0; t < NB; ++t) {
         float y = p[0] * vf[t];
         if (SLOW && base + lane >= seen[0]) y = 0.f;
-        mx_put_parts<C::W_PARTS>(pw + 4 * t * MX_P_PITCH + lane, MX_P_PITCH, y);
+        mx_put_parts<3>(pw + 4 * t * MX_P_PITCH + lane, MX_P_PITCH, y);
       }
       mx_wave_order();
 #pragma unroll
@@ -825,7 +816,7 @@ __global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T*
 #pragma unroll
         for (int t = 0; t < ACC; ++t) {
           const int w = h * ACC + t;
-          acc[0][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(aop, mx_operand(x.v[w >> 2][w & 3], 1.f), acc[0][t], 0, 0, 0);
+          acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(aop, mx_operand(x.v[w >> 2][w & 3], 1.f), acc[t], 0, 0, 0);
         }
       }
     } else {
@@ -836,9 +827,7 @@ __global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T*
         for (int i = 0; i < NQ; ++i) {
           float y = p[i] * vf[blk];
           if (SLOW && base + lane >= seen[i]) y = 0.f;
-          // fp32: rows 12 set + 4 part + query of the block's, bf16: NQ part + query
-          if constexpr (PARTS == 3) mx_put_parts<3>(pw + (blk * C::B_ROWS + 12 * (i / 4) + i % 4) * MX_P_PITCH + lane, 4 * MX_P_PITCH, y);
-          else mx_put_parts<2>(pw + (blk * C::B_ROWS + i) * MX_P_PITCH + lane, NQ * MX_P_PITCH, y);
+          mx_put_parts<3>(pw + (blk * C::B_ROWS + i) * MX_P_PITCH + lane, NQ * MX_P_PITCH, y);
         }
       mx_wave_order();
 #pragma unroll
@@ -847,12 +836,15 @@ __global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T*
         for (int h = 0; h < 2; ++h) {
           const int w = h * ACC + 2 * blk;
           const bf16x8_t v0 = mx_operand(x.v[w >> 2][w & 3], 1.f), v1 = mx_operand(x.v[(w + 1) >> 2][(w + 1) & 3], 1.f);
-#pragma unroll
-          for (int u = 0; u < QSETS; ++u) {
-            const int row = blk * C::B_ROWS + (PARTS == 3 ? 12 * u + (c < 12 ? c : c - 12) : c % (2 * NQ));
-            const bf16x8_t aop = as_bf16x8(*reinterpret_cast<const uint4_t*>(pr + row * MX_P_PITCH + h * 32));
-            acc[u][2 * blk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(aop, v0, acc[u][2 * blk], 0, 0, 0);
-            acc[u][2 * blk + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(aop, v1, acc[u][2 * blk + 1], 0, 0, 0);
+          auto weights = [&](int row) { return *reinterpret_cast<const uint4_t*>(pr + (blk * C::B_ROWS + row) * MX_P_PITCH + h * 32); };
+          const bf16x8_t aop = as_bf16x8(weights(NQ == 8 || c < 12 ? c : c - 12));
+          acc[2 * blk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(aop, v0, acc[2 * blk], 0, 0, 0);
+          acc[2 * blk + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(aop, v1, acc[2 * blk + 1], 0, 0, 0);
+          if constexpr (NQ == 8) {                                           // two parts fill the rows: the third is added to the second's
+            uint4_t third = weights(8 + c);
+            if (c < 8) third = uint4_t{0, 0, 0, 0};
+            acc[2 * blk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(third), v0, acc[2 * blk], 0, 0, 0);
+            acc[2 * blk + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(third), v1, acc[2 * blk + 1], 0, 0, 0);
           }
         }
     }
@@ -884,28 +876,21 @@ __global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T*
     if (lane == 0) { ow[i * (DP + 2)] = top[i]; ow[i * (DP + 2) + 1] = l; }
   }
 #pragma unroll
-  for (int u = 0; u < QSETS; ++u)
+  for (int t = 0; t < ACC; ++t) {
+    if constexpr (NQ == 1) {
+      const float y = (acc[t][2] + acc[t][1]) + acc[t][0];
+      if (kg == t / 2) ow[2 + 16 * t + c] = y;
+    } else {
 #pragma unroll
-    for (int t = 0; t < ACC; ++t) {
-      if constexpr (NQ == 1) {
-        const float y = PARTS == 3 ? (acc[0][t][2] + acc[0][t][1]) + acc[0][t][0] : acc[0][t][1] + acc[0][t][0];
-        if (kg == t / 2) ow[2 + 16 * t + c] = y;
-      } else if constexpr (PARTS == 3) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float y = kg < 3 ? acc[u][t][r] : 0.f;
-          y += __shfl_xor(y, 32);
-          y += __shfl_xor(y, 16);
-          if (kg == 0) ow[(4 * u + r) * (DP + 2) + 2 + 16 * t + c] = y;
-        }
-      } else {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float y = acc[0][t][r] + __shfl_xor(acc[0][t][r], 4 * NQ);      // the parts: row groups NQ / 4 apart
-          if (4 * kg + r < NQ) ow[(4 * kg + r) * (DP + 2) + 2 + 16 * t + c] = y;
-        }
+      for (int r = 0; r < 4; ++r) {
+        // the parts: in row groups NQ / 4 apart
+        float y = NQ == 8 || kg < 3 ? acc[t][r] : 0.f;
+        y += __shfl_xor(y, 32);
+        if constexpr (NQ == 4) y += __shfl_xor(y, 16);
+        if (4 * kg + r < NQ) ow[(4 * kg + r) * (DP + 2) + 2 + 16 * t + c] = y;
       }
     }
+  }
   __syncthreads();
   // The waves' results, in order.
   for (int x = tid; x < NQ * DP; x += blockDim.x) {

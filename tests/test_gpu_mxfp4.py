@@ -2,9 +2,8 @@
 
 Tolerances.  Stored values are unique (power-of-two scales, ties to even), so writing and reading compare equal.  Attention with
 fp32 rows: 1e-5 of the largest value, the bar of every fp32 kernel here.  With bf16 rows the result is rounded once, half a step
-(2^-8 of the value); a softmax weight p enters the product with V as two bf16 parts, each off by at most half its step, 2^-8 of
-p and 2^-8 of what the first left: 2^-16 of p, which moves the result by at most 2^-16 * sum(p |v|) (2^-15 where the part that is
-left rounds up to the next binade); the fp32 sums add 1e-5 as above."""
+(2^-8 of the value); the fp32 sums add 1e-5 as above.  The 2^-15 * sum(p |v|) that the bounds here add is more than the weights
+need, which keep all of their 24 bits: tests/test_gpu_mxfp4_weights.py holds them to that."""
 import math
 
 import numpy as np
