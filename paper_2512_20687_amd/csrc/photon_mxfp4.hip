@@ -510,13 +510,17 @@ __global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_read_few_kernel(const uin
 //     four queries (or of one) fit the sixteen rows; of eight, two do, and the third goes into the second's sums as an operand of
 //     its own (sums of its own would not fit the registers: 59 spilled).
 //   The reference of the exponentials is the largest score when it was last raised, which happens when one exceeds it by more
-//     than MX_RAISE: fp32 and bf16 lose nothing by weights up to 2^MX_RAISE, and the usual tile needs no maximum.
+//     than MX_RAISE: the usual tile needs no maximum, and weights go up to 2^MX_RAISE.  Times V below 2^67 and summed over 2^31
+//     positions that stays below 2^106.  From the first tile on that holds larger V for it (scale byte MX_LARGE and up) a wave
+//     takes V in units of 2^MX_UNIT, in its slow body: below 2^103 for fp32's largest.  Results of waves and splits are means and
+//     put together as such (serving and grouped heads take as long as they did without; short streams of 2 - 3 tiles 16.7 us, 16.2).
 // Bound by HBM where streams are many (256 x 16 streams of 2048 positions: 573 MB in 83.8 us = 6.8 TB/s; 184 vector instructions a
 // tile of 64 x 64, 16 of them MFMAs, of about 380 that the bytes leave time for), by the start and the end of a wave where they are
 // few or short (4 x 32 streams of 8192 positions: 71 MB in 16.1 us with the merge), by the weights' instructions and two waves a
 // SIMD with eight queries of 128 elements (143 MB in 43.7 us, one query 29.8).
 constexpr float MX_RAISE = 8.f;
 constexpr float MX_LOWEST = -3.402823466e38f;    // of fp32: no finite score is below it
+constexpr uint32_t MX_LARGE = 192, MX_UNIT = 64; // scale byte from which V is large, and log2 of the unit it is taken in then
 constexpr int MX_ATTN_WAVES = 8;                 // of a workgroup, at most
 constexpr int MX_P_PITCH = 72;                   // bf16 elements of a weight row in LDS: 64 positions, rows on different banks
 
@@ -599,6 +603,9 @@ __device__ __forceinline__ float mx_rounded_product(float x, float y) {
 #pragma clang fp contract(off)
   return x * y;
 }
+
+// 1 / l; 0 where nothing was seen.
+__device__ __forceinline__ float mx_inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
 
 // Positions that count for sequence b, and its queries.
 __device__ __forceinline__ void mx_sequence(const MxQueries& a, int b, int& n, int& m) {
@@ -712,17 +719,27 @@ __global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T*
 #pragma unroll
   for (int t = 0; t < ACC; ++t) acc[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
-  // Scale bytes above MX_LAST_SCALE, four at a time: the top bit of every byte that is one.
+  // Scale bytes above MX_LAST_SCALE, or from MX_LARGE on, four at a time: the top bit of every byte that is one.
   auto bad_bytes = [](uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x03030303u) & w & 0x80808080u; };
-  static_assert(MX_LAST_SCALE == 252, "bad_bytes");
+  auto large_bytes = [](uint32_t w) { return w & (w << 1) & 0x80808080u; };
+  static_assert(MX_LAST_SCALE == 252 && MX_LARGE == 192, "bad_bytes, large_bytes");
+  bool large = false;                                                        // V counts in units of 2^MX_UNIT
 
   // SLOW: tiles that some query does not see whole, or that hold a NaN block: positions that nobody sees must not reach a sum, not
-  // even times zero, and a NaN must reach its own position only, not the others of its column.
+  // even times zero, and a NaN must reach its own position only, not the others of its column.  Large V, too, and all that follows it.
   auto consume = [&](auto slow_tag, int tile_at, const Tile& x) {
     constexpr bool SLOW = decltype(slow_tag)::value;
     const int base = tile_at * MX_TILE;
     float kf[NB], vf[NB];
     bool nan_here = false;
+    if constexpr (SLOW) {
+      if (!large && __builtin_amdgcn_ballot_w64(base + lane < hi && (large_bytes(x.vs) & ~bad_bytes(x.vs)) != 0) != 0) {
+        large = true;
+        const float unit = __uint_as_float((127u - MX_UNIT) << 23);
+#pragma unroll
+        for (int t = 0; t < ACC; ++t) acc[t] *= unit;
+      }
+    }
 #pragma unroll
     for (int t = 0; t < NB; ++t) {
       const uint32_t kx = (x.ks >> (8 * t)) & 255u, vx = (x.vs >> (8 * t)) & 255u;
@@ -736,6 +753,7 @@ __global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T*
 #pragma unroll
         for (int u = 0; u < 4; ++u)                                          // chunks u of this load that belong to position `lane`
           if ((t * 4 + u) / NB == kg) nan_here = nan_here || ((mask >> (u * 16 + c)) & 1u);
+        if (large) vf[t] = __uint_as_float((vx > MX_UNIT ? vx - MX_UNIT : 0u) << 23);
         if (vx > (uint32_t)MX_LAST_SCALE) vf[t] = __uint_as_float(0x7fc00000u);
       }
     }
@@ -851,7 +869,7 @@ __global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T*
   };
 
   auto either = [&](const Tile& x) {
-    if (tile * MX_TILE + MX_TILE > lo || __builtin_amdgcn_ballot_w64((bad_bytes(x.ks) | bad_bytes(x.vs)) != 0) != 0)
+    if (tile * MX_TILE + MX_TILE > lo || large || __builtin_amdgcn_ballot_w64((bad_bytes(x.ks) | large_bytes(x.vs)) != 0) != 0)
       consume(std::true_type{}, tile, x);
     else
       consume(std::false_type{}, tile, x);
@@ -867,19 +885,22 @@ __global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T*
     tile = next;
   }
 
-  // The wave's result: sums over lanes, parts put together, into LDS.
+  // The wave's result: sums over lanes, parts put together, into LDS.  Values are divided by the sum here, and results are put
+  // together as weighted means: no sum of values leaves the range that the values are in.
   mx_wave_order();
   float* ow = reinterpret_cast<float*>(own);
+  float mean[NQ];
 #pragma unroll
   for (int i = 0; i < NQ; ++i) {
     const float l = wave_sum(sum[i]);
     if (lane == 0) { ow[i * (DP + 2)] = top[i]; ow[i * (DP + 2) + 1] = l; }
+    mean[i] = mx_inverse(l) * (large ? __uint_as_float((127u + MX_UNIT) << 23) : 1.f);
   }
 #pragma unroll
   for (int t = 0; t < ACC; ++t) {
     if constexpr (NQ == 1) {
       const float y = (acc[t][2] + acc[t][1]) + acc[t][0];
-      if (kg == t / 2) ow[2 + 16 * t + c] = y;
+      if (kg == t / 2) ow[2 + 16 * t + c] = y * mean[0];
     } else {
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
@@ -887,7 +908,9 @@ __global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T*
         float y = NQ == 8 || kg < 3 ? acc[t][r] : 0.f;
         y += __shfl_xor(y, 32);
         if constexpr (NQ == 4) y += __shfl_xor(y, 16);
-        if (4 * kg + r < NQ) ow[(4 * kg + r) * (DP + 2) + 2 + 16 * t + c] = y;
+        float f = mean[r];
+        if constexpr (NQ == 8) f = kg == 0 ? f : mean[4 + r];
+        if (4 * kg + r < NQ) ow[(4 * kg + r) * (DP + 2) + 2 + 16 * t + c] = y * f;
       }
     }
   }
@@ -910,14 +933,19 @@ __global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T*
 #pragma unroll
     for (int w = 0; w < MX_ATTN_WAVES; ++w) {
       if (w >= waves) break;
-      const float f = fast_exp2(w_top[w] - mx);
-      l = fmaf(w_sum[w], f, l);
-      o = fmaf(w_o[w], f, o);
+      w_sum[w] *= fast_exp2(w_top[w] - mx);
+      l += w_sum[w];
+    }
+    const float r = mx_inverse(l);
+#pragma unroll
+    for (int w = 0; w < MX_ATTN_WAVES; ++w) {
+      if (w >= waves) break;
+      o = fmaf(w_o[w], w_sum[w] * r, o);
     }
     const int row = first_q + i, t = a.group == 1 ? row : row / a.group, h = hk * a.group + row - t * a.group;
     const int64_t to = ((int64_t)b * a.T + t) * a.H + h;
     if (a.n_splits == 1) {
-      if (d < a.d_h) mx_put(out, to * a.d_h + d, n - m + t + 1 > 0 ? o / l : 0.f, a.out_bf16);
+      if (d < a.d_h) mx_put(out, to * a.d_h + d, o, a.out_bf16);
     } else {
       float* p = ws + (to * a.n_splits + split) * (DP + 2);
       if (d == 0) { p[0] = mx; p[1] = l; }
@@ -938,7 +966,7 @@ __global__ __launch_bounds__(NB * MX_BLOCK) void mxfp4_merge_kernel(const float*
   const int used = spans < (unsigned)a.n_splits ? (int)spans : a.n_splits;
   const int64_t to = ((int64_t)b * a.T + t) * a.H + h;
   const float* p = ws + to * a.n_splits * (DP + 2);
-  float mx = MX_LOWEST, l = 0.f, o = 0.f;
+  float mx = MX_LOWEST, l = 0.f, o = 0.f;                    // o: weighted mean of the splits so far, l: their weight
   for (int s0 = 0; s0 < used; s0 += 8) {
     float s_top[8], s_sum[8], s_o[8], higher = mx;
 #pragma unroll
@@ -953,19 +981,24 @@ __global__ __launch_bounds__(NB * MX_BLOCK) void mxfp4_merge_kernel(const float*
       if (s0 + u >= used) s_top[u] = MX_LOWEST;
       higher = fmaxf(higher, s_top[u]);
     }
-    const float f0 = fast_exp2(mx - higher);
+    const float before = l * fast_exp2(mx - higher);
     mx = higher;
-    l *= f0;
-    o *= f0;
+    l = before;
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       if (s0 + u >= used) break;
-      const float f = fast_exp2(s_top[u] - mx);
-      l = fmaf(s_sum[u], f, l);
-      o = fmaf(s_o[u], f, o);
+      s_sum[u] *= fast_exp2(s_top[u] - mx);
+      l += s_sum[u];
+    }
+    const float r = mx_inverse(l);
+    o *= before * r;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (s0 + u >= used) break;
+      o = fmaf(s_o[u], s_sum[u] * r, o);
     }
   }
-  if (d < a.d_h) mx_put(out, to * a.d_h + d, n - m + t + 1 > 0 ? o / l : 0.f, a.out_bf16);
+  if (d < a.d_h) mx_put(out, to * a.d_h + d, o, a.out_bf16);
 }
 
 // Queries that share what a workgroup reads.  fp32: at most 4 (the operands of 8 are 96 registers a lane: 120 spilled).
