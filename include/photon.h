@@ -171,14 +171,15 @@ PHOTON_API size_t photon_mxfp4_cache_bytes(int32_t Bt, int32_t H_kv, int32_t d_h
  *   n_new      [Bt] int32, device, or NULL: T; only the first n_new[b] rows of sequence b are used (a padded batch)
  *   status     NULL, or a device word that PHOTON_STATUS_CACHE_FULL is ORed into when a row has no place: entries outside
  *              [0, S_max) are not written
- * The entries around the written ones keep their bits. */
+ * The entries around the written ones keep their bits.  The caches must not share memory. */
 PHOTON_API int32_t photon_mxfp4_cache_write(const void* k, const void* v, int64_t row_stride, void* k_cache, void* v_cache,
                                             const int32_t* start, const int32_t* n_new, int32_t* status, int32_t Bt, int32_t T,
                                             int32_t H_kv, int32_t d_h, int64_t S_max, photon_dtype dt, void* stream);
 
 /* Reads entries back: row t of sequence b receives the values at position start[b] + t, exact in either dt (but for bf16
  * values whose scale is so small that they are below bf16's subnormals).  Arguments as for the write; rows past n_rows[b],
- * and rows whose position is outside [0, S_max), are left as they were. */
+ * and rows whose position is outside [0, S_max), are left as they were.  No row of k may share memory with one of v (rows that
+ * alternate, and columns of one matrix, do not). */
 PHOTON_API int32_t photon_mxfp4_cache_read(const void* k_cache, const void* v_cache, const int32_t* start, const int32_t* n_rows,
                                            void* k, void* v, int64_t row_stride, int32_t Bt, int32_t T, int32_t H_kv, int32_t d_h,
                                            int64_t S_max, photon_dtype dt, void* stream);

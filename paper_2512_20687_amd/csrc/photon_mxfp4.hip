@@ -1088,6 +1088,13 @@ int64_t mx_row_steps(int T) { return ((int64_t)T + MX_STEP - 2) / MX_STEP + 1; }
 int mx_row_waves(int T) { const int64_t n = mx_row_steps(T); return n < MX_WAVES ? (int)n : MX_WAVES; }
 int64_t mx_row_groups(int T) { return (mx_row_steps(T) + mx_row_waves(T) - 1) / mx_row_waves(T); }
 
+// Whether any of `rows` rows of `width` elements from a on, `stride` apart, shares an element with one of as many from b on.
+bool rows_overlap(const void* a, const void* b, size_t esz, int64_t stride, int64_t width, int64_t rows) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  const int64_t apart = (int64_t)((x < y ? y - x : x - y) / esz), m = apart / stride, past = apart - m * stride;   // row m of the one begins `past` before the other
+  return (m < rows && past < width) || (m + 1 < rows && stride - past < width);
+}
+
 int32_t rows_args(const char* who, const void* k, const void* v, const void* kc, const void* vc, int64_t row_stride, const MxRows& a, photon_dtype dt) {
   const size_t esz = dtype_size(dt);
   PHOTON_REQUIRE(k && v && aligned(k, esz) && aligned(v, esz), PHOTON_ERR_INVALID_ARG, "%s: k and v must be non-null device pointers to whole elements", who);
@@ -1194,6 +1201,8 @@ extern "C" int32_t photon_mxfp4_cache_write(const void* k, const void* v, int64_
   if (Bt == 0 || T == 0) return PHOTON_OK;
   const MxRows a = mx_rows(start, n_new, row_stride, T, H_kv, d_h, S_max);
   PHOTON_TRY(rows_args(__func__, k, v, k_cache, v_cache, row_stride, a, dt));
+  PHOTON_REQUIRE(!rows_overlap(k_cache, v_cache, 1, INT64_MAX, (int64_t)mx_cache_bytes(Bt, H_kv, d_h, S_max), 1), PHOTON_ERR_INVALID_ARG,
+                 "%s: K and V need a cache each: these overlap", __func__);
   return (dt == PHOTON_F32 ? launch_rows_t<float> : launch_rows_t<bf16_t>)(true, k, v, k_cache, v_cache, status, a, Bt, (hipStream_t)stream);
 }
 
@@ -1205,7 +1214,8 @@ extern "C" int32_t photon_mxfp4_cache_read(const void* k_cache, const void* v_ca
   if (Bt == 0 || T == 0) return PHOTON_OK;
   const MxRows a = mx_rows(start, n_rows, row_stride, T, H_kv, d_h, S_max);
   PHOTON_TRY(rows_args(__func__, k, v, k_cache, v_cache, row_stride, a, dt));
-  PHOTON_REQUIRE(k != v, PHOTON_ERR_INVALID_ARG, "%s: k and v overlap", __func__);
+  PHOTON_REQUIRE(!rows_overlap(k, v, dtype_size(dt), row_stride, (int64_t)H_kv * d_h, (int64_t)Bt * T), PHOTON_ERR_INVALID_ARG,
+                 "%s: k and v overlap", __func__);
   return (dt == PHOTON_F32 ? launch_rows_t<float> : launch_rows_t<bf16_t>)(false, k, v, k_cache, v_cache, nullptr, a, Bt, (hipStream_t)stream);
 }
 
