@@ -805,8 +805,7 @@ __global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T*
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         // row 4 kg + r of the value products is of query (4 kg + r) % NQ
-        float f = shrink[r % NQ];
-        if constexpr (NQ == 8) f = (kg & 1) == 0 ? f : shrink[4 + r];
+        const float f0 = shrink[r % NQ], f1 = shrink[(4 + r) % NQ], f = NQ == 8 && (kg & 1) ? f1 : f0;
 #pragma unroll
         for (int t = 0; t < ACC; ++t) acc[t][r] *= f;
       }
@@ -908,8 +907,7 @@ __global__ __launch_bounds__(MX_ATTN_WAVES * 64) void mxfp4_attn_kernel(const T*
         float y = NQ == 8 || kg < 3 ? acc[t][r] : 0.f;
         y += __shfl_xor(y, 32);
         if constexpr (NQ == 4) y += __shfl_xor(y, 16);
-        float f = mean[r];
-        if constexpr (NQ == 8) f = kg == 0 ? f : mean[4 + r];
+        const float f0 = mean[r], f1 = mean[(4 + r) % NQ], f = NQ == 8 && kg ? f1 : f0;
         if (4 * kg + r < NQ) ow[(4 * kg + r) * (DP + 2) + 2 + 16 * t + c] = y * f;
       }
     }

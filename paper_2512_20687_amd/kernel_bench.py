@@ -1,14 +1,15 @@
 """Per-kernel throughput of the hot path's entry points at the shapes of the
 benchmark configurations, each against the roofline that bounds it.
 
-    python -m paper_2512_20687_amd.kernel_bench [--only copy,module,probe,a1,a2,mx,a3,encoder,prefill,schedules,linear]
+    python -m paper_2512_20687_amd.kernel_bench [--only copy,module,probe,a1,a2,mx,a3,encoder,prefill,schedules,storage,linear]
 
 Prints one JSON object per line: a streaming-read ceiling (a trivial read-only
 kernel over 2 GiB), the chunker GEMM (bf16 MFMA peak), the coarse decode
 attention at the configuration-3 shape and over a flat 131072-key cache (HBM
 peak), the 4-bit cache written, read back and attended over (HBM peak), chunk-local attention in tile mode (HBM peak), the encoders' whole-sequence causal
-attention (bf16 MFMA peak on the causal half's flops) and the few-row linear
-maps of one block (HBM peak on weight bytes).  Inputs are seeded and synthetic,
+attention (bf16 MFMA peak on the causal half's flops), whole steps and prefills with
+the coarse cache in its three types, and the few-row linear maps of one block (HBM
+peak on weight bytes).  Inputs are seeded and synthetic,
 drawn on the GPU; buffers below 1 GiB are rotated so that no cache can serve a
 launch from the previous one.  Timing: HIP events on the launch stream around
 `iters` back-to-back launches after a warm-up, so a launch's time includes the
@@ -133,6 +134,9 @@ def bench_a2():
 
 def bench_mx():
     """The 4-bit cache: rows of a prompt in and out, and attention of one query per sequence (grouped heads as well)."""
+    def sets(nbytes):
+        return max(1, -(-(1 << 30) // nbytes))                # so many take turns
+
     def make(Bt, H, d_h, S):
         k, v = ph.mxfp4_cache(Bt, H, d_h, S), ph.mxfp4_cache(Bt, H, d_h, S)
         for b in range(Bt):
@@ -141,27 +145,84 @@ def bench_mx():
         return k, v
 
     for Bt, T, H, d_h, dtype, what in ((4, 8192, 32, 64, torch.float32, "cfg3 prompt"), (4, 8192, 32, 64, torch.bfloat16, "cfg3 prompt"),
-                                       (256, 1, 16, 64, torch.float32, "cfg4 append"), (256, 1, 32, 52, torch.float32, "600M append")):
-        k, v = (torch.randn((Bt, T, H, d_h), device="cuda").to(dtype) for _ in range(2))
-        kc, vc = ph.mxfp4_cache(Bt, H, d_h, T), ph.mxfp4_cache(Bt, H, d_h, T)
-        nbytes = 2 * k.numel() * k.element_size() + kc.numel() * 2 if T > 1 else 2 * k.numel() * k.element_size()
+                                       (256, 1, 16, 64, torch.float32, "cfg4 append"), (256, 1, 32, 52, torch.float32, "600M append"),
+                                       (4, 4, 32, 64, torch.float32, "cfg3, four units")):
+        size = ph.photon_mxfp4_cache_bytes(Bt, H, d_h, T)
+        rows = Bt * T * H * d_h * (4 if dtype == torch.float32 else 2)
+        n = sets(2 * (size + rows))
+        data = [[torch.randn((Bt, T, H, d_h), device="cuda").to(dtype) for _ in range(2)] + [ph.mxfp4_cache(Bt, H, d_h, T) for _ in range(2)] for _ in range(n)]
+        nbytes = 2 * rows + (2 * size if T > 64 else 0)
         shape = f"{what}: Bt={Bt} T={T} H={H} d_h={d_h} {str(dtype)[6:]}"
-        iters = 20 if T > 1 else 200
-        _emit("mxfp4_write_kernel", shape, _time_us(lambda i: ph.photon_mxfp4_cache_write(k, v, kc, vc), iters), bytes_=nbytes)
-        _emit("mxfp4_read_kernel", shape, _time_us(lambda i: ph.photon_mxfp4_cache_read(kc, vc, k, v), iters), bytes_=nbytes)
-        del k, v, kc, vc
+        iters = max(20, 2 * n)
+        _emit("mxfp4 write", shape, _time_us(lambda i: ph.photon_mxfp4_cache_write(*data[i % n]), iters, warm=n), bytes_=nbytes)
+        _emit("mxfp4 read", shape, _time_us(lambda i: ph.photon_mxfp4_cache_read(*data[i % n][2:], *data[i % n][:2]), iters, warm=n), bytes_=nbytes)
+        del data
     for Bt, H, H_kv, d_h, S, dtype, what in ((4, 32, 32, 64, 8320, torch.float32, "cfg3"), (256, 16, 16, 64, 2112, torch.float32, "cfg4"),
-                                             (4, 32, 32, 64, 131072, torch.float32, "flat comparison"), (8, 32, 4, 128, 32768, torch.bfloat16, "grouped heads")):
-        caches = [make(Bt, H_kv, d_h, S) for _ in range(1 if S > 100000 else 3)]
+                                             (4, 32, 32, 64, 131072, torch.float32, "flat comparison"), (8, 32, 4, 128, 32768, torch.bfloat16, "grouped heads"),
+                                             (8, 32, 4, 128, 32768, torch.float32, "grouped heads")):
+        nbytes = 2 * Bt * H_kv * S * (d_h // 2 + d_h // 32)
+        caches = [make(Bt, H_kv, d_h, S) for _ in range(sets(nbytes))]
         q = torch.randn((Bt, 1, H, d_h), device="cuda").to(dtype)
         out, lens = torch.empty_like(q), torch.full((Bt,), S, dtype=torch.int32, device="cuda")
-        n = ph.photon_mxfp4_decode_attn_auto_splits(Bt, 1, H, H_kv, S)
-        ws = torch.empty(max(16, ph.photon_mxfp4_decode_attn_workspace_bytes(Bt, 1, H, d_h, n)), dtype=torch.uint8, device="cuda")
-        us = _time_us(lambda i: ph.photon_mxfp4_decode_attn(q, *caches[i % len(caches)], lens, out, workspace=ws), 60)
-        _emit("mxfp4_attn_kernel" + (" + mxfp4_merge_kernel" if n > 1 else ""), f"{what}: Bt={Bt} H={H} H_kv={H_kv} S={S} d_h={d_h} splits={n}", us,
-              bytes_=2 * Bt * H_kv * S * (d_h // 2 + d_h // 32))
+        auto = ph.photon_mxfp4_decode_attn_auto_splits(Bt, 1, H, H_kv, S)
+        for n in (auto,) if H == H_kv else (auto, max(1, auto // 2)):
+            ws = torch.empty(max(16, ph.photon_mxfp4_decode_attn_workspace_bytes(Bt, 1, H, d_h, n)), dtype=torch.uint8, device="cuda")
+            us = _time_us(lambda i: ph.photon_mxfp4_decode_attn(q, *caches[i % len(caches)], lens, out, n_splits=n, workspace=ws), 4 * max(15, len(caches)),
+                          warm=len(caches))
+            _emit("mxfp4_attn_kernel" + (" + mxfp4_merge_kernel" if n > 1 else ""),
+                  f"{what}: Bt={Bt} H={H} H_kv={H_kv} S={S} d_h={d_h} {str(dtype)[6:]} splits={n}", us, bytes_=nbytes)
         del caches, q, out, ws
         torch.cuda.empty_cache()
+
+
+def bench_storage():
+    """Decode steps (graphs of eight pipelined ones) and prefills with the coarse cache in bf16, 8 bits and 4 bits."""
+    import os
+    sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    import seeded_inputs as si
+    from dataclasses import replace
+    per_graph, iters = 8, 6
+    for name in ("cfg4_bf16_serving", "cfg3_bf16_128k", "paper_600m"):
+        wl = si.WORKLOADS[name]
+        S_max = (wl.S0 + per_graph * (iters + 3) + 127) // 128 * 128
+        for kv in ("", "fp8", "mxfp4"):
+            cfg = replace(wl.cfg, kv_dtype=kv)
+            model = ph.PhotonModel(cfg, si.make_weights(cfg, 0, device="cuda", encoders=False))
+            state = ph.PhotonState(model, wl.Bt, S_max, pipeline=True)
+            state.seq_len.fill_(wl.S0)
+            for x in (state.x_top, state.carry):
+                x.normal_()
+            for x in (state.k, state.v):                      # finite whatever the type
+                x.normal_() if kv == "" else x.random_(0, 110)
+            toks = [torch.empty((wl.Bt, cfg.meta_context), dtype=torch.int32, device="cuda") for _ in range(per_graph)]
+
+            def steps():
+                for t in toks:
+                    ph.photon_decode_step(model, state, t)
+                ph.photon_decode_join(state)
+            ph.photon_decode_step(model, state, toks[0])
+            ph.photon_decode_join(state)
+            torch.cuda.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                steps()
+            us = _time_us(lambda i: g.replay(), iters) / per_graph
+            print(json.dumps({"kernel": "photon_decode_step", "shape": f"{name}, coarse cache in {kv or 'bf16'}", "ms_per_step": round(us / 1e3, 3),
+                              "global_kv_cache_bytes": 2 * state.k.numel() * state.k.element_size()}), flush=True)
+            del model, state, g, toks
+            torch.cuda.empty_cache()
+    for name, Bt in (("cfg2_bf16_8k", 16), ("cfg3_bf16_128k", 1)):
+        wl = si.WORKLOADS[name]
+        for kv in ("", "mxfp4"):
+            cfg = replace(wl.cfg, kv_dtype=kv)
+            model = ph.PhotonModel(cfg, si.make_weights(cfg, 0, device="cuda"))
+            state = ph.PhotonState(model, Bt, wl.S0 + 64)
+            tok = torch.randint(0, cfg.vocab, (Bt, wl.T), dtype=torch.int32, device="cuda")
+            ws = torch.empty(ph.photon_prefill_workspace_bytes(cfg, Bt, wl.T), dtype=torch.uint8, device="cuda")
+            us = _time_us(lambda i: ph.photon_prefill(model, state, tok, workspace=ws), 3, warm=1)
+            print(json.dumps({"kernel": "photon_prefill", "shape": f"{name}, {Bt} sequences, coarse cache in {kv or 'bf16'}", "ms": round(us / 1e3, 3)}), flush=True)
+            del model, state, tok, ws
+            torch.cuda.empty_cache()
 
 
 def bench_a3():
@@ -408,7 +469,7 @@ def bench_linear():
             del ws
 
 
-ALL = {"copy": bench_copy, "module": bench_module, "probe": bench_probe, "a1": bench_a1, "a2": bench_a2, "mx": bench_mx, "a3": bench_a3, "encoder": bench_encoder_attn, "prefill": bench_prefill, "schedules": bench_schedules, "linear": bench_linear}
+ALL = {"copy": bench_copy, "module": bench_module, "probe": bench_probe, "a1": bench_a1, "a2": bench_a2, "mx": bench_mx, "a3": bench_a3, "encoder": bench_encoder_attn, "prefill": bench_prefill, "schedules": bench_schedules, "storage": bench_storage, "linear": bench_linear}
 
 
 def main(argv=None):
