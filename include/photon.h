@@ -192,12 +192,13 @@ PHOTON_API int32_t photon_mxfp4_cache_read(const void* k_cache, const void* v_ca
  *   seq_len  [Bt] int32, device; values outside [0, S_max] count as the nearer end
  *   n_new    [Bt] int32, device, or NULL: T; queries past n_new[b] are skipped, their rows of out left as they were
  *   out      [Bt, T, H, d_h] dt
- * Scores, softmax, weights and sums are in fp32 for either dt; a bf16 result is rounded once.  The result is finite wherever
- * scores and V are, V as large as the format holds included.  K and V blocks whose scale byte is 0 (values below 2^-124) count as
- * zeros, and V blocks below 2^-60 may where entries in use are 2^67 and more.  The positions are split over n_splits workgroups
- * per stream (0 = choose from the shape); partial results are merged in a fixed order, so the result is run-to-run deterministic
- * for a given n_splits.  n_splits > 1 needs a workspace of photon_mxfp4_decode_attn_workspace_bytes() bytes (no initialisation;
- * calls that share one must be stream-ordered). */
+ * Scores, softmax, weights and sums are in fp32 for either dt; a bf16 result is rounded once.  The result is finite wherever V
+ * is and, in fp32, q . K and 2 * scale * q . K are.  K and V blocks whose scale byte is 0 (values below 2^-124) count as zeros,
+ * and V blocks below 2^-60 may where entries in use are 2^67 and more.
+ * The positions are split over n_splits workgroups per stream (0 = choose from shape and dt, at most what _auto_splits says);
+ * partial results are merged in a fixed order, so the result is run-to-run deterministic for a given n_splits.  n_splits > 1
+ * needs a workspace of photon_mxfp4_decode_attn_workspace_bytes() bytes (no initialisation; calls that share one must be
+ * stream-ordered). */
 PHOTON_API size_t photon_mxfp4_decode_attn_workspace_bytes(int32_t Bt, int32_t T, int32_t H, int32_t d_h, int32_t n_splits);
 PHOTON_API int32_t photon_mxfp4_decode_attn_auto_splits(int32_t Bt, int32_t T, int32_t H, int32_t H_kv, int64_t S_max);
 PHOTON_API int32_t photon_mxfp4_decode_attn(const void* q, int64_t q_stride, const void* k_cache, const void* v_cache,

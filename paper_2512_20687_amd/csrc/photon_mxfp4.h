@@ -45,6 +45,6 @@ int32_t launch_mx_write(const float* k, const float* v, int64_t row_stride, void
 // photon_mxfp4_decode_attn with seq_len[b] + add entries; out_bf16: the fp32 results rounded to bf16.
 int32_t launch_mx_attn(const float* q, const void* kc, const void* vc, const int32_t* seq_len, int add, void* out, bool out_bf16, int Bt, int T, int H,
                        int d_h, int64_t S_max, float scale, int n_splits, void* ws, hipStream_t st);
-int mx_auto_splits(int Bt, int T, int H, int H_kv, int64_t S_max);
+int mx_auto_splits(int Bt, int T, int H, int H_kv, int64_t S_max, bool f32);
 
 }  // namespace photon

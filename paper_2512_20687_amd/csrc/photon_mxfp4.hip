@@ -1003,9 +1003,11 @@ __global__ __launch_bounds__(NB * MX_BLOCK) void mxfp4_merge_kernel(const float*
 int mx_query_rows(int64_t queries, bool f32) { return queries <= 1 ? 1 : queries <= 4 || f32 ? 4 : 8; }
 
 // One workgroup of eight waves per compute unit where streams are few, as long as a wave has four tiles: 128 streams of 128 tiles
-// take 16.9 us in 2 splits, 19.9 in 1, 17.9 in 4; 16 streams of 32 tiles 7.3 us in 1, 8.2 in 2 (the merge is a launch).
-int mx_auto_splits(int Bt, int T, int H, int H_kv, int64_t S_max) {
-  const int64_t queries = (int64_t)T * (H / H_kv), rows = mx_query_rows(queries, false);
+// take 16.9 us in 2 splits, 19.9 in 1, 17.9 in 4; 16 streams of 32 tiles 7.3 us in 1, 8.2 in 2 (the merge is a launch).  Eight
+// queries of 128 elements over 32 streams of 512 tiles: bf16, one workgroup for all, 42.7 us in 8 splits, 61.4 in 4; fp32, two
+// workgroups, 67.2 in 8 and 60.6 in 4.
+int mx_auto_splits(int Bt, int T, int H, int H_kv, int64_t S_max, bool f32) {
+  const int64_t queries = (int64_t)T * (H / H_kv), rows = mx_query_rows(queries, f32);
   const int64_t groups = (int64_t)Bt * H_kv * ((queries + rows - 1) / rows), tiles = (S_max + MX_TILE - 1) / MX_TILE;
   int64_t splits = 256 / groups;
   const int64_t most = tiles / (4 * MX_ATTN_WAVES);
@@ -1224,7 +1226,7 @@ extern "C" size_t photon_mxfp4_decode_attn_workspace_bytes(int32_t Bt, int32_t T
 
 extern "C" int32_t photon_mxfp4_decode_attn_auto_splits(int32_t Bt, int32_t T, int32_t H, int32_t H_kv, int64_t S_max) {
   if (Bt <= 0 || T <= 0 || H_kv <= 0 || H < H_kv || S_max <= 0) return 1;
-  return mx_auto_splits(Bt, T, H, H_kv, S_max);
+  return mx_auto_splits(Bt, T, H, H_kv, S_max, false);       // bf16 rows: the more of the two
 }
 
 extern "C" int32_t photon_mxfp4_decode_attn(const void* q, int64_t q_stride, const void* k_cache, const void* v_cache, const int32_t* seq_len,
@@ -1247,7 +1249,7 @@ extern "C" int32_t photon_mxfp4_decode_attn(const void* q, int64_t q_stride, con
                  PHOTON_ERR_UNSUPPORTED, "%s: T=%d queries of %d heads a K/V head are too many", __func__, T, H / H_kv);
   PHOTON_REQUIRE(q_stride >= (int64_t)H * d_h, PHOTON_ERR_INVALID_ARG, "%s: q_stride=%lld is less than a row of %d heads of %d", __func__,
                  (long long)q_stride, H, d_h);
-  if (n_splits == 0) n_splits = photon_mxfp4_decode_attn_auto_splits(Bt, T, H, H_kv, S_max);
+  if (n_splits == 0) n_splits = mx_auto_splits(Bt, T, H, H_kv, S_max, dt == PHOTON_F32);
   if (n_splits > 1) {
     const size_t need = photon_mxfp4_decode_attn_workspace_bytes(Bt, T, H, d_h, n_splits);
     PHOTON_REQUIRE(workspace != nullptr && aligned16(workspace) && workspace_bytes >= need, PHOTON_ERR_WORKSPACE,

@@ -624,7 +624,7 @@ static int32_t stream_step(const Ctx& x, const photon_module_weights& mod, void*
   const int pitch = kv_row_elems(c.d_h);
   const size_t layer_cache = layer_cache_bytes(c, x.Bt, S_cap);
   const bool mx = c.kv_dt == PHOTON_MXFP4;
-  if (mx) n_splits = std::min(n_splits, mx_auto_splits(x.Bt, units, c.H, c.H, S_cap));   // partial results of the same size
+  if (mx) n_splits = std::min(n_splits, mx_auto_splits(x.Bt, units, c.H, c.H, S_cap, true));   // partial results of the same size
   const float scale = 1.0f / sqrtf((float)c.d_h);
   for (int i = 0; i < c.n_layers; ++i) {
     const photon_layer_weights& lw = mod.layers[i];
