@@ -26,9 +26,9 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 // Neighbouring workgroups take neighbouring heads of the same positions (but see launch_rows), those of one die (blocks are dealt to
 // the eight dies in turn) heads that lie side by side, since heads of 52 to 60 elements share lines (4 x 8192 bf16 rows of 32 x 60
 // elements: written in 190 us and read back in 148 without, in 120 and 109 with).
-// Measured for four prompts of 8192 rows of 32 x 64 elements (K and V): fp32 written in 113 us = 5.4 TB/s (537 MB in, 71 MB out) and
-// read back in 118 = 5.1; bf16 in 70 us = 4.9 and 67 = 5.1.  Without its stores the write takes 97 us (fp32): memory is the bound,
-// in both directions.
+// Measured for four prompts of 8192 rows of 32 x 64 elements (K and V, 1.2 GB of them in turn): fp32 written in 104 us = 5.8 TB/s
+// (537 MB in, 71 MB out) and read back in 128 = 4.7, in turn with each other 114 and 120; bf16 in 71 us = 4.8 and 73 = 4.7.  Without
+// its stores the write takes 97 us (fp32): memory is the bound, in both directions.
 
 constexpr int MX_WAVES = 4;      // waves of a workgroup, at most: 64 positions
 constexpr int MX_STEP = 16;      // positions of a wave
@@ -327,8 +327,10 @@ __global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_read_kernel(const uint8_t
 // what bounds a step's append.  Up to MX_FEW rows per sequence are taken with a lane per 8 elements of a head instead, all rows
 // of 64 / (4 NB) heads by one wave: 256 sequences append one bf16 row of 32 x 52 elements in 4.4 us (7.9 with the kernel above),
 // three in 5.3 (9.8), four in 6.1 (9.9) and read them back in 3.5 (5.8), 4.5 (7.6) and 5.0 (7.8); four sequences of 32 x 64 fp32
-// elements one in 2.9 (3.5), four in 4.0 (3.5).  V words are put together nibble by nibble, 8 of them a lane, in the one or two
-// groups of 8 positions that the rows are in.
+// elements one in 2.9 (3.5), four in 4.0 (3.5).  These are kernels by themselves, their rows and tiles in the chip's caches; from
+// HBM 256 sequences' three rows take 5.6 and 5.0, four sequences' one 4.8 and 4.7.  The rule goes by the rows of a sequence alone: four
+// of few sequences lose the half microsecond above, which shows in a graph only (a call from the host takes 6 us either way).
+// V words are put together nibble by nibble, 8 of them a lane, in the one or two groups of 8 positions that the rows are in.
 constexpr int MX_FEW = 4;        // rows of a sequence, at most
 
 struct MxFew {
@@ -514,10 +516,11 @@ __global__ __launch_bounds__(MX_WAVES * 64) void mxfp4_read_few_kernel(const uin
 //     positions that stays below 2^106.  From the first tile on that holds larger V for it (scale byte MX_LARGE and up) a wave
 //     takes V in units of 2^MX_UNIT, in its slow body: below 2^103 for fp32's largest.  Results of waves and splits are means and
 //     put together as such (serving and grouped heads take as long as they did without; short streams of 2 - 3 tiles 16.7 us, 16.2).
-// Bound by HBM where streams are many (256 x 16 streams of 2048 positions: 573 MB in 83.8 us = 6.8 TB/s; 184 vector instructions a
+// Bound by HBM where streams are many (256 x 16 streams of 2048 positions: 573 MB in 84.5 us = 6.8 TB/s; 186 vector instructions a
 // tile of 64 x 64, 16 of them MFMAs, of about 380 that the bytes leave time for), by the start and the end of a wave where they are
-// few or short (4 x 32 streams of 8192 positions: 71 MB in 16.1 us with the merge), by the weights' instructions and two waves a
-// SIMD with eight queries of 128 elements (143 MB in 43.7 us, one query 29.8).
+// few or short (4 x 32 streams of 8192 positions: 71 MB in 15.8 us with the merge, 16.8 with none of it in a cache), by the weights'
+// instructions and two waves a SIMD with eight queries of 128 elements (699 a tile, 64 of them MFMAs: 143 MB in 42.3 us, four
+// queries 33, one 28).
 constexpr float MX_RAISE = 8.f;
 constexpr float MX_LOWEST = -3.402823466e38f;    // of fp32: no finite score is below it
 constexpr uint32_t MX_LARGE = 192, MX_UNIT = 64; // scale byte from which V is large, and log2 of the unit it is taken in then
