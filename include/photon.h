@@ -41,7 +41,7 @@ extern "C" {
 #endif
 
 /* PHOTON_FP8_E4M3: 8-bit floating point (OCP E4M3: bias 7, no infinities, largest finite value 448), accepted only
- * as the storage type of a coarse K/V cache (photon_config.kv_dt, photon_coarse_decode_attn). */
+ * as the storage type of a coarse K/V cache (photon_config.kv_dt, photon_coarse_decode_attn, photon_paged_cache.kv_dt). */
 /* PHOTON_MXFP4: 4-bit floating point in blocks of 32 under a scale (see photon_mxfp4_cache_write), accepted only as
  * photon_config.kv_dt. */
 typedef enum { PHOTON_F32 = 0, PHOTON_BF16 = 1, PHOTON_FP8_E4M3 = 2, PHOTON_MXFP4 = 3 } photon_dtype;
@@ -205,6 +205,93 @@ PHOTON_API int32_t photon_mxfp4_decode_attn(const void* q, int64_t q_stride, con
                                             const int32_t* seq_len, const int32_t* n_new, void* out, int32_t Bt, int32_t T, int32_t H,
                                             int32_t H_kv, int32_t d_h, int64_t S_max, float scale, int32_t n_splits, void* workspace,
                                             size_t workspace_bytes, photon_dtype dt, void* stream);
+
+/* --------------------------------------------------------------------------
+ * Paged K/V cache: a variant of the coarsest stream's cache (Eq. 12-13) whose
+ * entries live in pages that sequences are given as they grow, or share (a
+ * prompt that several of them begin with).
+ *
+ * Layout.  A pool (one for K, one for V) is [n_pages][H_kv][page_size][d_p] in
+ * kv_dt, d_p = photon_kv_row_elems(d_h): a page holds page_size consecutive
+ * entries of a sequence, all K/V heads.  Entry s of sequence b is row
+ * s % page_size of page page_table[b][s / page_size].  Columns d_h .. d_p-1 of
+ * entries in use must hold zeros (photon_paged_cache_write does that); places
+ * never written, and table places behind a sequence's last entry, may hold
+ * anything.  Every call checks a page's number before it uses it: an entry whose
+ * page is outside [0, n_pages) is not there.  It is neither written, moved nor
+ * seen, and PHOTON_STATUS_BAD_PAGE is ORed into the call's status word.
+ *
+ * page_size: 16, 32, 64, 128 or 256.  kv_dt: fp32, bf16, or E4M3 bytes (rounded
+ * to nearest even, saturated at +-448, no scale), with rows of either dtype.
+ * Pools must be 16-byte aligned and may not share memory.  Rows (q, k, v,
+ * q_out, out) need the alignment of their elements only; whole multiples of 16
+ * bytes (pointer, stride, d_h / 2) are read fastest.  d_h in [1, 128];
+ * max_pages * page_size <= 2^31 - 256.  Bt == 0 or T == 0 is a no-op.
+ * -------------------------------------------------------------------------- */
+typedef struct photon_paged_cache {   /* host struct of device pointers, read during the call only */
+  void* k_pages;
+  void* v_pages;
+  const int32_t* page_table;          /* [Bt][max_pages] */
+  int32_t n_pages;                    /* pages of a pool */
+  int32_t page_size;                  /* entries of a page */
+  int32_t max_pages;                  /* table places of a sequence */
+  int32_t H_kv, d_h;
+  photon_dtype kv_dt;
+} photon_paged_cache;
+
+/* Appends T new rows per sequence: row t of sequence b becomes entry start[b] + t, and its K is rotated (as the encoder's is:
+ * pairs (i, i + d_h/2), angle position * rope_theta^(-2i/d_h)) on the way.
+ *   k, v       rows [Bt*T] of [H_kv, d_h] dt, row_stride elements from one to the next (parts of a QKV projection's rows included)
+ *   q, q_out   both NULL, or rows [Bt*T] of [H, d_h] dt, q_stride and q_out_stride elements apart: q_out receives the rows of q,
+ *              rotated alike (q_out == q with one stride rotates in place; other overlaps are not allowed)
+ *   start      [Bt] int32, device, or NULL: 0 (a prompt)
+ *   n_new      [Bt] int32, device, or NULL: T; only the first n_new[b] rows of sequence b are used (a padded batch)
+ *   position   [Bt][T] int32, device, or NULL: start[b] + t; the rotary position of a row where it is not its place (nodes of a
+ *              drafted tree sit at their depth).  Any value; angles are formed to 2^-31 turns
+ *   rope_theta 0: no rotation; else >= 1 and d_h even
+ *   status     NULL, or a device word: PHOTON_STATUS_CACHE_FULL is ORed into it when a row's entry is outside [0, max_pages *
+ *              page_size) (it is not written), PHOTON_STATUS_BAD_PAGE as above.  q_out does not depend on either
+ * Rotation in fp32, one rounding on store.  Two rows of a call that go to one place (a page that is twice in the table) leave
+ * either of them there. */
+PHOTON_API int32_t photon_paged_cache_write(const photon_paged_cache* cache, const void* k, const void* v, int64_t row_stride,
+                                            const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride, const int32_t* start,
+                                            const int32_t* n_new, const int32_t* position, int32_t* status, int32_t Bt, int32_t T,
+                                            int32_t H, float rope_theta, photon_dtype dt, void* stream);
+
+/* Moves entries within every sequence, K and V: entry start[b] + i becomes what entry start[b] + from[b][i] was before the call,
+ * i < n[b].  Keeps the accepted path of a drafted tree: its nodes, written behind each other, move up to the sequence's end.
+ *   from       [Bt][T] int32, device; any order, entries may repeat
+ *   n          [Bt] int32, device, or NULL: T.  T <= 64
+ *   status     as for the write
+ * An entry that comes from, or would go to, a place that is not there is left out.  A page that another sequence of the call
+ * reads is not to be written by this one. */
+PHOTON_API int32_t photon_paged_cache_move(const photon_paged_cache* cache, const int32_t* start, const int32_t* from, const int32_t* n,
+                                           int32_t* status, int32_t Bt, int32_t T, void* stream);
+
+/* Attention of T new queries per sequence over the pages; H / H_kv consecutive query heads share a K/V head.  The last n_new[b] of
+ * the seq_len[b] entries are the queries' own (written before).  Query t < n_new[b] sees all entries before them and, of the own
+ * ones, those up to t; or, with `tree`, own entry j where bit j of tree[b][t] is set (its ancestors and itself):
+ *     out[b,t,h,:] = softmax(scale * q[b,t,h,:] . K) V   over what it sees; nothing: zeros.
+ *   q        rows [Bt*T] of [H, d_h] dt, q_stride elements from one to the next
+ *   seq_len  [Bt] int32, device; values outside [0, S_max] count as the nearer end.  Own entries before entry 0 are not there
+ *   n_new    [Bt] int32, device, or NULL: T; queries past n_new[b] are skipped, their rows of out left as they were
+ *   tree     [Bt][T] uint64, device, or NULL.  T <= 64 with it; bits n_new[b] and up count for nothing
+ *   out      [Bt, T, H, d_h] dt
+ *   status   NULL, or a device word that PHOTON_STATUS_BAD_PAGE is ORed into
+ *   S_max    the most entries that a sequence has, at most max_pages * page_size (a bound that is close chooses better splits)
+ * Scores, softmax, weights and sums are in fp32 for either dt; a bf16 result is rounded once.  Entries that a query does not see
+ * do not touch its result, whatever they hold.  Results are finite wherever scale * q . K and the sum of |V| over the entries
+ * seen are, in fp32.
+ * The entries are split over n_splits workgroups per stream (0 = choose from shape and dt); partial results are merged in a fixed
+ * order, so the result is run-to-run deterministic for a given n_splits.  The workspace holds them:
+ * photon_paged_attn_workspace_bytes() of the same arguments, for either dt (0 bytes for n_splits == 1, or where 0 chooses 1; no
+ * initialisation; calls that share one must be stream-ordered). */
+PHOTON_API size_t photon_paged_attn_workspace_bytes(const photon_paged_cache* cache, int32_t Bt, int32_t T, int32_t H, int64_t S_max,
+                                                    int32_t n_splits);
+PHOTON_API int32_t photon_paged_attn(const photon_paged_cache* cache, const void* q, int64_t q_stride, const int32_t* seq_len,
+                                     const int32_t* n_new, const uint64_t* tree, void* out, int32_t* status, int32_t Bt, int32_t T,
+                                     int32_t H, int64_t S_max, float scale, int32_t n_splits, void* workspace, size_t workspace_bytes,
+                                     photon_dtype dt, void* stream);
 
 /* --------------------------------------------------------------------------
  * Chunk-local causal attention of the local decoders (paper Eq. 6-7): every
@@ -381,8 +468,9 @@ typedef struct photon_state {
 typedef enum {
   PHOTON_STATUS_CACHE_FULL = 1,       /* a sequence had seq_len == S_max on entry: its count stays, its new K/V entry
                                          overwrites the last one and its results of the step are not valid */
-  PHOTON_STATUS_BARRIER_TIMEOUT = 2   /* a grid-barrier wait of a persistent launch ran out (see photon_set_persistent):
+  PHOTON_STATUS_BARRIER_TIMEOUT = 2,  /* a grid-barrier wait of a persistent launch ran out (see photon_set_persistent):
                                          every workgroup left the kernel; the step's results are not valid */
+  PHOTON_STATUS_BAD_PAGE = 4          /* paged cache only: a page's number is outside the pool */
 } photon_step_status;
 
 /* Optional outputs for inspection (each pointer may be NULL). */

@@ -1,0 +1,591 @@
+// Attention over a paged K/V cache: the kernel.
+//
+// Mathematics.  For the rows q_r of a stream (token t, query head h; T * H / H_kv of them share a K/V head), one pass over the
+// entries keeps per row the reference top_r, the sum l_r = sum_j 2^(s_rj - top_r) and o_r = sum_j 2^(s_rj - top_r) V_j, with
+// s_rj = q_r . K_j * scale * log2 e.  top_r rises only when a score exceeds it by 2^RAISE (then l_r and o_r shrink), so that most
+// steps need nothing from another lane.  The result is o_r / l_r; parts of the entries are put together as means weighted by
+// l_r 2^top_r.
+//
+// Operands.  A wave takes R tiles of 16 rows over steps of 32 entries, in registers alone:
+//   S^T = K Q^T   A: 16 entries x elements, a lane's operand is what it loads of one entry's row; B: 16 rows x elements.  Lane
+//                 (c, g) = (lane % 16, lane / 16) receives the scores of row c with entries 4 g .. 4 g + 3 of either tile of 16
+//   O^T = V^T P^T B: those weights as they are: contraction index 8 g + i is entry 4 g + i of the first tile (i < 4) or
+//                 4 g + i - 4 of the second.  A: elements x entries: a lane loads elements 2 NB c .. of eight entries and interleaves
+//                 pairs of entries (v_perm_b32, one for every two values), since the contraction runs over entries
+// so that neither the weights nor V change lanes, nothing goes through LDS, and a row's shrinking factor is in the lane that needs
+// it.  fp32 pages: the same with 16x16x4 fp32 products, in which V needs no interleaving.
+//
+// Precision.  Products of bf16 and E4M3 entries (which bf16 holds exactly) run on the bf16 matrix cores.  fp32 queries enter as three
+// bf16 parts, weights as two parts (17 bits; the result is rounded to 9) for bf16 rows and as three for fp32 rows.
+#pragma once
+#include <float.h>
+
+#include "photon_device.h"
+#include "photon_paged.h"
+
+namespace photon {
+
+constexpr int PAGED_STEP = 32;                 // entries of a step
+constexpr int PAGED_WAVES = 4;                 // of a workgroup
+constexpr float PAGED_RAISE = 8.f;
+constexpr float PAGED_LOWEST = -FLT_MAX;       // a row's reference before it saw a score
+
+struct PagedAttnArgs {
+  PagedPools pool;
+  const void* q;
+  void* out;
+  float* ws;                                   // n_splits > 1: [rows of out][n_splits][d_p], then [rows of out][n_splits][top, sum]
+  const int32_t *seq_len, *n_new;
+  const uint64_t* tree;
+  int32_t* status;
+  int64_t q_stride;
+  int32_t S_max, Bt, T, H, group, row_groups, n_splits, units;   // units: streams * splits
+  float scale_log2e;
+  bool q_pieces, out_pieces;                   // rows of q, of out: aligned to 4 elements
+};
+
+// Launches over the tile of rows that `a` calls for; one translation unit per page type.
+int32_t paged_attn_f32(const PagedAttnArgs& a, bool f32_rows, hipStream_t st);
+int32_t paged_attn_bf16(const PagedAttnArgs& a, bool f32_rows, hipStream_t st);
+int32_t paged_attn_e4m3(const PagedAttnArgs& a, bool f32_rows, hipStream_t st);
+
+// Row tiles of a wave and waves side by side over rows, by the rows that share a K/V head.
+struct PagedTile { int tiles, waves; };
+inline PagedTile paged_tile(int64_t rows) {
+  return rows <= 16 ? PagedTile{1, 1} : rows <= 32 ? PagedTile{2, 1} : rows <= 64 ? PagedTile{2, 2} : PagedTile{2, 4};
+}
+
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t uint2v_t __attribute__((ext_vector_type(2)));
+
+// x * y, not merged with a subtraction that follows: the reference was rounded, too.
+__device__ __forceinline__ float rounded_product(float x, float y) {
+#pragma clang fp contract(off)
+  return x * y;
+}
+__device__ __forceinline__ uint32_t high_halves(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); }
+__device__ __forceinline__ float high_part(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+// Over the four lanes that share a row (16 apart).
+template <typename F> __device__ __forceinline__ float over_row(float x, F f) {
+  const uint2v_t r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  const uint2v_t h = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return f(__uint_as_float(h[0]), __uint_as_float(h[1]));
+}
+
+template <int BYTES> __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w) {
+  if constexpr (BYTES >= 16) {
+#pragma unroll
+    for (int i = 0; i < BYTES / 16; ++i) {
+      const uint4_t x = *reinterpret_cast<const uint4_t*>(p + 16 * i);
+      w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
+    }
+  } else if constexpr (BYTES == 8) {
+    const uint2v_t x = *reinterpret_cast<const uint2v_t*>(p);
+    w[0] = x[0]; w[1] = x[1];
+  } else if constexpr (BYTES == 4) {
+    w[0] = *reinterpret_cast<const uint32_t*>(p);
+  } else {
+    w[0] = *reinterpret_cast<const uint16_t*>(p);
+  }
+}
+
+// Elements e of words of a pool's type as fp32, and whether one of a word's is no finite number.
+template <typename KV> __device__ __forceinline__ float element(const uint8_t* row, int d);
+template <> __device__ __forceinline__ float element<float>(const uint8_t* row, int d) { return reinterpret_cast<const float*>(row)[d]; }
+template <> __device__ __forceinline__ float element<bf16_t>(const uint8_t* row, int d) { return to_f32<bf16_t>(reinterpret_cast<const bf16_t*>(row)[d]); }
+template <> __device__ __forceinline__ float element<fp8_t>(const uint8_t* row, int d) {
+  return __builtin_amdgcn_cvt_f32_fp8((int)row[d], 0);
+}
+template <typename KV> __device__ __forceinline__ uint32_t without_unbounded(uint32_t w) {
+  if constexpr (sizeof(KV) == 4) return (w & 0x7f800000u) == 0x7f800000u ? 0u : w;
+  if constexpr (sizeof(KV) == 2) return w & ~(((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u));
+  if constexpr (sizeof(KV) == 1) {
+    const uint32_t nan = (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;    // a one in every byte that is NaN
+    return w & ~(nan * 255u);
+  }
+}
+
+// What a kernel of these types holds: NB = d_p / 32.
+template <typename KV, typename T, int NB> struct PagedTypes {
+  static constexpr bool F32 = sizeof(KV) == 4;
+  static constexpr int DP = 32 * NB, TILES = 2 * NB;                             // TILES of 16 elements: the value products of a row tile
+  static constexpr int K_WORDS = 2 * NB * (int)sizeof(KV);                       // of a lane, per tile of 16 entries
+  static constexpr int V_BYTES = 2 * NB * (int)sizeof(KV), V_WORDS = V_BYTES < 4 ? 1 : V_BYTES / 4;   // of a lane, per entry
+  static constexpr int Q_PARTS = F32 || sizeof(T) == 2 ? 1 : 3, P_PARTS = sizeof(T) == 2 ? 2 : 3;
+  static constexpr int Q_WORDS = F32 ? 8 * NB : 4 * NB * Q_PARTS;
+};
+
+// Element that word 0 of product f's operand begins with in lane group g (bf16 operands: eight from there; fp32: four).
+template <typename KV, int NB> __device__ __forceinline__ int operand_element(int f, int g) {
+  if constexpr (sizeof(KV) == 4) return 16 * f + 4 * g;                          // f < 2 NB
+  if constexpr (sizeof(KV) == 2) return 32 * f + 8 * g;                          // f < NB
+  return NB == 4 ? (f / 2) * 64 + 16 * g + (f % 2) * 8 : NB == 2 ? 16 * g + 8 * f : 8 * g;
+}
+
+template <typename KV, int NB> __device__ __forceinline__ void load_keys(const uint8_t* row, int g, uint32_t (&w)[2 * NB * sizeof(KV)]) {
+  if constexpr (sizeof(KV) == 1) {
+    if constexpr (NB == 4) { load_words<16>(row + 16 * g, w); load_words<16>(row + 64 + 16 * g, w + 4); }
+    else if constexpr (NB == 2) load_words<16>(row + 16 * g, w);
+    else load_words<8>(row + 8 * g, w);
+  } else {
+#pragma unroll
+    for (int f = 0; f < NB * (int)sizeof(KV) / 2; ++f) load_words<16>(row + 64 * f + 16 * g, w + 4 * f);
+  }
+}
+
+// The bf16 operand of product f out of a lane's key words.
+template <typename KV> __device__ __forceinline__ bf16x8_t key_operand(const uint32_t* w, int f) {
+  uint4_t x;
+  if constexpr (sizeof(KV) == 2) {
+    x = uint4_t{w[4 * f], w[4 * f + 1], w[4 * f + 2], w[4 * f + 3]};
+  } else {
+    x.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * f], 1.f, false));
+    x.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * f], 1.f, true));
+    x.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * f + 1], 1.f, false));
+    x.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * f + 1], 1.f, true));
+  }
+  return as_bf16x8(x);
+}
+
+// The bf16 operand of element j (of a lane's 2 NB): eight entries.
+template <typename KV, int VW> __device__ __forceinline__ bf16x8_t value_operand(const uint32_t (&v)[8][VW], int j) {
+  uint32_t x[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(KV) == 2) {
+      x[i] = __builtin_amdgcn_perm(v[2 * i + 1][j / 2], v[2 * i][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
+    } else {
+      const uint32_t both = __builtin_amdgcn_perm(v[2 * i + 1][j / 4], v[2 * i][j / 4], j % 4 < 2 ? 0x05010400u : 0x07030602u);
+      x[i] = j % 2 ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(both, 1.f, true))
+                   : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(both, 1.f, false));
+    }
+  }
+  return as_bf16x8(uint4_t{x[0], x[1], x[2], x[3]});
+}
+
+// Four elements of a row of q from element d on; zeros behind the head.
+template <typename T> __device__ __forceinline__ void load_query4(const T* row, int d, int d_h, bool pieces, float (&x)[4]) {
+  if (pieces && d + 4 <= d_h) {
+    if constexpr (sizeof(T) == 4) {
+      const float4_t r = *reinterpret_cast<const float4_t*>(row + d);
+      x[0] = r.x; x[1] = r.y; x[2] = r.z; x[3] = r.w;
+    } else {
+      const uint2v_t r = *reinterpret_cast<const uint2v_t*>(row + d);
+      x[0] = bf16_lo(r[0]); x[1] = bf16_hi(r[0]); x[2] = bf16_lo(r[1]); x[3] = bf16_hi(r[1]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = d + e < d_h ? to_f32<T>(row[d + e]) : 0.f;
+  }
+}
+// Four elements of a row of out.
+template <typename T> __device__ __forceinline__ void store_result4(T* row, int d, int d_h, bool pieces, const float (&x)[4]) {
+  if (pieces && d + 4 <= d_h) {
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4_t*>(row + d) = float4_t{x[0], x[1], x[2], x[3]};
+    else *reinterpret_cast<uint2v_t*>(row + d) = uint2v_t{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (d + e < d_h) row[d + e] = from_f32<T>(x[e]);
+  }
+}
+
+// Entries that count for sequence b, its queries, and the entries before theirs (less than 0: the first own ones are not there).
+__device__ __forceinline__ void paged_sequence(const PagedAttnArgs& a, int b, int& n, int& m, int& past) {
+  n = a.seq_len[b];
+  n = n < 0 ? 0 : n > a.S_max ? a.S_max : n;
+  m = a.n_new ? a.n_new[b] : a.T;
+  m = m < 0 ? 0 : m > a.T ? a.T : m;
+  past = n - m;
+}
+
+// R row tiles a wave, RW waves side by side over rows; the other PAGED_WAVES / RW deal the steps among themselves.
+template <typename KV, typename T, int NB, int R, int RW>
+__global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnArgs a) {
+  using Y = PagedTypes<KV, T, NB>;
+  constexpr int DP = Y::DP, TILES = Y::TILES, KW = PAGED_WAVES / RW, PITCH = DP + 4;
+  __shared__ __align__(16) float results[KW > 1 ? PAGED_WAVES * 16 * PITCH : 4];
+  __shared__ float stats[PAGED_WAVES][16][2];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
+  const int kw = wave % KW, rw = wave / KW;
+
+  // The workgroups of a stream's row groups read the same entries: they are given numbers that are equal modulo 8, one die's, in turn.
+  int unit = blockIdx.x, row_group = 0;
+  if (a.row_groups > 1) {
+    const int y = blockIdx.x >> 3;
+    row_group = y % a.row_groups;
+    unit = (y / a.row_groups) * 8 + (blockIdx.x & 7);
+    if (unit >= a.units) return;
+  }
+  const int hk = unit % a.pool.H_kv, split = unit / a.pool.H_kv % a.n_splits, b = unit / a.pool.H_kv / a.n_splits;
+
+  int n, m, past;
+  paged_sequence(a, b, n, m, past);
+  const int64_t rows = (int64_t)m * a.group;
+  const int64_t group_first = (int64_t)row_group * (RW * R * 16), first = group_first + rw * (R * 16);
+  if (group_first >= rows) return;
+  const int64_t group_last = min(group_first + RW * R * 16, rows) - 1;
+  const int hi = a.tree ? n : min(n, past + (int)(group_last / a.group) + 1);               // entries that a row of the workgroup sees
+  const int steps = hi <= 0 ? 0 : (hi + PAGED_STEP - 1) / PAGED_STEP;
+  const int s0 = (int)((int64_t)steps * split / a.n_splits), s1 = (int)((int64_t)steps * (split + 1) / a.n_splits);
+  const int all_see = a.tree ? past : past + (int)(min(first, rows - 1) / a.group) + 1;    // entries that every row of the wave sees
+
+  // Rows: those behind the last are given its values and not stored.
+  uint32_t qw[R][Y::Q_WORDS];
+  int limit[R];
+  uint64_t bits[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int64_t row = min(first + r * 16 + c, rows - 1);
+    const int t = (int)(row / a.group), h = hk * a.group + (int)(row - (int64_t)t * a.group);
+    limit[r] = past + t + 1;
+    bits[r] = 0;
+    if (a.tree) bits[r] = a.tree[(int64_t)b * a.T + t] & (m == 64 ? ~0ull : (1ull << m) - 1);
+    const T* from = (const T*)a.q + ((int64_t)b * a.T + t) * a.q_stride + (int64_t)h * a.pool.d_h;
+    if constexpr (Y::F32) {
+#pragma unroll
+      for (int f = 0; f < 2 * NB; ++f) {
+        float x[4];
+        load_query4<T>(from, operand_element<KV, NB>(f, g), a.pool.d_h, a.q_pieces, x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) qw[r][4 * f + e] = __float_as_uint(x[e]);
+      }
+    } else {
+#pragma unroll
+      for (int f = 0; f < NB; ++f)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          float x[4];
+          load_query4<T>(from, operand_element<KV, NB>(f, g) + 4 * half, a.pool.d_h, a.q_pieces, x);
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) {
+            float u = x[e], v = x[e + 1];
+#pragma unroll
+            for (int part = 0; part < Y::Q_PARTS; ++part) {
+              qw[r][(part * NB + f) * 4 + half * 2 + e / 2] = high_halves(u, v);
+              u -= high_part(u);
+              v -= high_part(v);
+            }
+          }
+        }
+    }
+  }
+  auto visible = [&](int r, int entry) {
+    if (!a.tree) return entry < limit[r];
+    return entry < past || ((bits[r] >> ((unsigned)(entry - past) & 63u)) & 1u) != 0;
+  };
+
+  float top[R], sum[R];
+  f32x4_t acc[R][TILES];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    top[r] = PAGED_LOWEST;
+    sum[r] = 0.f;
+#pragma unroll
+    for (int j = 0; j < TILES; ++j) acc[r][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // Where 16 entries from `entry` on lie; < 0: nowhere (behind the last, or a page outside the pool)
+  const int32_t* table = a.pool.table + (int64_t)b * a.pool.max_pages;
+  auto place = [&](int entry) -> int64_t {
+    if (entry >= n) return -1;
+    const int page = table[entry >> a.pool.page_shift];
+    if (page < 0 || page >= a.pool.n_pages) {
+      if (a.status && lane == 0) atomicOr(a.status, (int)PHOTON_STATUS_BAD_PAGE);
+      return -1;
+    }
+    return page * a.pool.page_bytes + hk * a.pool.head_bytes + (int64_t)((entry & ((1 << a.pool.page_shift) - 1)) * a.pool.row_bytes);
+  };
+  const int k_lane = c * a.pool.row_bytes, v_lane = 4 * g * a.pool.row_bytes + c * Y::V_BYTES;
+  uint32_t kx[2][Y::K_WORDS], vx[8][Y::V_WORDS];
+  auto load_k = [&](const int64_t (&at)[2]) {                                      // from nowhere: the pool's first entries, in bounds, not used
+#pragma unroll
+    for (int i = 0; i < 2; ++i) load_keys<KV, NB>(a.pool.k + (at[i] < 0 ? 0 : at[i]) + k_lane, g, kx[i]);
+  };
+  auto load_v = [&](const int64_t (&at)[2]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) load_words<Y::V_BYTES>(a.pool.v + (at[i / 4] < 0 ? 0 : at[i / 4]) + v_lane + (i % 4) * a.pool.row_bytes, vx[i]);
+  };
+
+  const bool has_rows = first < rows;
+  int step = s0 + kw;
+  int64_t at[2] = {-1, -1};
+  if (has_rows && step < s1) {
+    at[0] = place(step * PAGED_STEP);
+    at[1] = place(step * PAGED_STEP + 16);
+    load_k(at);
+    load_v(at);
+  }
+#pragma unroll 1
+  while (has_rows && step < s1) {
+    const int base = step * PAGED_STEP, next = step + KW;
+    int64_t next_at[2] = {-1, -1};
+    if (next < s1) {
+      next_at[0] = place(next * PAGED_STEP);
+      next_at[1] = place(next * PAGED_STEP + 16);
+    }
+    float s[R][8];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      f32x4_t d[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) d[r] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      if constexpr (Y::F32) {
+#pragma unroll
+        for (int f = 0; f < 8 * NB; ++f)
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+            d[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kx[i][f]), __uint_as_float(qw[r][f]), d[r], 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int f = 0; f < NB; ++f) {
+          const bf16x8_t key = key_operand<KV>(kx[i], f);
+#pragma unroll
+          for (int part = Y::Q_PARTS - 1; part >= 0; --part)
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+              const uint32_t* w = qw[r] + (part * NB + f) * 4;
+              d[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, as_bf16x8(uint4_t{w[0], w[1], w[2], w[3]}), d[r], 0, 0, 0);
+            }
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[r][4 * i + e] = rounded_product(d[r][e], a.scale_log2e);
+    }
+    if (next < s1) load_k(next_at);
+
+    const bool partial = base + PAGED_STEP > all_see || at[0] < 0 || at[1] < 0;
+    if (partial) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int entry = base + (i / 4) * 16 + 4 * g + i % 4;
+        const bool there = entry < n && at[i / 4] >= 0;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+          if (!there || !visible(r, entry)) s[r][i] = -INFINITY;
+      }
+    }
+    // weights
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float highest = s[r][0];
+#pragma unroll
+      for (int i = 1; i < 8; ++i) highest = fmaxf(highest, s[r][i]);
+      if (__builtin_amdgcn_ballot_w64(highest - top[r] > PAGED_RAISE) != 0) {
+        const float higher = fmaxf(top[r], over_row(highest, [](float x, float y) { return fmaxf(x, y); }));
+        const float shrink = fast_exp2(top[r] - higher);
+        top[r] = higher;
+        sum[r] *= shrink;
+#pragma unroll
+        for (int j = 0; j < TILES; ++j) acc[r][j] *= shrink;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        s[r][i] = fast_exp2(s[r][i] - top[r]);
+        sum[r] += s[r][i];
+      }
+    }
+    if (partial) {
+      // Entries that no row sees may hold anything: zeros.
+      uint32_t unbounded = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const bool there = base + (i / 4) * 16 + 4 * g + i % 4 < n && at[i / 4] >= 0;
+#pragma unroll
+        for (int w = 0; w < Y::V_WORDS; ++w) {
+          vx[i][w] = there ? vx[i][w] : 0u;
+          if (without_unbounded<KV>(vx[i][w]) != vx[i][w]) unbounded |= 1u << i;
+        }
+      }
+      // What one row sees and another does not may be an infinity or NaN, too: 0 times it is not 0, so these are added row by row.
+      if (m > 1 && __builtin_amdgcn_ballot_w64(unbounded != 0) != 0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const uint64_t lanes = __builtin_amdgcn_ballot_w64((unbounded >> i) & 1u);
+#pragma unroll 1
+          for (int other = 0; other < 4; ++other) {
+            if (((lanes >> (16 * other)) & 0xffffu) == 0) continue;
+            const int entry = base + (i / 4) * 16 + 4 * other + i % 4;
+            const uint8_t* row = a.pool.v + at[i / 4] + (4 * other + i % 4) * a.pool.row_bytes;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+              const float p = __shfl(s[r][i], 16 * other + c);
+              if (!visible(r, entry)) continue;
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int j = 0; j < TILES; ++j) {
+                  const float x = element<KV>(row, TILES * (4 * g + e) + j);
+                  if (!(fabsf(x) <= FLT_MAX)) acc[r][j][e] += p * x;
+                }
+            }
+          }
+#pragma unroll
+          for (int w = 0; w < Y::V_WORDS; ++w) vx[i][w] = without_unbounded<KV>(vx[i][w]);
+        }
+      }
+    }
+    if constexpr (Y::F32) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < TILES; ++j)
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+            acc[r][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vx[i][j]), s[r][i], acc[r][j], 0, 0, 0);
+    } else {
+      bf16x8_t p[R][Y::P_PARTS];
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        uint32_t w[Y::P_PARTS][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float x = s[r][2 * i], y = s[r][2 * i + 1];
+#pragma unroll
+          for (int part = 0; part + 1 < Y::P_PARTS; ++part) {
+            w[part][i] = high_halves(x, y);
+            x -= high_part(x);
+            y -= high_part(y);
+          }
+          w[Y::P_PARTS - 1][i] = pack_bf16x2(x, y);
+        }
+#pragma unroll
+        for (int part = 0; part < Y::P_PARTS; ++part) p[r][part] = as_bf16x8(uint4_t{w[part][0], w[part][1], w[part][2], w[part][3]});
+      }
+#pragma unroll
+      for (int j = 0; j < TILES; ++j) {
+        const bf16x8_t value = value_operand<KV, Y::V_WORDS>(vx, j);
+#pragma unroll
+        for (int part = Y::P_PARTS - 1; part >= 0; --part)
+#pragma unroll
+          for (int r = 0; r < R; ++r) acc[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value, p[r][part], acc[r][j], 0, 0, 0);
+      }
+    }
+    if (next < s1) load_v(next_at);
+    at[0] = next_at[0];
+    at[1] = next_at[1];
+    step = next;
+  }
+
+  // Results: lane (c, g) holds elements 8 NB g .. + 8 NB - 1 of its rows.  Each wave divides by its sum, and waves are put together as
+  // weighted means: no sum of values leaves the range that a wave's own is in.
+  const auto to_row = [&](int64_t row) {                                            // row of out
+    const int64_t t = row / a.group;
+    return ((int64_t)b * a.T + t) * a.H + hk * a.group + (row - t * a.group);
+  };
+  const auto emit = [&](int64_t row, int d, const float (&x)[4], float row_top, float row_sum) {
+    const int64_t to = to_row(row);
+    if (a.n_splits == 1) {
+      if (d < a.pool.d_h) store_result4<T>((T*)a.out + to * a.pool.d_h, d, a.pool.d_h, a.out_pieces, x);
+      return;
+    }
+    const int64_t piece = to * a.n_splits + split;
+    *reinterpret_cast<float4_t*>(a.ws + piece * DP + d) = float4_t{x[0], x[1], x[2], x[3]};
+    if (d == 0) {
+      float* st = a.ws + (int64_t)a.Bt * a.T * a.H * a.n_splits * DP + piece * 2;
+      st[0] = row_top;
+      st[1] = row_sum;
+    }
+  };
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const float l = over_row(sum[r], [](float x, float y) { return x + y; });
+    const float mean = l == 0.f ? 0.f : 1.f / l;
+    const int64_t row = first + r * 16 + c;
+    if constexpr (KW == 1) {
+      if (row < rows) {
+#pragma unroll
+        for (int x = 0; x < 8 * NB; x += 4) {
+          float o[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] = acc[r][(x + e) % TILES][(x + e) / TILES] * mean;
+          emit(row, 8 * NB * g + x, o, top[r], l);
+        }
+      }
+    } else {
+      if (r > 0) __syncthreads();
+      if (row < rows) {
+#pragma unroll
+        for (int x = 0; x < 8 * NB; x += 4) {
+          float4_t o;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] = acc[r][(x + e) % TILES][(x + e) / TILES] * mean;
+          *reinterpret_cast<float4_t*>(results + (wave * 16 + c) * PITCH + 8 * NB * g + x) = o;
+        }
+        if (g == 0) { stats[wave][c][0] = top[r]; stats[wave][c][1] = l; }
+      }
+      __syncthreads();
+      for (int x = tid; x < RW * 16 * (DP / 4); x += PAGED_WAVES * 64) {
+        const int d = x % (DP / 4) * 4, i = x / (DP / 4) % 16, of = x / (DP / 4) / 16 * KW;
+        const int64_t to = group_first + of / KW * (R * 16) + r * 16 + i;
+        if (to >= rows) continue;
+        float w_top = PAGED_LOWEST, w_sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < KW; ++w) w_top = fmaxf(w_top, stats[of + w][i][0]);
+        float weight[KW];
+#pragma unroll
+        for (int w = 0; w < KW; ++w) {
+          weight[w] = stats[of + w][i][1] * fast_exp2(stats[of + w][i][0] - w_top);
+          w_sum += weight[w];
+        }
+        const float inverse = w_sum == 0.f ? 0.f : 1.f / w_sum;
+#pragma unroll
+        for (int w = 0; w < KW; ++w) {
+          const float4_t y = *reinterpret_cast<const float4_t*>(results + ((of + w) * 16 + i) * PITCH + d);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] = fmaf(y[e], weight[w] * inverse, o[e]);
+        }
+        emit(to, d, o, w_top, w_sum);
+      }
+    }
+  }
+}
+
+// The splits' results of a row, in order, DP / 4 lanes to a row.
+template <typename T, int NB> __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
+  constexpr int DP = 32 * NB, LANES = DP / 4;
+  const int64_t to = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+  if (to >= (int64_t)a.Bt * a.T * a.H) return;
+  const int d = threadIdx.x % LANES * 4;
+  const int64_t token = to / a.H;
+  const int b = (int)(token / a.T), t = (int)(token - (int64_t)b * a.T);
+  int m = a.n_new ? a.n_new[b] : a.T;
+  if (t >= m) return;
+  const float* values = a.ws + to * a.n_splits * DP + d;
+  const float* stats = a.ws + (int64_t)a.Bt * a.T * a.H * a.n_splits * DP + to * a.n_splits * 2;
+  float top = PAGED_LOWEST, sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < a.n_splits; ++s) top = fmaxf(top, stats[2 * s]);
+  for (int s = 0; s < a.n_splits; ++s) sum += stats[2 * s + 1] * fast_exp2(stats[2 * s] - top);
+  const float inverse = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll 4
+  for (int s = 0; s < a.n_splits; ++s) {
+    const float4_t y = *reinterpret_cast<const float4_t*>(values + (int64_t)s * DP);
+    const float w = stats[2 * s + 1] * fast_exp2(stats[2 * s] - top) * inverse;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = fmaf(y[e], w, o[e]);
+  }
+  if (d < a.pool.d_h) store_result4<T>((T*)a.out + to * a.pool.d_h, d, a.pool.d_h, a.out_pieces, o);
+}
+
+template <typename KV, typename T, int NB, int R, int RW> int32_t paged_launch(const PagedAttnArgs& a, hipStream_t st) {
+  const unsigned grid = a.row_groups > 1 ? (unsigned)((a.units + 7) / 8 * 8) * (unsigned)a.row_groups : (unsigned)a.units;
+  PHOTON_LAUNCH(KC_COARSE_ATTN, st, (paged_attn_kernel<KV, T, NB, R, RW>), dim3(grid), dim3(PAGED_WAVES * 64), 0, st, a);
+  return check_launch("paged_attn_kernel");
+}
+template <typename KV, typename T, int NB> int32_t paged_launch_rows(const PagedAttnArgs& a, hipStream_t st) {
+  const PagedTile tile = paged_tile((int64_t)a.T * a.group);
+  if (tile.tiles == 1) return paged_launch<KV, T, NB, 1, 1>(a, st);
+  if (tile.waves == 1) return paged_launch<KV, T, NB, 2, 1>(a, st);
+  if (tile.waves == 2) return paged_launch<KV, T, NB, 2, 2>(a, st);
+  return paged_launch<KV, T, NB, 2, 4>(a, st);
+}
+template <typename KV> int32_t paged_launch_types(const PagedAttnArgs& a, bool f32_rows, hipStream_t st) {
+  const int nb = kv_row_elems(a.pool.d_h) / 32;
+  if (f32_rows) return nb == 1 ? paged_launch_rows<KV, float, 1>(a, st) : nb == 2 ? paged_launch_rows<KV, float, 2>(a, st) : paged_launch_rows<KV, float, 4>(a, st);
+  return nb == 1 ? paged_launch_rows<KV, bf16_t, 1>(a, st) : nb == 2 ? paged_launch_rows<KV, bf16_t, 2>(a, st) : paged_launch_rows<KV, bf16_t, 4>(a, st);
+}
+
+}  // namespace photon
