@@ -159,6 +159,23 @@ __device__ __forceinline__ uint32_t pack_f16x2_unit(float lo, float hi) {
 }
 __device__ __forceinline__ bf16x8_t as_bf16x8(const uint4_t& v) { return __builtin_bit_cast(bf16x8_t, v); }
 
+// 16 bytes per lane from global memory straight into LDS: lane l lands at lds_base + 16 l (lds_base: byte offset in
+// LDS, wave-uniform).  Written as an instruction rather than through the compiler's builtin: the compiler treats
+// the builtin as an access to both memories that may complete out of order, and while one is in flight it makes
+// every wait for an LDS read a wait for ALL LDS reads, which serialises the operand prefetch below.  Completion is
+// tracked by hand (s_waitcnt vmcnt) at the one place per slab where it matters.
+// m0 (the LDS base of the load) is named as clobbered so that the compiler keeps no value of its own in it across the
+// statement; it notes that m0 is a reserved register, which is the point here.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void load16_to_lds(const void* gsrc, uint32_t lds_base) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(gsrc), "s"(lds_base) : "memory", "m0");
+}
+__device__ __forceinline__ void load4_to_lds(const void* gsrc, uint32_t lds_base) {   // 4 bytes per lane
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(gsrc), "s"(lds_base) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
 // cos and sin of the rotary angle pos * theta^(-2i/d_h); the angle is formed in double because positions reach 10^5
 __device__ __forceinline__ void rope_angle(int pos, int i, int d_h, float theta, float& c, float& s) {
   if (theta == 0.f) { c = 1.f; s = 0.f; return; }

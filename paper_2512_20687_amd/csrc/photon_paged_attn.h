@@ -2,8 +2,8 @@
 //
 // Mathematics.  For the rows q_r of a stream (token t, query head h; T * H / H_kv of them share a K/V head), one pass over the
 // entries keeps per row the reference top_r, the sum l_r = sum_j 2^(s_rj - top_r) and o_r = sum_j 2^(s_rj - top_r) V_j, with
-// s_rj = q_r . K_j * scale * log2 e.  top_r rises only when a score exceeds it by 2^RAISE (then l_r and o_r shrink), so that most
-// steps need nothing from another lane.  The result is o_r / l_r; parts of the entries are put together as means weighted by
+// s_rj = q_r . K_j * scale * log2 e.  top_r rises only when weights pass RAISE (then l_r and o_r shrink), so that most steps need
+// nothing from another lane.  The result is o_r / l_r; parts of the entries are put together as means weighted by
 // l_r 2^top_r.
 //
 // Operands.  A wave takes R tiles of 16 rows over steps of 32 entries, in registers alone:
@@ -20,6 +20,8 @@
 #pragma once
 #include <float.h>
 
+#include <type_traits>
+
 #include "photon_device.h"
 #include "photon_paged.h"
 
@@ -27,7 +29,7 @@ namespace photon {
 
 constexpr int PAGED_STEP = 32;                 // entries of a step
 constexpr int PAGED_WAVES = 4;                 // of a workgroup
-constexpr float PAGED_RAISE = 8.f;
+constexpr float PAGED_RAISE = 256.f;          // sum of a lane's eight weights of a step from which on the reference rises
 constexpr float PAGED_LOWEST = -FLT_MAX;       // a row's reference before it saw a score
 
 struct PagedAttnArgs {
@@ -44,16 +46,21 @@ struct PagedAttnArgs {
   bool q_pieces, out_pieces;                   // rows of q, of out: aligned to 4 elements
 };
 
-// Launches over the tile of rows that `a` calls for; one translation unit per page type.
-int32_t paged_attn_f32(const PagedAttnArgs& a, bool f32_rows, hipStream_t st);
-int32_t paged_attn_bf16(const PagedAttnArgs& a, bool f32_rows, hipStream_t st);
-int32_t paged_attn_e4m3(const PagedAttnArgs& a, bool f32_rows, hipStream_t st);
-
-// Row tiles of a wave and waves side by side over rows, by the rows that share a K/V head.
-struct PagedTile { int tiles, waves; };
-inline PagedTile paged_tile(int64_t rows) {
-  return rows <= 16 ? PagedTile{1, 1} : rows <= 32 ? PagedTile{2, 1} : rows <= 64 ? PagedTile{2, 2} : PagedTile{2, 4};
+// How the rows that share a K/V head are taken: row tiles of a wave, waves side by side over rows, and by which kernel.
+struct PagedTile {
+  int tiles, waves;
+  bool wide;                                   // photon_paged_attn_wide.h's
+  int rows() const { return 16 * tiles * waves; }
+};
+inline PagedTile paged_tile(int64_t rows, bool f32_rows, photon_dtype kv_dt) {
+  if (rows > 64 && !f32_rows && kv_dt == PHOTON_BF16) return PagedTile{2, rows <= 128 ? 4 : 8, true};
+  return rows <= 16 ? PagedTile{1, 1, false} : rows <= 32 ? PagedTile{2, 1, false} : rows <= 64 ? PagedTile{2, 2, false} : PagedTile{2, 4, false};
 }
+
+// Launches over the tile of rows that `a` calls for; one translation unit per page type.
+int32_t paged_attn_f32(const PagedAttnArgs& a, const PagedTile& tile, bool f32_rows, hipStream_t st);
+int32_t paged_attn_bf16(const PagedAttnArgs& a, const PagedTile& tile, bool f32_rows, hipStream_t st);
+int32_t paged_attn_e4m3(const PagedAttnArgs& a, const PagedTile& tile, bool f32_rows, hipStream_t st);
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t uint2v_t __attribute__((ext_vector_type(2)));
@@ -90,13 +97,7 @@ template <int BYTES> __device__ __forceinline__ void load_words(const uint8_t* p
   }
 }
 
-// Elements e of words of a pool's type as fp32, and whether one of a word's is no finite number.
-template <typename KV> __device__ __forceinline__ float element(const uint8_t* row, int d);
-template <> __device__ __forceinline__ float element<float>(const uint8_t* row, int d) { return reinterpret_cast<const float*>(row)[d]; }
-template <> __device__ __forceinline__ float element<bf16_t>(const uint8_t* row, int d) { return to_f32<bf16_t>(reinterpret_cast<const bf16_t*>(row)[d]); }
-template <> __device__ __forceinline__ float element<fp8_t>(const uint8_t* row, int d) {
-  return __builtin_amdgcn_cvt_f32_fp8((int)row[d], 0);
-}
+// A word of a pool's elements with zeros in place of infinities and NaN.
 template <typename KV> __device__ __forceinline__ uint32_t without_unbounded(uint32_t w) {
   if constexpr (sizeof(KV) == 4) return (w & 0x7f800000u) == 0x7f800000u ? 0u : w;
   if constexpr (sizeof(KV) == 2) return w & ~(((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u));
@@ -149,7 +150,7 @@ template <typename KV> __device__ __forceinline__ bf16x8_t key_operand(const uin
 }
 
 // The bf16 operand of element j (of a lane's 2 NB): eight entries.
-template <typename KV, int VW> __device__ __forceinline__ bf16x8_t value_operand(const uint32_t (&v)[8][VW], int j) {
+template <typename KV, int VW> __device__ __forceinline__ uint4_t value_operand(const uint32_t (&v)[8][VW], int j) {
   uint32_t x[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -161,7 +162,7 @@ template <typename KV, int VW> __device__ __forceinline__ bf16x8_t value_operand
                    : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(both, 1.f, false));
     }
   }
-  return as_bf16x8(uint4_t{x[0], x[1], x[2], x[3]});
+  return uint4_t{x[0], x[1], x[2], x[3]};
 }
 
 // Four elements of a row of q from element d on; zeros behind the head.
@@ -191,13 +192,203 @@ template <typename T> __device__ __forceinline__ void store_result4(T* row, int 
   }
 }
 
+// What one row sees and another does not may be an infinity or NaN, and 0 times it is not 0.  Such steps put zeros in the products, and
+// a second product tells which rows see which: operands of 2^16 for NaN, 2^8 for -infinity, 1 for infinity, 0 else, times 1 where a
+// row sees an entry.  Sums over 32 entries are exact, and their digits say what is added to the row's element.
+__device__ __forceinline__ float unbounded_code(float x) { return fabsf(x) <= FLT_MAX ? 0.f : x != x ? 0x1p16f : x < 0.f ? 0x1p8f : 1.f; }
+__device__ __forceinline__ uint4_t unbounded_codes(uint4_t w) {               // of bf16 pairs
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = high_halves(unbounded_code(bf16_lo(w[i])), unbounded_code(bf16_hi(w[i])));
+  return w;
+}
+__device__ __forceinline__ uint4_t seen_operand(uint32_t seen) {              // 1 where a lane's row sees its entry, in bf16
+  uint4_t w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = ((seen >> (2 * i)) & 1u ? 0x3f80u : 0u) | ((seen >> (2 * i + 1)) & 1u ? 0x3f800000u : 0u);
+  return w;
+}
+__device__ __forceinline__ void add_unbounded(f32x4_t& acc, const f32x4_t& digits) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t t = (uint32_t)digits[e];
+    if (t != 0) acc[e] += t >= 0x10000u || (t >= 0x100u && (t & 0xffu)) ? NAN : t >= 0x100u ? -INFINITY : INFINITY;
+  }
+}
+
 // Entries that count for sequence b, its queries, and the entries before theirs (less than 0: the first own ones are not there).
 __device__ __forceinline__ void paged_sequence(const PagedAttnArgs& a, int b, int& n, int& m, int& past) {
-  n = a.seq_len[b];
+  n = __builtin_amdgcn_readfirstlane(a.seq_len[b]);
   n = n < 0 ? 0 : n > a.S_max ? a.S_max : n;
-  m = a.n_new ? a.n_new[b] : a.T;
+  m = a.n_new ? __builtin_amdgcn_readfirstlane(a.n_new[b]) : a.T;
   m = m < 0 ? 0 : m > a.T ? a.T : m;
   past = n - m;
+}
+
+// Which stream, split and row group a workgroup takes.  The workgroups of a stream's row groups read the same entries: they are given
+// numbers that are equal modulo 8, one die's, in turn.
+__device__ __forceinline__ bool paged_unit(const PagedAttnArgs& a, int& row_group, int& hk, int& split, int& b) {
+  int unit = blockIdx.x;
+  row_group = 0;
+  if (a.row_groups > 1) {
+    const int y = blockIdx.x >> 3;
+    row_group = y % a.row_groups;
+    unit = (y / a.row_groups) * 8 + (blockIdx.x & 7);
+    if (unit >= a.units) return false;
+  }
+  hk = unit % a.pool.H_kv;
+  split = unit / a.pool.H_kv % a.n_splits;
+  b = unit / a.pool.H_kv / a.n_splits;
+  return true;
+}
+
+// Row `row` of stream (b, hk): its row of out.
+__device__ __forceinline__ int64_t paged_row(const PagedAttnArgs& a, int b, int hk, int64_t row) {
+  const int64_t t = row / a.group;
+  return ((int64_t)b * a.T + t) * a.H + hk * a.group + (row - t * a.group);
+}
+// Four elements of a row's result: to out, or with its reference and sum to the workspace.
+template <typename T, int DP>
+__device__ __forceinline__ void paged_emit(const PagedAttnArgs& a, int64_t to, int split, int d, const float (&x)[4], float top, float sum) {
+  if (a.n_splits == 1) {
+    if (d < a.pool.d_h) store_result4<T>((T*)a.out + to * a.pool.d_h, d, a.pool.d_h, a.out_pieces, x);
+    return;
+  }
+  const int64_t piece = to * a.n_splits + split;
+  *reinterpret_cast<float4_t*>(a.ws + piece * DP + d) = float4_t{x[0], x[1], x[2], x[3]};
+  if (d == 0) {
+    float* st = a.ws + (int64_t)a.Bt * a.T * a.H * a.n_splits * DP + piece * 2;
+    st[0] = top;
+    st[1] = sum;
+  }
+}
+// Where the 16 entries from `entry` on of a sequence of n lie; < 0: nowhere (behind the last, or a page outside the pool, which `bad`
+// remembers).
+__device__ __forceinline__ int64_t paged_place(const PagedAttnArgs& a, const int32_t* table, int hk, int entry, int n, bool& bad) {
+  if (entry >= n) return -1;
+  const int page = __builtin_amdgcn_readfirstlane(table[entry >> a.pool.page_shift]);
+  const bool there = page >= 0 && page < a.pool.n_pages;
+  bad = bad || !there;
+  return there ? page * a.pool.page_bytes + hk * a.pool.head_bytes + (int64_t)((entry & ((1 << a.pool.page_shift) - 1)) * a.pool.row_bytes) : -1;
+}
+__device__ __forceinline__ void paged_say(const PagedAttnArgs& a, bool bad, int lane) {
+  if (bad && a.status && lane == 0) atomicOr(a.status, (int)PHOTON_STATUS_BAD_PAGE);
+}
+
+// R tiles of 16 rows as a wave holds them: operands of the score products, and what each row sees.
+template <typename KV, typename T, int NB, int R> struct PagedRows {
+  using Y = PagedTypes<KV, T, NB>;
+  uint32_t w[R][Y::Q_WORDS];
+  int limit[R];                                // entries below are seen (without a tree)
+  uint64_t bits[R];                            // own entries that are seen (with one)
+
+  // Rows `first` .. of a stream that has `rows`: those behind the last are given its values and not stored.
+  __device__ __forceinline__ void load(const PagedAttnArgs& a, int b, int hk, int m, int past, int64_t first, int64_t rows, int c, int g) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int64_t row = min(first + r * 16 + c, rows - 1);
+      const int t = (int)(row / a.group), h = hk * a.group + (int)(row - (int64_t)t * a.group);
+      limit[r] = past + t + 1;
+      bits[r] = 0;
+      if (a.tree) bits[r] = a.tree[(int64_t)b * a.T + t] & (m == 64 ? ~0ull : (1ull << m) - 1);
+      const T* from = (const T*)a.q + ((int64_t)b * a.T + t) * a.q_stride + (int64_t)h * a.pool.d_h;
+      if constexpr (Y::F32) {
+#pragma unroll
+        for (int f = 0; f < 2 * NB; ++f) {
+          float x[4];
+          load_query4<T>(from, operand_element<KV, NB>(f, g), a.pool.d_h, a.q_pieces, x);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) w[r][4 * f + e] = __float_as_uint(x[e]);
+        }
+      } else {
+#pragma unroll
+        for (int f = 0; f < NB; ++f)
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            float x[4];
+            load_query4<T>(from, operand_element<KV, NB>(f, g) + 4 * half, a.pool.d_h, a.q_pieces, x);
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+              float u = x[e], v = x[e + 1];
+#pragma unroll
+              for (int part = 0; part < Y::Q_PARTS; ++part) {
+                w[r][(part * NB + f) * 4 + half * 2 + e / 2] = high_halves(u, v);
+                u -= high_part(u);
+                v -= high_part(v);
+              }
+            }
+          }
+      }
+    }
+  }
+  __device__ __forceinline__ bool visible(const PagedAttnArgs& a, int r, int entry, int past) const {
+    if (!a.tree) return entry < limit[r];
+    return entry < past || ((bits[r] >> ((unsigned)(entry - past) & 63u)) & 1u) != 0;
+  }
+  // Which of the lane's eight entries of a step (4 g .. + 3 of tiles at base and base + 16) row tile r sees: bits.
+  __device__ __forceinline__ uint32_t seen(const PagedAttnArgs& a, int r, int base, int g, int n, int past, const bool (&there)[2]) const {
+    uint32_t s = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int entry = base + (i / 4) * 16 + 4 * g + i % 4;
+      if (entry < n && there[i / 4] && visible(a, r, entry, past)) s |= 1u << i;
+    }
+    return s;
+  }
+  __device__ __forceinline__ bf16x8_t operand(int r, int part, int f) const {
+    const uint32_t* x = w[r] + (part * NB + f) * 4;
+    return as_bf16x8(uint4_t{x[0], x[1], x[2], x[3]});
+  }
+};
+
+// Score products are used behind a branch, where this compiler (clang 22 of ROCm 7.2) does not keep the distance that a matrix
+// instruction's result needs on the path that skips the branch's body: entries 4 g + 3 of a step were read too early.  The distance, 19
+// instructions for the longest product here, is kept by hand: results pass through this before anything reads them.
+template <int R> __device__ __forceinline__ void settle(f32x4_t (&d)[R][2]) {
+  if constexpr (R == 1) asm volatile("s_nop 15\n\ts_nop 3" : "+v"(d[0][0]), "+v"(d[0][1]));
+  else asm volatile("s_nop 15\n\ts_nop 3" : "+v"(d[0][0]), "+v"(d[0][1]), "+v"(d[1][0]), "+v"(d[1][1]));
+}
+// The same behind a loop whose last products the code after it reads.
+__device__ __forceinline__ void settle_all() { asm volatile("s_nop 15\n\ts_nop 3" ::: "memory"); }
+
+// Weights of a lane's eight scores d of one row: p = 2^(d scale - top), 0 where PARTIAL and `seen` has no bit.  Whether a score exceeds
+// the reference too far is told by the sum, so that the ordinary step has no comparisons; then the reference becomes the row's
+// maximum, and what was summed shrinks.  d * scale - top is one fused operation while references are below 2^20, whose rounding the
+// row's weights share as a factor near 1; beyond (`far`) the product is rounded as the reference was.
+template <bool PARTIAL, int TILES>
+__device__ __forceinline__ void paged_weights(const f32x4_t (&d)[2], float scale, uint32_t seen, bool& far, float& top, float& sum,
+                                              f32x4_t (&acc)[TILES], float (&p)[8]) {
+  auto weigh = [&]() {
+    if (far) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = rounded_product(d[i / 4][i % 4], scale) - top;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = fmaf(d[i / 4][i % 4], scale, -top);
+    }
+    if constexpr (PARTIAL) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[i] = (seen >> i) & 1u ? p[i] : -INFINITY;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = fast_exp2(p[i]);
+    return ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+  };
+  float s = weigh();
+  if (__builtin_amdgcn_ballot_w64(s > PAGED_RAISE) != 0) {
+    float highest = PAGED_LOWEST;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (!PARTIAL || ((seen >> i) & 1u)) highest = fmaxf(highest, rounded_product(d[i / 4][i % 4], scale));
+    const float higher = fmaxf(top, over_row(highest, [](float x, float y) { return fmaxf(x, y); }));
+    const float shrink = fast_exp2(top - higher);
+    top = higher;
+    sum *= shrink;
+#pragma unroll
+    for (int j = 0; j < TILES; ++j) acc[j] *= shrink;
+    far = far || __builtin_amdgcn_ballot_w64(fabsf(higher) > 0x1p20f && higher != PAGED_LOWEST) != 0;
+    s = weigh();
+  }
+  sum += s;
 }
 
 // R row tiles a wave, RW waves side by side over rows; the other PAGED_WAVES / RW deal the steps among themselves.
@@ -210,16 +401,8 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
   const int kw = wave % KW, rw = wave / KW;
 
-  // The workgroups of a stream's row groups read the same entries: they are given numbers that are equal modulo 8, one die's, in turn.
-  int unit = blockIdx.x, row_group = 0;
-  if (a.row_groups > 1) {
-    const int y = blockIdx.x >> 3;
-    row_group = y % a.row_groups;
-    unit = (y / a.row_groups) * 8 + (blockIdx.x & 7);
-    if (unit >= a.units) return;
-  }
-  const int hk = unit % a.pool.H_kv, split = unit / a.pool.H_kv % a.n_splits, b = unit / a.pool.H_kv / a.n_splits;
-
+  int row_group, hk, split, b;
+  if (!paged_unit(a, row_group, hk, split, b)) return;
   int n, m, past;
   paged_sequence(a, b, n, m, past);
   const int64_t rows = (int64_t)m * a.group;
@@ -231,52 +414,11 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
   const int s0 = (int)((int64_t)steps * split / a.n_splits), s1 = (int)((int64_t)steps * (split + 1) / a.n_splits);
   const int all_see = a.tree ? past : past + (int)(min(first, rows - 1) / a.group) + 1;    // entries that every row of the wave sees
 
-  // Rows: those behind the last are given its values and not stored.
-  uint32_t qw[R][Y::Q_WORDS];
-  int limit[R];
-  uint64_t bits[R];
-#pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const int64_t row = min(first + r * 16 + c, rows - 1);
-    const int t = (int)(row / a.group), h = hk * a.group + (int)(row - (int64_t)t * a.group);
-    limit[r] = past + t + 1;
-    bits[r] = 0;
-    if (a.tree) bits[r] = a.tree[(int64_t)b * a.T + t] & (m == 64 ? ~0ull : (1ull << m) - 1);
-    const T* from = (const T*)a.q + ((int64_t)b * a.T + t) * a.q_stride + (int64_t)h * a.pool.d_h;
-    if constexpr (Y::F32) {
-#pragma unroll
-      for (int f = 0; f < 2 * NB; ++f) {
-        float x[4];
-        load_query4<T>(from, operand_element<KV, NB>(f, g), a.pool.d_h, a.q_pieces, x);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) qw[r][4 * f + e] = __float_as_uint(x[e]);
-      }
-    } else {
-#pragma unroll
-      for (int f = 0; f < NB; ++f)
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          float x[4];
-          load_query4<T>(from, operand_element<KV, NB>(f, g) + 4 * half, a.pool.d_h, a.q_pieces, x);
-#pragma unroll
-          for (int e = 0; e < 4; e += 2) {
-            float u = x[e], v = x[e + 1];
-#pragma unroll
-            for (int part = 0; part < Y::Q_PARTS; ++part) {
-              qw[r][(part * NB + f) * 4 + half * 2 + e / 2] = high_halves(u, v);
-              u -= high_part(u);
-              v -= high_part(v);
-            }
-          }
-        }
-    }
-  }
-  auto visible = [&](int r, int entry) {
-    if (!a.tree) return entry < limit[r];
-    return entry < past || ((bits[r] >> ((unsigned)(entry - past) & 63u)) & 1u) != 0;
-  };
+  PagedRows<KV, T, NB, R> q;
+  q.load(a, b, hk, m, past, first, rows, c, g);
 
   float top[R], sum[R];
+  bool far = false;
   f32x4_t acc[R][TILES];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
@@ -286,17 +428,9 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
     for (int j = 0; j < TILES; ++j) acc[r][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
 
-  // Where 16 entries from `entry` on lie; < 0: nowhere (behind the last, or a page outside the pool)
   const int32_t* table = a.pool.table + (int64_t)b * a.pool.max_pages;
-  auto place = [&](int entry) -> int64_t {
-    if (entry >= n) return -1;
-    const int page = table[entry >> a.pool.page_shift];
-    if (page < 0 || page >= a.pool.n_pages) {
-      if (a.status && lane == 0) atomicOr(a.status, (int)PHOTON_STATUS_BAD_PAGE);
-      return -1;
-    }
-    return page * a.pool.page_bytes + hk * a.pool.head_bytes + (int64_t)((entry & ((1 << a.pool.page_shift) - 1)) * a.pool.row_bytes);
-  };
+  bool bad = false;
+  auto place = [&](int entry) { return paged_place(a, table, hk, entry, n, bad); };
   const int k_lane = c * a.pool.row_bytes, v_lane = 4 * g * a.pool.row_bytes + c * Y::V_BYTES;
   uint32_t kx[2][Y::K_WORDS], vx[8][Y::V_WORDS];
   auto load_k = [&](const int64_t (&at)[2]) {                                      // from nowhere: the pool's first entries, in bounds, not used
@@ -317,26 +451,27 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
     load_k(at);
     load_v(at);
   }
-#pragma unroll 1
-  while (has_rows && step < s1) {
+  // One step; the next one's entries are requested as soon as their registers are free.  PARTIAL: not every row sees every entry of it.
+  auto take = [&](auto partial) {
+    constexpr bool PARTIAL = decltype(partial)::value;
+    const bool there[2] = {at[0] >= 0, at[1] >= 0};
     const int base = step * PAGED_STEP, next = step + KW;
     int64_t next_at[2] = {-1, -1};
     if (next < s1) {
       next_at[0] = place(next * PAGED_STEP);
       next_at[1] = place(next * PAGED_STEP + 16);
     }
-    float s[R][8];
+    f32x4_t d[R][2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      f32x4_t d[R];
 #pragma unroll
-      for (int r = 0; r < R; ++r) d[r] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int r = 0; r < R; ++r) d[r][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
       if constexpr (Y::F32) {
 #pragma unroll
         for (int f = 0; f < 8 * NB; ++f)
 #pragma unroll
           for (int r = 0; r < R; ++r)
-            d[r] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kx[i][f]), __uint_as_float(qw[r][f]), d[r], 0, 0, 0);
+            d[r][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kx[i][f]), __uint_as_float(q.w[r][f]), d[r][i], 0, 0, 0);
       } else {
 #pragma unroll
         for (int f = 0; f < NB; ++f) {
@@ -344,87 +479,49 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
 #pragma unroll
           for (int part = Y::Q_PARTS - 1; part >= 0; --part)
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-              const uint32_t* w = qw[r] + (part * NB + f) * 4;
-              d[r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, as_bf16x8(uint4_t{w[0], w[1], w[2], w[3]}), d[r], 0, 0, 0);
-            }
+            for (int r = 0; r < R; ++r) d[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q.operand(r, part, f), d[r][i], 0, 0, 0);
         }
       }
-#pragma unroll
-      for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[r][4 * i + e] = rounded_product(d[r][e], a.scale_log2e);
     }
+    settle(d);
     if (next < s1) load_k(next_at);
 
-    const bool partial = base + PAGED_STEP > all_see || at[0] < 0 || at[1] < 0;
-    if (partial) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int entry = base + (i / 4) * 16 + 4 * g + i % 4;
-        const bool there = entry < n && at[i / 4] >= 0;
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-          if (!there || !visible(r, entry)) s[r][i] = -INFINITY;
-      }
-    }
-    // weights
+    float s[R][8];
+    uint32_t seen[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      float highest = s[r][0];
-#pragma unroll
-      for (int i = 1; i < 8; ++i) highest = fmaxf(highest, s[r][i]);
-      if (__builtin_amdgcn_ballot_w64(highest - top[r] > PAGED_RAISE) != 0) {
-        const float higher = fmaxf(top[r], over_row(highest, [](float x, float y) { return fmaxf(x, y); }));
-        const float shrink = fast_exp2(top[r] - higher);
-        top[r] = higher;
-        sum[r] *= shrink;
-#pragma unroll
-        for (int j = 0; j < TILES; ++j) acc[r][j] *= shrink;
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        s[r][i] = fast_exp2(s[r][i] - top[r]);
-        sum[r] += s[r][i];
-      }
+      seen[r] = PARTIAL ? q.seen(a, r, base, g, n, past, there) : 0u;
+      paged_weights<PARTIAL>(d[r], a.scale_log2e, seen[r], far, top[r], sum[r], acc[r], s[r]);
     }
-    if (partial) {
+    bool some = false;                                                      // an infinity or NaN that some row sees
+    if constexpr (PARTIAL) {
       // Entries that no row sees may hold anything: zeros.
-      uint32_t unbounded = 0;
+      bool unbounded = false;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const bool there = base + (i / 4) * 16 + 4 * g + i % 4 < n && at[i / 4] >= 0;
+        const bool used = base + (i / 4) * 16 + 4 * g + i % 4 < n && there[i / 4];
 #pragma unroll
         for (int w = 0; w < Y::V_WORDS; ++w) {
-          vx[i][w] = there ? vx[i][w] : 0u;
-          if (without_unbounded<KV>(vx[i][w]) != vx[i][w]) unbounded |= 1u << i;
+          vx[i][w] = used ? vx[i][w] : 0u;
+          unbounded = unbounded || without_unbounded<KV>(vx[i][w]) != vx[i][w];
         }
       }
-      // What one row sees and another does not may be an infinity or NaN, too: 0 times it is not 0, so these are added row by row.
-      if (m > 1 && __builtin_amdgcn_ballot_w64(unbounded != 0) != 0) {
+      some = m > 1 && __builtin_amdgcn_ballot_w64(unbounded) != 0;
+    }
+    if constexpr (Y::F32 && PARTIAL) {
+      if (some) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint64_t lanes = __builtin_amdgcn_ballot_w64((unbounded >> i) & 1u);
-#pragma unroll 1
-          for (int other = 0; other < 4; ++other) {
-            if (((lanes >> (16 * other)) & 0xffffu) == 0) continue;
-            const int entry = base + (i / 4) * 16 + 4 * other + i % 4;
-            const uint8_t* row = a.pool.v + at[i / 4] + (4 * other + i % 4) * a.pool.row_bytes;
+        for (int j = 0; j < TILES; ++j) {
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-              const float p = __shfl(s[r][i], 16 * other + c);
-              if (!visible(r, entry)) continue;
+          for (int r = 0; r < R; ++r) {
+            f32x4_t digits = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int j = 0; j < TILES; ++j) {
-                  const float x = element<KV>(row, TILES * (4 * g + e) + j);
-                  if (!(fabsf(x) <= FLT_MAX)) acc[r][j][e] += p * x;
-                }
-            }
+            for (int i = 0; i < 8; ++i)
+              digits = __builtin_amdgcn_mfma_f32_16x16x4f32(unbounded_code(__uint_as_float(vx[i][j])), (seen[r] >> i) & 1u ? 1.f : 0.f, digits, 0, 0, 0);
+            add_unbounded(acc[r][j], digits);
           }
 #pragma unroll
-          for (int w = 0; w < Y::V_WORDS; ++w) vx[i][w] = without_unbounded<KV>(vx[i][w]);
+          for (int i = 0; i < 8; ++i) vx[i][j] = without_unbounded<KV>(vx[i][j]);
         }
       }
     }
@@ -457,39 +554,39 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
       }
 #pragma unroll
       for (int j = 0; j < TILES; ++j) {
-        const bf16x8_t value = value_operand<KV, Y::V_WORDS>(vx, j);
+        uint4_t value = value_operand<KV, Y::V_WORDS>(vx, j);
+        if constexpr (PARTIAL) {
+          if (some) {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+              add_unbounded(acc[r][j], __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(unbounded_codes(value)), as_bf16x8(seen_operand(seen[r])),
+                                                                               f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) value[i] = without_unbounded<bf16_t>(value[i]);
+          }
+        }
 #pragma unroll
         for (int part = Y::P_PARTS - 1; part >= 0; --part)
 #pragma unroll
-          for (int r = 0; r < R; ++r) acc[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value, p[r][part], acc[r][j], 0, 0, 0);
+          for (int r = 0; r < R; ++r) acc[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(value), p[r][part], acc[r][j], 0, 0, 0);
       }
     }
     if (next < s1) load_v(next_at);
     at[0] = next_at[0];
     at[1] = next_at[1];
     step = next;
-  }
+  };
+  // Steps that every row sees whole come first; from the first other one on, all are taken with care.  Code of both in one loop would
+  // cost the ordinary steps their registers.
+#pragma unroll 1
+  while (has_rows && step < s1 && (step + 1) * PAGED_STEP <= all_see && at[0] >= 0 && at[1] >= 0) take(std::false_type{});
+#pragma unroll 1
+  while (has_rows && step < s1) take(std::true_type{});
+  settle_all();
+  paged_say(a, bad, lane);
 
   // Results: lane (c, g) holds elements 8 NB g .. + 8 NB - 1 of its rows.  Each wave divides by its sum, and waves are put together as
   // weighted means: no sum of values leaves the range that a wave's own is in.
-  const auto to_row = [&](int64_t row) {                                            // row of out
-    const int64_t t = row / a.group;
-    return ((int64_t)b * a.T + t) * a.H + hk * a.group + (row - t * a.group);
-  };
-  const auto emit = [&](int64_t row, int d, const float (&x)[4], float row_top, float row_sum) {
-    const int64_t to = to_row(row);
-    if (a.n_splits == 1) {
-      if (d < a.pool.d_h) store_result4<T>((T*)a.out + to * a.pool.d_h, d, a.pool.d_h, a.out_pieces, x);
-      return;
-    }
-    const int64_t piece = to * a.n_splits + split;
-    *reinterpret_cast<float4_t*>(a.ws + piece * DP + d) = float4_t{x[0], x[1], x[2], x[3]};
-    if (d == 0) {
-      float* st = a.ws + (int64_t)a.Bt * a.T * a.H * a.n_splits * DP + piece * 2;
-      st[0] = row_top;
-      st[1] = row_sum;
-    }
-  };
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const float l = over_row(sum[r], [](float x, float y) { return x + y; });
@@ -502,7 +599,7 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
           float o[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[e] = acc[r][(x + e) % TILES][(x + e) / TILES] * mean;
-          emit(row, 8 * NB * g + x, o, top[r], l);
+          paged_emit<T, DP>(a, paged_row(a, b, hk, row), split, 8 * NB * g + x, o, top[r], l);
         }
       }
     } else {
@@ -538,7 +635,7 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[e] = fmaf(y[e], weight[w] * inverse, o[e]);
         }
-        emit(to, d, o, w_top, w_sum);
+        paged_emit<T, DP>(a, paged_row(a, b, hk, to), split, d, o, w_top, w_sum);
       }
     }
   }
@@ -575,17 +672,16 @@ template <typename KV, typename T, int NB, int R, int RW> int32_t paged_launch(c
   PHOTON_LAUNCH(KC_COARSE_ATTN, st, (paged_attn_kernel<KV, T, NB, R, RW>), dim3(grid), dim3(PAGED_WAVES * 64), 0, st, a);
   return check_launch("paged_attn_kernel");
 }
-template <typename KV, typename T, int NB> int32_t paged_launch_rows(const PagedAttnArgs& a, hipStream_t st) {
-  const PagedTile tile = paged_tile((int64_t)a.T * a.group);
+template <typename KV, typename T, int NB> int32_t paged_launch_rows(const PagedAttnArgs& a, const PagedTile& tile, hipStream_t st) {
   if (tile.tiles == 1) return paged_launch<KV, T, NB, 1, 1>(a, st);
   if (tile.waves == 1) return paged_launch<KV, T, NB, 2, 1>(a, st);
   if (tile.waves == 2) return paged_launch<KV, T, NB, 2, 2>(a, st);
   return paged_launch<KV, T, NB, 2, 4>(a, st);
 }
-template <typename KV> int32_t paged_launch_types(const PagedAttnArgs& a, bool f32_rows, hipStream_t st) {
+template <typename KV> int32_t paged_launch_types(const PagedAttnArgs& a, const PagedTile& tile, bool f32_rows, hipStream_t st) {
   const int nb = kv_row_elems(a.pool.d_h) / 32;
-  if (f32_rows) return nb == 1 ? paged_launch_rows<KV, float, 1>(a, st) : nb == 2 ? paged_launch_rows<KV, float, 2>(a, st) : paged_launch_rows<KV, float, 4>(a, st);
-  return nb == 1 ? paged_launch_rows<KV, bf16_t, 1>(a, st) : nb == 2 ? paged_launch_rows<KV, bf16_t, 2>(a, st) : paged_launch_rows<KV, bf16_t, 4>(a, st);
+  if (f32_rows) return nb == 1 ? paged_launch_rows<KV, float, 1>(a, tile, st) : nb == 2 ? paged_launch_rows<KV, float, 2>(a, tile, st) : paged_launch_rows<KV, float, 4>(a, tile, st);
+  return nb == 1 ? paged_launch_rows<KV, bf16_t, 1>(a, tile, st) : nb == 2 ? paged_launch_rows<KV, bf16_t, 2>(a, tile, st) : paged_launch_rows<KV, bf16_t, 4>(a, tile, st);
 }
 
 }  // namespace photon

@@ -5,15 +5,19 @@ namespace photon {
 namespace {
 
 // Workgroups over the entries of a stream, and the fewest steps that are worth one.
-int paged_auto_splits(int Bt, int T, int H, int H_kv, int64_t S_max) {
+int paged_auto_splits(int Bt, int T, int H, int H_kv, int64_t S_max, bool f32_rows, photon_dtype kv_dt) {
   const int64_t rows = (int64_t)T * (H / H_kv);
-  const PagedTile tile = paged_tile(rows);
-  const int64_t per = 16 * tile.tiles * tile.waves, groups = (int64_t)Bt * H_kv * ((rows + per - 1) / per);
+  const PagedTile tile = paged_tile(rows, f32_rows, kv_dt);
+  const int64_t groups = (int64_t)Bt * H_kv * ((rows + tile.rows() - 1) / tile.rows());
   const int64_t steps = (S_max + PAGED_STEP - 1) / PAGED_STEP;
   int64_t splits = 512 / groups;
-  const int64_t most = steps * tile.waves / (4 * PAGED_WAVES);
+  const int64_t most = tile.wide ? steps / 8 : steps * tile.waves / (4 * PAGED_WAVES);
   splits = splits > most ? most : splits;
   return (int)(splits < 1 ? 1 : splits > 256 ? 256 : splits);
+}
+int paged_most_splits(const photon_paged_cache* c, int Bt, int T, int H, int64_t S_max) {   // of either dtype of rows
+  const int a = paged_auto_splits(Bt, T, H, c->H_kv, S_max, false, c->kv_dt), b = paged_auto_splits(Bt, T, H, c->H_kv, S_max, true, c->kv_dt);
+  return a > b ? a : b;
 }
 
 template <typename T, int NB> int32_t launch_merge(const PagedAttnArgs& a, hipStream_t st) {
@@ -50,7 +54,7 @@ using namespace photon;
 
 extern "C" size_t photon_paged_attn_workspace_bytes(const photon_paged_cache* cache, int32_t Bt, int32_t T, int32_t H, int64_t S_max, int32_t n_splits) {
   if (cache == nullptr || cache->H_kv <= 0 || Bt <= 0 || T <= 0 || H < cache->H_kv || S_max <= 0 || kv_row_elems(cache->d_h) == 0) return 0;
-  return workspace_bytes_of(cache, Bt, T, H, n_splits == 0 ? paged_auto_splits(Bt, T, H, cache->H_kv, S_max) : n_splits);
+  return workspace_bytes_of(cache, Bt, T, H, n_splits == 0 ? paged_most_splits(cache, Bt, T, H, S_max) : n_splits);
 }
 
 extern "C" int32_t photon_paged_attn(const photon_paged_cache* cache, const void* q, int64_t q_stride, const int32_t* seq_len, const int32_t* n_new,
@@ -68,7 +72,8 @@ extern "C" int32_t photon_paged_attn(const photon_paged_cache* cache, const void
   PHOTON_REQUIRE(q && out && element_aligned(q, esz) && element_aligned(out, esz), PHOTON_ERR_INVALID_ARG, "%s: q and out must be non-null device pointers to whole elements", __func__);
   PHOTON_REQUIRE(seq_len != nullptr, PHOTON_ERR_INVALID_ARG, "%s: seq_len is null", __func__);
   PHOTON_REQUIRE(q_stride >= (int64_t)H * d_h, PHOTON_ERR_INVALID_ARG, "%s: q_stride=%lld is less than a row of %d heads of %d", __func__, (long long)q_stride, H, d_h);
-  if (n_splits == 0) n_splits = paged_auto_splits(Bt, T, H, cache->H_kv, S_max);
+  const bool f32 = dt == PHOTON_F32;
+  if (n_splits == 0) n_splits = paged_auto_splits(Bt, T, H, cache->H_kv, S_max, f32, cache->kv_dt);
   if (n_splits > 1) {
     const size_t need = workspace_bytes_of(cache, Bt, T, H, n_splits);
     PHOTON_REQUIRE(workspace != nullptr && aligned16(workspace) && workspace_bytes >= need, PHOTON_ERR_WORKSPACE,
@@ -78,20 +83,19 @@ extern "C" int32_t photon_paged_attn(const photon_paged_cache* cache, const void
   a.seq_len = seq_len; a.n_new = n_new; a.tree = tree; a.status = status;
   a.q_stride = q_stride; a.S_max = (int32_t)S_max; a.Bt = Bt; a.T = T; a.H = H; a.group = H / cache->H_kv; a.n_splits = n_splits;
   const int64_t rows = (int64_t)T * a.group;
-  const PagedTile tile = paged_tile(rows);
-  const int64_t per = 16 * tile.tiles * tile.waves, groups = (rows + per - 1) / per, units = (int64_t)Bt * cache->H_kv * n_splits;
-  PHOTON_REQUIRE((units + 7) * groups <= (int64_t)0xffffffff / (PAGED_WAVES * 64), PHOTON_ERR_UNSUPPORTED,
+  const PagedTile tile = paged_tile(rows, f32, cache->kv_dt);
+  const int64_t groups = (rows + tile.rows() - 1) / tile.rows(), units = (int64_t)Bt * cache->H_kv * n_splits;
+  PHOTON_REQUIRE((units + 7) * groups <= (int64_t)0xffffffff / 512, PHOTON_ERR_UNSUPPORTED,
                  "%s: Bt=%d, T=%d, H=%d, n_splits=%d are too many workgroups", __func__, Bt, T, H, n_splits);
   a.row_groups = (int32_t)groups; a.units = (int32_t)units;
   a.scale_log2e = scale * LOG2E;
   a.q_pieces = d_h % 4 == 0 && q_stride % 4 == 0 && element_aligned(q, 4 * esz);
   a.out_pieces = d_h % 4 == 0 && element_aligned(out, 4 * esz);
-  const bool f32 = dt == PHOTON_F32;
   hipStream_t st = (hipStream_t)stream;
   switch (cache->kv_dt) {
-    case PHOTON_F32: PHOTON_TRY(paged_attn_f32(a, f32, st)); break;
-    case PHOTON_BF16: PHOTON_TRY(paged_attn_bf16(a, f32, st)); break;
-    default: PHOTON_TRY(paged_attn_e4m3(a, f32, st)); break;
+    case PHOTON_F32: PHOTON_TRY(paged_attn_f32(a, tile, f32, st)); break;
+    case PHOTON_BF16: PHOTON_TRY(paged_attn_bf16(a, tile, f32, st)); break;
+    default: PHOTON_TRY(paged_attn_e4m3(a, tile, f32, st)); break;
   }
   if (n_splits == 1) return PHOTON_OK;
   return f32 ? launch_merge_t<float>(a, st) : launch_merge_t<bf16_t>(a, st);

@@ -3,6 +3,8 @@
 
 namespace photon {
 
-int32_t paged_attn_e4m3(const PagedAttnArgs& a, bool f32_rows, hipStream_t st) { return paged_launch_types<fp8_t>(a, f32_rows, st); }
+int32_t paged_attn_e4m3(const PagedAttnArgs& a, const PagedTile& tile, bool f32_rows, hipStream_t st) {
+  return paged_launch_types<fp8_t>(a, tile, f32_rows, st);
+}
 
 }  // namespace photon

@@ -1,0 +1,237 @@
+// Attention over a paged K/V cache of many rows that share a K/V head (trees, pieces of a prompt): bf16 rows, bf16 pages.
+//
+// The mathematics is photon_paged_attn.h's.  With 16 rows and more to a wave the matrix cores and the softmax bound it, not the entries:
+// a workgroup of WAVES waves of 32 rows stages 64 entries of K and V at a time in LDS (two buffers, loads straight to LDS while the
+// other buffer is worked on, one barrier per stage), so that entries are read once for all its rows.
+//   K     16-byte chunks of a row are permuted by row, so that the 16 rows of an operand lie in different banks
+//   V     pairs of chunks likewise; ds_read_b64_tr_b16 hands a lane four entries of one element, as the contraction over entries takes
+//         them: the interleaving of the register kernel is the LDS's work here
+#pragma once
+#include "photon_paged_attn.h"
+
+namespace photon {
+
+constexpr int WIDE_STAGE = 64;                 // entries of a stage
+constexpr int WIDE_TILES = 2;                  // row tiles of a wave
+
+typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) short4_t* lds_short4_t;
+
+// Every load and LDS access of this wave is complete, and every wave of the workgroup is here.
+__device__ __forceinline__ void wide_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+template <int NB, int WAVES> __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_wide_kernel(PagedAttnArgs a) {
+  using Y = PagedTypes<bf16_t, bf16_t, NB>;
+  constexpr int DP = Y::DP, TILES = Y::TILES, R = WIDE_TILES, ROW = 2 * DP, CHUNKS = ROW / 16;
+  constexpr int LOADS = WIDE_STAGE * ROW / 1024, ROWS_LOAD = 1024 / ROW, PER = 2 * LOADS / WAVES;   // loads of a matrix; rows of one; a wave's, of both
+  extern __shared__ __align__(16) char wide_lds[];                           // [2 buffers][K, V][64][ROW]
+  const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)wide_lds));
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
+
+  int row_group, hk, split, b;
+  if (!paged_unit(a, row_group, hk, split, b)) return;
+  int n, m, past;
+  paged_sequence(a, b, n, m, past);
+  const int64_t rows = (int64_t)m * a.group;
+  const int64_t group_first = (int64_t)row_group * (WAVES * R * 16), first = group_first + wave * (R * 16);
+  if (group_first >= rows) return;
+  const int64_t group_last = min(group_first + WAVES * R * 16, rows) - 1, last = min(first + R * 16, rows) - 1;
+  const int hi = a.tree ? n : min(n, past + (int)(group_last / a.group) + 1);
+  const int stages = hi <= 0 ? 0 : (hi + WIDE_STAGE - 1) / WIDE_STAGE;
+  const int s0 = (int)((int64_t)stages * split / a.n_splits), s1 = (int)((int64_t)stages * (split + 1) / a.n_splits);
+  const bool has_rows = first < rows;
+  const int wave_hi = !has_rows ? 0 : a.tree ? n : min(n, past + (int)(last / a.group) + 1);
+
+  PagedRows<bf16_t, bf16_t, NB, R> q;
+  q.load(a, b, hk, m, past, first, rows, c, g);
+  float top[R], sum[R];
+  bool far = false;
+  f32x4_t acc[R][TILES];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    top[r] = PAGED_LOWEST;
+    sum[r] = 0.f;
+#pragma unroll
+    for (int j = 0; j < TILES; ++j) acc[r][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // A row's 16-byte chunk i lies at chunk i ^ k_turn(row) of the row (K), i ^ v_turn(row) (V).
+  auto k_turn = [](int row) { return (row * NB / 4) & (CHUNKS - 1); };
+  auto v_turn = [](int row) { return ((row * NB / 4) & (CHUNKS / 2 - 1)) * 2; };
+  const int32_t* table = a.pool.table + (int64_t)b * a.pool.max_pages;
+  bool bad_page = false;
+  struct Places { int64_t at[4]; };                                          // of a stage's tiles of 16 entries
+  auto places = [&](int stage) {
+    Places p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p.at[i] = paged_place(a, table, hk, stage * WIDE_STAGE + 16 * i, n, bad_page);
+    return p;
+  };
+  // Load u of this wave is load (wave + WAVES u) of the stage: ROWS_LOAD rows, one tile's; from nowhere: the pool's first entries.
+  int from[PER];
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int i = wave + WAVES * u, row = i % LOADS * ROWS_LOAD + lane / CHUNKS, chunk = lane % CHUNKS;
+    from[u] = row % 16 * ROW + (chunk ^ (i < LOADS ? k_turn(row) : v_turn(row))) * 16;
+  }
+  auto stage_in = [&](const Places& p, int buffer) {
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      const int i = wave + WAVES * u, tile = i % LOADS * ROWS_LOAD / 16;
+      const int64_t at = tile == 0 ? p.at[0] : tile == 1 ? p.at[1] : tile == 2 ? p.at[2] : p.at[3];
+      load16_to_lds((i < LOADS ? a.pool.k : a.pool.v) + (at < 0 ? 0 : at) + from[u], lds + buffer * (2 * WIDE_STAGE * ROW) + i * 1024);
+    }
+  };
+  // LDS places of this lane's operands, of the first tile
+  int k_at[NB], v_at[TILES];
+#pragma unroll
+  for (int f = 0; f < NB; ++f) k_at[f] = c * ROW + ((4 * f + g) ^ k_turn(c)) * 16;
+#pragma unroll
+  for (int j = 0; j < TILES; ++j) {
+    const int row = 4 * g + (c >> 2);
+    v_at[j] = WIDE_STAGE * ROW + row * ROW + ((2 * j + ((c & 3) >> 1)) ^ v_turn(row)) * 16 + (c & 1) * 8;
+  }
+
+  // One step: `in` is where its K begins.  PARTIAL: not every row sees every entry of it.
+  auto take = [&](auto partial, const char* in, int base, const Places& now, int half) {
+    constexpr bool PARTIAL = decltype(partial)::value;
+    const bool there[2] = {(half ? now.at[2] : now.at[0]) >= 0, (half ? now.at[3] : now.at[1]) >= 0};
+    f32x4_t d[R][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) d[r][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int f = 0; f < NB; ++f) {
+        const bf16x8_t key = as_bf16x8(*reinterpret_cast<const uint4_t*>(in + i * 16 * ROW + k_at[f]));
+#pragma unroll
+        for (int r = 0; r < R; ++r) d[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q.operand(r, 0, f), d[r][i], 0, 0, 0);
+      }
+    }
+    settle(d);
+    float s[R][8];
+    uint32_t seen[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      seen[r] = PARTIAL ? q.seen(a, r, base, g, n, past, there) : 0u;
+      paged_weights<PARTIAL>(d[r], a.scale_log2e, seen[r], far, top[r], sum[r], acc[r], s[r]);
+    }
+    uint4_t keep = {~0u, ~0u, ~0u, ~0u};                                   // of a lane's eight entries
+    bool some = false;                                                   // an infinity or NaN that some row sees
+    if constexpr (PARTIAL) {
+      // Entries that no row sees may hold anything: zeros.
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int entry = base + i / 2 * 16 + 4 * g + i % 2 * 2;
+        keep[i] = (entry < n && there[i / 2] ? 0xffffu : 0u) | (entry + 1 < n && there[i / 2] ? 0xffff0000u : 0u);
+      }
+      if (m > 1) {
+        const int mine = lane / 2;                                         // entry of the step that this lane looks at, half of its row
+        const bool used = base + mine < n && (mine < 16 ? there[0] : there[1]);
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < CHUNKS / 2; ++i) {
+          const uint4_t x = *reinterpret_cast<const uint4_t*>(in + WIDE_STAGE * ROW + mine * ROW + (lane % 2 * (CHUNKS / 2) + i) * 16);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) bad = bad || without_unbounded<bf16_t>(x[e]) != x[e];
+        }
+        some = __builtin_amdgcn_ballot_w64(bad && used) != 0;
+      }
+    }
+    bf16x8_t p[R][2];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      uint4_t high, low;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = s[r][2 * i], y = s[r][2 * i + 1];
+        high[i] = high_halves(x, y);
+        low[i] = pack_bf16x2(x - high_part(x), y - high_part(y));
+      }
+      p[r][0] = as_bf16x8(high);
+      p[r][1] = as_bf16x8(low);
+    }
+#pragma unroll
+    for (int j = 0; j < TILES; ++j) {
+      uint4_t value;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const short4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t)(in + i * 16 * ROW + v_at[j]));
+        const uint2v_t w = __builtin_bit_cast(uint2v_t, x);
+        value[2 * i] = w[0];
+        value[2 * i + 1] = w[1];
+      }
+      if constexpr (PARTIAL) {
+        __builtin_amdgcn_sched_barrier(0);                               // rare code: few registers rather than overlap
+        value &= keep;
+        if (some) {
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+            add_unbounded(acc[r][j], __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(unbounded_codes(value)), as_bf16x8(seen_operand(seen[r])),
+                                                                             f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) value[i] = without_unbounded<bf16_t>(value[i]);
+        }
+      }
+#pragma unroll
+      for (int part = 1; part >= 0; --part)
+#pragma unroll
+        for (int r = 0; r < R; ++r) acc[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(value), p[r][part], acc[r][j], 0, 0, 0);
+    }
+  };
+
+  // Stages that every row of the workgroup sees whole come first; from the first other one on, all steps are taken with care.  Code of
+  // both in one loop would cost the ordinary steps their registers.
+  const int group_sees = a.tree ? past : past + (int)(group_first / a.group) + 1;
+  Places now = places(s0), next = now;
+  int stage = s0;
+  if (s0 < s1) stage_in(now, 0);
+  auto begin = [&]() -> const char* {                                        // this stage is there, the next one on its way
+    const int buffer = (stage - s0) & 1;
+    if (stage + 1 < s1) next = places(stage + 1);
+    wide_barrier();                                                          // the other buffer is no longer read
+    if (stage + 1 < s1) stage_in(next, buffer ^ 1);
+    return wide_lds + buffer * (2 * WIDE_STAGE * ROW);
+  };
+#pragma unroll 1
+  for (; stage < s1 && (stage + 1) * WIDE_STAGE <= group_sees && now.at[0] >= 0 && now.at[1] >= 0 && now.at[2] >= 0 && now.at[3] >= 0; ++stage, now = next) {
+    const char* in = begin();
+    if (!has_rows) continue;
+#pragma unroll 1
+    for (int half = 0; half < 2; ++half) take(std::false_type{}, in + half * (PAGED_STEP * ROW), stage * WIDE_STAGE + half * PAGED_STEP, now, half);
+  }
+#pragma unroll 1
+  for (; stage < s1; ++stage, now = next) {
+    const char* in = begin();
+#pragma unroll 1
+    for (int half = 0; half < 2; ++half) {
+      const int base = stage * WIDE_STAGE + half * PAGED_STEP;
+      if (base < wave_hi) take(std::true_type{}, in + half * (PAGED_STEP * ROW), base, now, half);
+    }
+  }
+  settle_all();
+  paged_say(a, bad_page, lane);
+
+  // lane (c, g) holds elements 16 j + 4 g .. + 3 of its rows
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const float l = over_row(sum[r], [](float x, float y) { return x + y; });
+    const float mean = l == 0.f ? 0.f : 1.f / l;
+    const int64_t row = first + r * 16 + c;
+    if (row >= rows) continue;
+    const int64_t to = paged_row(a, b, hk, row);
+#pragma unroll
+    for (int j = 0; j < TILES; ++j) {
+      const float o[4] = {acc[r][j][0] * mean, acc[r][j][1] * mean, acc[r][j][2] * mean, acc[r][j][3] * mean};
+      paged_emit<bf16_t, DP>(a, to, split, 16 * j + 4 * g, o, top[r], l);
+    }
+  }
+}
+
+template <int NB, int WAVES> int32_t paged_launch_wide(const PagedAttnArgs& a, hipStream_t st) {
+  const unsigned grid = a.row_groups > 1 ? (unsigned)((a.units + 7) / 8 * 8) * (unsigned)a.row_groups : (unsigned)a.units;
+  PHOTON_LAUNCH(KC_COARSE_ATTN, st, (paged_attn_wide_kernel<NB, WAVES>), dim3(grid), dim3(WAVES * 64), 2 * 2 * WIDE_STAGE * 64 * NB, st, a);
+  return check_launch("paged_attn_wide_kernel");
+}
+
+}  // namespace photon
