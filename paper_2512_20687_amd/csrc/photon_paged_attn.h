@@ -324,11 +324,11 @@ template <typename KV, typename T, int NB, int R> struct PagedRows {
     if (!a.tree) return entry < limit[r];
     return entry < past || ((bits[r] >> ((unsigned)(entry - past) & 63u)) & 1u) != 0;
   }
-  // Which of the lane's eight entries of a step (4 g .. + 3 of tiles at base and base + 16) row tile r sees: bits.
-  __device__ __forceinline__ uint32_t seen(const PagedAttnArgs& a, int r, int base, int g, int n, int past, const bool (&there)[2]) const {
+  // Which of the lane's entries (4 g .. + 3 of the N tiles of 16 from base on) row tile r sees: bits.
+  template <int N> __device__ __forceinline__ uint32_t seen(const PagedAttnArgs& a, int r, int base, int g, int n, int past, const bool (&there)[N]) const {
     uint32_t s = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 4 * N; ++i) {
       const int entry = base + (i / 4) * 16 + 4 * g + i % 4;
       if (entry < n && there[i / 4] && visible(a, r, entry, past)) s |= 1u << i;
     }
@@ -343,52 +343,65 @@ template <typename KV, typename T, int NB, int R> struct PagedRows {
 // Score products are used behind a branch, where this compiler (clang 22 of ROCm 7.2) does not keep the distance that a matrix
 // instruction's result needs on the path that skips the branch's body: entries 4 g + 3 of a step were read too early.  The distance, 19
 // instructions for the longest product here, is kept by hand: results pass through this before anything reads them.
-template <int R> __device__ __forceinline__ void settle(f32x4_t (&d)[R][2]) {
-  if constexpr (R == 1) asm volatile("s_nop 15\n\ts_nop 3" : "+v"(d[0][0]), "+v"(d[0][1]));
-  else asm volatile("s_nop 15\n\ts_nop 3" : "+v"(d[0][0]), "+v"(d[0][1]), "+v"(d[1][0]), "+v"(d[1][1]));
+template <int R, int N> __device__ __forceinline__ void settle(f32x4_t (&d)[R][N]) {
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(d[r][i]));            // volatile: these stay before the distance,
+  asm volatile("s_nop 15\n\ts_nop 3");
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(d[r][i]));            // and these behind it
 }
-// The same behind a loop whose last products the code after it reads.
-__device__ __forceinline__ void settle_all() { asm volatile("s_nop 15\n\ts_nop 3" ::: "memory"); }
 
-// Weights of a lane's eight scores d of one row: p = 2^(d scale - top), 0 where PARTIAL and `seen` has no bit.  Whether a score exceeds
-// the reference too far is told by the sum, so that the ordinary step has no comparisons; then the reference becomes the row's
-// maximum, and what was summed shrinks.  d * scale - top is one fused operation while references are below 2^20, whose rounding the
-// row's weights share as a factor near 1; beyond (`far`) the product is rounded as the reference was.
-template <bool PARTIAL, int TILES>
-__device__ __forceinline__ void paged_weights(const f32x4_t (&d)[2], float scale, uint32_t seen, bool& far, float& top, float& sum,
-                                              f32x4_t (&acc)[TILES], float (&p)[8]) {
+// Weights of a lane's scores d of its rows: p = 2^(d scale - top).  Whether one exceeds the reference too far is told by the sums, so
+// that an ordinary step has no comparisons; then references become the rows' maxima, and what was summed shrinks.  The product with
+// the scale is rounded, as the reference was: fused with the subtraction it would keep digits that the reference lost, which are an
+// exponent of their own once scores pass 2^24.  CAREFUL: 0 where `seen` has no bit.
+template <bool CAREFUL, int R, int N, int TILES>
+__device__ __forceinline__ void paged_weights(const f32x4_t (&d)[R][N], float scale, const uint32_t (&seen)[R], float (&top)[R], float (&sum)[R],
+                                              f32x4_t (&acc)[R][TILES], float (&p)[R][4 * N]) {
+  float s[R];
   auto weigh = [&]() {
-    if (far) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = rounded_product(d[i / 4][i % 4], scale) - top;
-    } else {
+    for (int r = 0; r < R; ++r) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = fmaf(d[i / 4][i % 4], scale, -top);
+      for (int i = 0; i < 4 * N; ++i) p[r][i] = rounded_product(d[r][i / 4][i % 4], scale) - top[r];
+      if constexpr (CAREFUL) {
+#pragma unroll
+        for (int i = 0; i < 4 * N; ++i) p[r][i] = (seen[r] >> i) & 1u ? p[r][i] : -INFINITY;
+      }
+#pragma unroll
+      for (int i = 0; i < 4 * N; ++i) p[r][i] = fast_exp2(p[r][i]);
+      float part[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) part[i] = (p[r][4 * i] + p[r][4 * i + 1]) + (p[r][4 * i + 2] + p[r][4 * i + 3]);
+      s[r] = part[0] + part[1];
+      if constexpr (N == 4) s[r] += part[2] + part[3];
     }
-    if constexpr (PARTIAL) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = (seen >> i) & 1u ? p[i] : -INFINITY;
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) p[i] = fast_exp2(p[i]);
-    return ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
   };
-  float s = weigh();
-  if (__builtin_amdgcn_ballot_w64(s > PAGED_RAISE) != 0) {
-    float highest = PAGED_LOWEST;
+  weigh();
+  bool above = s[0] > PAGED_RAISE;
+  if constexpr (R == 2) above = above || s[1] > PAGED_RAISE;
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(above) != 0, 0)) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (!PARTIAL || ((seen >> i) & 1u)) highest = fmaxf(highest, rounded_product(d[i / 4][i % 4], scale));
-    const float higher = fmaxf(top, over_row(highest, [](float x, float y) { return fmaxf(x, y); }));
-    const float shrink = fast_exp2(top - higher);
-    top = higher;
-    sum *= shrink;
+    for (int r = 0; r < R; ++r) {
+      float highest = PAGED_LOWEST;
 #pragma unroll
-    for (int j = 0; j < TILES; ++j) acc[j] *= shrink;
-    far = far || __builtin_amdgcn_ballot_w64(fabsf(higher) > 0x1p20f && higher != PAGED_LOWEST) != 0;
-    s = weigh();
+      for (int i = 0; i < 4 * N; ++i)
+        if (!CAREFUL || ((seen[r] >> i) & 1u)) highest = fmaxf(highest, rounded_product(d[r][i / 4][i % 4], scale));
+      const float higher = fmaxf(top[r], over_row(highest, [](float x, float y) { return fmaxf(x, y); }));
+      const float shrink = fast_exp2(top[r] - higher);
+      top[r] = higher;
+      sum[r] *= shrink;
+#pragma unroll
+      for (int j = 0; j < TILES; ++j) acc[r][j] *= shrink;
+    }
+    weigh();
   }
-  sum += s;
+#pragma unroll
+  for (int r = 0; r < R; ++r) sum[r] += s[r];
 }
 
 // R row tiles a wave, RW waves side by side over rows; the other PAGED_WAVES / RW deal the steps among themselves.
@@ -418,7 +431,6 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
   q.load(a, b, hk, m, past, first, rows, c, g);
 
   float top[R], sum[R];
-  bool far = false;
   f32x4_t acc[R][TILES];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
@@ -451,9 +463,9 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
     load_k(at);
     load_v(at);
   }
-  // One step; the next one's entries are requested as soon as their registers are free.  PARTIAL: not every row sees every entry of it.
-  auto take = [&](auto partial) {
-    constexpr bool PARTIAL = decltype(partial)::value;
+  // One step; the next one's entries are requested as soon as their registers are free.  CAREFUL: a row may not see every entry of it.
+  auto take = [&](auto careful) {
+    constexpr bool CAREFUL = decltype(careful)::value;
     const bool there[2] = {at[0] >= 0, at[1] >= 0};
     const int base = step * PAGED_STEP, next = step + KW;
     int64_t next_at[2] = {-1, -1};
@@ -487,14 +499,14 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
     if (next < s1) load_k(next_at);
 
     float s[R][8];
-    uint32_t seen[R];
+    uint32_t seen[R] = {};
+    if constexpr (CAREFUL) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      seen[r] = PARTIAL ? q.seen(a, r, base, g, n, past, there) : 0u;
-      paged_weights<PARTIAL>(d[r], a.scale_log2e, seen[r], far, top[r], sum[r], acc[r], s[r]);
+      for (int r = 0; r < R; ++r) seen[r] = q.template seen<2>(a, r, base, g, n, past, there);
     }
+    paged_weights<CAREFUL, R, 2, TILES>(d, a.scale_log2e, seen, top, sum, acc, s);
     bool some = false;                                                      // an infinity or NaN that some row sees
-    if constexpr (PARTIAL) {
+    if constexpr (CAREFUL) {
       // Entries that no row sees may hold anything: zeros.
       bool unbounded = false;
 #pragma unroll
@@ -508,7 +520,7 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
       }
       some = m > 1 && __builtin_amdgcn_ballot_w64(unbounded) != 0;
     }
-    if constexpr (Y::F32 && PARTIAL) {
+    if constexpr (Y::F32 && CAREFUL) {
       if (some) {
 #pragma unroll
         for (int j = 0; j < TILES; ++j) {
@@ -555,7 +567,7 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
 #pragma unroll
       for (int j = 0; j < TILES; ++j) {
         uint4_t value = value_operand<KV, Y::V_WORDS>(vx, j);
-        if constexpr (PARTIAL) {
+        if constexpr (CAREFUL) {
           if (some) {
 #pragma unroll
             for (int r = 0; r < R; ++r)
@@ -576,13 +588,13 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
     at[1] = next_at[1];
     step = next;
   };
-  // Steps that every row sees whole come first; from the first other one on, all are taken with care.  Code of both in one loop would
-  // cost the ordinary steps their registers.
+  // Steps that every row sees whole come first; from the first other one on, all are taken with care.  Code of both
+  // in one loop would cost the ordinary steps their registers.
 #pragma unroll 1
   while (has_rows && step < s1 && (step + 1) * PAGED_STEP <= all_see && at[0] >= 0 && at[1] >= 0) take(std::false_type{});
 #pragma unroll 1
   while (has_rows && step < s1) take(std::true_type{});
-  settle_all();
+  settle(acc);
   paged_say(a, bad, lane);
 
   // Results: lane (c, g) holds elements 8 NB g .. + 8 NB - 1 of its rows.  Each wave divides by its sum, and waves are put together as

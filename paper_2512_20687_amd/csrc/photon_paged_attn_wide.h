@@ -45,7 +45,6 @@ template <int NB, int WAVES> __global__ __launch_bounds__(WAVES * 64, 2) void pa
   PagedRows<bf16_t, bf16_t, NB, R> q;
   q.load(a, b, hk, m, past, first, rows, c, g);
   float top[R], sum[R];
-  bool far = false;
   f32x4_t acc[R][TILES];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
@@ -92,91 +91,111 @@ template <int NB, int WAVES> __global__ __launch_bounds__(WAVES * 64, 2) void pa
     v_at[j] = WIDE_STAGE * ROW + row * ROW + ((2 * j + ((c & 3) >> 1)) ^ v_turn(row)) * 16 + (c & 1) * 8;
   }
 
-  // One step: `in` is where its K begins.  PARTIAL: not every row sees every entry of it.
-  auto take = [&](auto partial, const char* in, int base, const Places& now, int half) {
-    constexpr bool PARTIAL = decltype(partial)::value;
-    const bool there[2] = {(half ? now.at[2] : now.at[0]) >= 0, (half ? now.at[3] : now.at[1]) >= 0};
-    f32x4_t d[R][2];
+  // One stage, in LDS at `in`: all its scores, their weights, then the values, 32 entries at a time.  CAREFUL: a row may not see every
+  // entry of it.
+  auto take = [&](auto careful, const char* in, int base, const Places& now) {
+    constexpr bool CAREFUL = decltype(careful)::value;
+    f32x4_t d[R][4];
+    // A tile's operands are requested a tile ahead: the compiler, left to itself, reads each right before its use.
+    uint4_t key[2][NB];
+    auto read_keys = [&](int i) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+      for (int f = 0; f < NB; ++f) key[i & 1][f] = *reinterpret_cast<const uint4_t*>(in + i * 16 * ROW + k_at[f]);
+    };
+    read_keys(0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (i < 3) read_keys(i + 1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int r = 0; r < R; ++r) d[r][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int f = 0; f < NB; ++f) {
-        const bf16x8_t key = as_bf16x8(*reinterpret_cast<const uint4_t*>(in + i * 16 * ROW + k_at[f]));
+      for (int f = 0; f < NB; ++f)
 #pragma unroll
-        for (int r = 0; r < R; ++r) d[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q.operand(r, 0, f), d[r][i], 0, 0, 0);
-      }
+        for (int r = 0; r < R; ++r) d[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(key[i & 1][f]), q.operand(r, 0, f), d[r][i], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
     }
     settle(d);
-    float s[R][8];
-    uint32_t seen[R];
+    float s[R][16];
+    uint32_t seen[R] = {};
+    const bool there[4] = {now.at[0] >= 0, now.at[1] >= 0, now.at[2] >= 0, now.at[3] >= 0};
+    if constexpr (CAREFUL) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      seen[r] = PARTIAL ? q.seen(a, r, base, g, n, past, there) : 0u;
-      paged_weights<PARTIAL>(d[r], a.scale_log2e, seen[r], far, top[r], sum[r], acc[r], s[r]);
+      for (int r = 0; r < R; ++r) seen[r] = q.template seen<4>(a, r, base, g, n, past, there);
     }
-    uint4_t keep = {~0u, ~0u, ~0u, ~0u};                                   // of a lane's eight entries
-    bool some = false;                                                   // an infinity or NaN that some row sees
-    if constexpr (PARTIAL) {
-      // Entries that no row sees may hold anything: zeros.
+    paged_weights<CAREFUL, R, 4, TILES>(d, a.scale_log2e, seen, top, sum, acc, s);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int entry = base + i / 2 * 16 + 4 * g + i % 2 * 2;
-        keep[i] = (entry < n && there[i / 2] ? 0xffffu : 0u) | (entry + 1 < n && there[i / 2] ? 0xffff0000u : 0u);
-      }
-      if (m > 1) {
-        const int mine = lane / 2;                                         // entry of the step that this lane looks at, half of its row
-        const bool used = base + mine < n && (mine < 16 ? there[0] : there[1]);
-        bool bad = false;
+    for (int half = 0; half < 2; ++half) {
+      const char* values = in + half * PAGED_STEP * ROW;
+      uint4_t keep = {~0u, ~0u, ~0u, ~0u};                                   // of a lane's eight entries
+      bool some = false;                                                     // an infinity or NaN that some row sees
+      if constexpr (CAREFUL) {
+        // Entries that no row sees may hold anything: zeros.
 #pragma unroll
-        for (int i = 0; i < CHUNKS / 2; ++i) {
-          const uint4_t x = *reinterpret_cast<const uint4_t*>(in + WIDE_STAGE * ROW + mine * ROW + (lane % 2 * (CHUNKS / 2) + i) * 16);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) bad = bad || without_unbounded<bf16_t>(x[e]) != x[e];
+        for (int i = 0; i < 4; ++i) {
+          const int entry = base + half * PAGED_STEP + i / 2 * 16 + 4 * g + i % 2 * 2;
+          const bool tile = there[2 * half + i / 2];
+          keep[i] = (entry < n && tile ? 0xffffu : 0u) | (entry + 1 < n && tile ? 0xffff0000u : 0u);
         }
-        some = __builtin_amdgcn_ballot_w64(bad && used) != 0;
-      }
-    }
-    bf16x8_t p[R][2];
+        if (m > 1) {
+          const int mine = half * PAGED_STEP + lane / 2;                     // entry of the stage that this lane looks at, half of its row
+          const bool used = base + mine < n && (lane < 32 ? there[2 * half] : there[2 * half + 1]);
+          bool bad = false;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      uint4_t high, low;
+          for (int i = 0; i < CHUNKS / 2; ++i) {
+            const uint4_t x = *reinterpret_cast<const uint4_t*>(in + WIDE_STAGE * ROW + mine * ROW + (lane % 2 * (CHUNKS / 2) + i) * 16);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float x = s[r][2 * i], y = s[r][2 * i + 1];
-        high[i] = high_halves(x, y);
-        low[i] = pack_bf16x2(x - high_part(x), y - high_part(y));
-      }
-      p[r][0] = as_bf16x8(high);
-      p[r][1] = as_bf16x8(low);
-    }
-#pragma unroll
-    for (int j = 0; j < TILES; ++j) {
-      uint4_t value;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const short4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t)(in + i * 16 * ROW + v_at[j]));
-        const uint2v_t w = __builtin_bit_cast(uint2v_t, x);
-        value[2 * i] = w[0];
-        value[2 * i + 1] = w[1];
-      }
-      if constexpr (PARTIAL) {
-        __builtin_amdgcn_sched_barrier(0);                               // rare code: few registers rather than overlap
-        value &= keep;
-        if (some) {
-#pragma unroll
-          for (int r = 0; r < R; ++r)
-            add_unbounded(acc[r][j], __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(unbounded_codes(value)), as_bf16x8(seen_operand(seen[r])),
-                                                                             f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0));
-#pragma unroll
-          for (int i = 0; i < 4; ++i) value[i] = without_unbounded<bf16_t>(value[i]);
+            for (int e = 0; e < 4; ++e) bad = bad || without_unbounded<bf16_t>(x[e]) != x[e];
+          }
+          some = __builtin_amdgcn_ballot_w64(bad && used) != 0;
         }
       }
+      bf16x8_t p[R][2];
 #pragma unroll
-      for (int part = 1; part >= 0; --part)
+      for (int r = 0; r < R; ++r) {
+        uint4_t high, low;
 #pragma unroll
-        for (int r = 0; r < R; ++r) acc[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(value), p[r][part], acc[r][j], 0, 0, 0);
+        for (int i = 0; i < 4; ++i) {
+          const float x = s[r][8 * half + 2 * i], y = s[r][8 * half + 2 * i + 1];
+          high[i] = high_halves(x, y);
+          low[i] = pack_bf16x2(x - high_part(x), y - high_part(y));
+        }
+        p[r][0] = as_bf16x8(high);
+        p[r][1] = as_bf16x8(low);
+      }
+      constexpr int AHEAD = 2;                                               // operands requested ahead
+      uint4_t ahead[AHEAD];
+      auto read_values = [&](int j) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint2v_t w = __builtin_bit_cast(uint2v_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t)(values + i * 16 * ROW + v_at[j])));
+          ahead[j % AHEAD][2 * i] = w[0];
+          ahead[j % AHEAD][2 * i + 1] = w[1];
+        }
+      };
+#pragma unroll
+      for (int j = 0; j < AHEAD && j < TILES; ++j) read_values(j);
+#pragma unroll
+      for (int j = 0; j < TILES; ++j) {
+        uint4_t value = ahead[j % AHEAD];
+        if (j + AHEAD < TILES) read_values(j + AHEAD);
+        __builtin_amdgcn_sched_barrier(6);                                   // arithmetic may pass
+        if constexpr (CAREFUL) {
+          value &= keep;
+          if (some) {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+              add_unbounded(acc[r][j], __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(unbounded_codes(value)), as_bf16x8(seen_operand(seen[r] >> (8 * half))),
+                                                                               f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) value[i] = without_unbounded<bf16_t>(value[i]);
+          }
+        }
+#pragma unroll
+        for (int part = 1; part >= 0; --part)
+#pragma unroll
+          for (int r = 0; r < R; ++r) acc[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(value), p[r][part], acc[r][j], 0, 0, 0);
+      }
     }
   };
 
@@ -196,20 +215,14 @@ template <int NB, int WAVES> __global__ __launch_bounds__(WAVES * 64, 2) void pa
 #pragma unroll 1
   for (; stage < s1 && (stage + 1) * WIDE_STAGE <= group_sees && now.at[0] >= 0 && now.at[1] >= 0 && now.at[2] >= 0 && now.at[3] >= 0; ++stage, now = next) {
     const char* in = begin();
-    if (!has_rows) continue;
-#pragma unroll 1
-    for (int half = 0; half < 2; ++half) take(std::false_type{}, in + half * (PAGED_STEP * ROW), stage * WIDE_STAGE + half * PAGED_STEP, now, half);
+    if (has_rows) take(std::false_type{}, in, stage * WIDE_STAGE, now);
   }
 #pragma unroll 1
   for (; stage < s1; ++stage, now = next) {
     const char* in = begin();
-#pragma unroll 1
-    for (int half = 0; half < 2; ++half) {
-      const int base = stage * WIDE_STAGE + half * PAGED_STEP;
-      if (base < wave_hi) take(std::true_type{}, in + half * (PAGED_STEP * ROW), base, now, half);
-    }
+    if (stage * WIDE_STAGE < wave_hi) take(std::true_type{}, in, stage * WIDE_STAGE, now);
   }
-  settle_all();
+  settle(acc);
   paged_say(a, bad_page, lane);
 
   // lane (c, g) holds elements 16 j + 4 g .. + 3 of its rows
