@@ -278,18 +278,15 @@ __device__ __forceinline__ void paged_say(const PagedAttnArgs& a, bool bad, int 
 template <typename KV, typename T, int NB, int R> struct PagedRows {
   using Y = PagedTypes<KV, T, NB>;
   uint32_t w[R][Y::Q_WORDS];
-  int limit[R];                                // entries below are seen (without a tree)
+  int limit[R];                                // entries below are seen (without a tree); set by look(), as the next
   uint64_t bits[R];                            // own entries that are seen (with one)
 
   // Rows `first` .. of a stream that has `rows`: those behind the last are given its values and not stored.
-  __device__ __forceinline__ void load(const PagedAttnArgs& a, int b, int hk, int m, int past, int64_t first, int64_t rows, int c, int g) {
+  __device__ __forceinline__ void load(const PagedAttnArgs& a, int b, int hk, int64_t first, int64_t rows, int c, int g) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int64_t row = min(first + r * 16 + c, rows - 1);
       const int t = (int)(row / a.group), h = hk * a.group + (int)(row - (int64_t)t * a.group);
-      limit[r] = past + t + 1;
-      bits[r] = 0;
-      if (a.tree) bits[r] = a.tree[(int64_t)b * a.T + t] & (m == 64 ? ~0ull : (1ull << m) - 1);
       const T* from = (const T*)a.q + ((int64_t)b * a.T + t) * a.q_stride + (int64_t)h * a.pool.d_h;
       if constexpr (Y::F32) {
 #pragma unroll
@@ -318,6 +315,15 @@ template <typename KV, typename T, int NB, int R> struct PagedRows {
             }
           }
       }
+    }
+  }
+  __device__ __forceinline__ void look(const PagedAttnArgs& a, int b, int m, int past, int64_t first, int64_t rows, int c) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int t = (int)(min(first + r * 16 + c, rows - 1) / a.group);
+      limit[r] = past + t + 1;
+      bits[r] = 0;
+      if (a.tree) bits[r] = a.tree[(int64_t)b * a.T + t] & (m == 64 ? ~0ull : (1ull << m) - 1);
     }
   }
   __device__ __forceinline__ bool visible(const PagedAttnArgs& a, int r, int entry, int past) const {
@@ -428,7 +434,7 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
   const int all_see = a.tree ? past : past + (int)(min(first, rows - 1) / a.group) + 1;    // entries that every row of the wave sees
 
   PagedRows<KV, T, NB, R> q;
-  q.load(a, b, hk, m, past, first, rows, c, g);
+  q.load(a, b, hk, first, rows, c, g);
 
   float top[R], sum[R];
   f32x4_t acc[R][TILES];
@@ -592,6 +598,7 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
   // in one loop would cost the ordinary steps their registers.
 #pragma unroll 1
   while (has_rows && step < s1 && (step + 1) * PAGED_STEP <= all_see && at[0] >= 0 && at[1] >= 0) take(std::false_type{});
+  q.look(a, b, m, past, first, rows, c);
 #pragma unroll 1
   while (has_rows && step < s1) take(std::true_type{});
   settle(acc);

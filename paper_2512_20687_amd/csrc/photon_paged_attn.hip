@@ -10,7 +10,7 @@ int paged_auto_splits(int Bt, int T, int H, int H_kv, int64_t S_max, bool f32_ro
   const PagedTile tile = paged_tile(rows, f32_rows, kv_dt);
   const int64_t groups = (int64_t)Bt * H_kv * ((rows + tile.rows() - 1) / tile.rows());
   const int64_t steps = (S_max + PAGED_STEP - 1) / PAGED_STEP;
-  int64_t splits = (tile.wide ? 256 : 512) / groups;
+  int64_t splits = (tile.wide && tile.waves == 8 ? 256 : 512) / groups;
   const int64_t most = tile.wide ? steps / 8 : steps * tile.waves / (4 * PAGED_WAVES);
   splits = splits > most ? most : splits;
   return (int)(splits < 1 ? 1 : splits > 256 ? 256 : splits);

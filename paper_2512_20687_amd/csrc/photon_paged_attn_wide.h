@@ -17,10 +17,21 @@ constexpr int WIDE_TILES = 2;                  // row tiles of a wave
 typedef short short4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) short4_t* lds_short4_t;
 
+// load16_to_lds from a wave-uniform address and an offset per lane: no arithmetic per load.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void load16_to_lds_from(const void* base, uint32_t offset, uint32_t lds_base) {
+  const uint64_t at = reinterpret_cast<uint64_t>(base);
+  const uint64_t in = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at);
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(in), "s"(__builtin_amdgcn_readfirstlane(lds_base)) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
 // Every load and LDS access of this wave is complete, and every wave of the workgroup is here.
 __device__ __forceinline__ void wide_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-template <int NB, int WAVES> __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_wide_kernel(PagedAttnArgs a) {
+// PAGES: of a stage (its 64 entries lie in one page, or in up to four).
+template <int NB, int WAVES, int PAGES> __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_wide_kernel(PagedAttnArgs a) {
   using Y = PagedTypes<bf16_t, bf16_t, NB>;
   constexpr int DP = Y::DP, TILES = Y::TILES, R = WIDE_TILES, ROW = 2 * DP, CHUNKS = ROW / 16;
   constexpr int LOADS = WIDE_STAGE * ROW / 1024, ROWS_LOAD = 1024 / ROW, PER = 2 * LOADS / WAVES;   // loads of a matrix; rows of one; a wave's, of both
@@ -43,7 +54,7 @@ template <int NB, int WAVES> __global__ __launch_bounds__(WAVES * 64, 2) void pa
   const int wave_hi = !has_rows ? 0 : a.tree ? n : min(n, past + (int)(last / a.group) + 1);
 
   PagedRows<bf16_t, bf16_t, NB, R> q;
-  q.load(a, b, hk, m, past, first, rows, c, g);
+  q.load(a, b, hk, first, rows, c, g);
   float top[R], sum[R];
   f32x4_t acc[R][TILES];
 #pragma unroll
@@ -59,53 +70,74 @@ template <int NB, int WAVES> __global__ __launch_bounds__(WAVES * 64, 2) void pa
   auto v_turn = [](int row) { return ((row * NB / 4) & (CHUNKS / 2 - 1)) * 2; };
   const int32_t* table = a.pool.table + (int64_t)b * a.pool.max_pages;
   bool bad_page = false;
-  struct Places { int64_t at[4]; };                                          // of a stage's tiles of 16 entries
-  auto places = [&](int stage) {
-    Places p;
+  constexpr int PART = WIDE_STAGE / PAGES;                                   // entries that are together for certain
+  struct Pages { int32_t page[PAGES]; };
+  auto pages = [&](int stage) {                                              // behind the last entry: the last one's
+    Pages p;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) p.at[i] = paged_place(a, table, hk, stage * WIDE_STAGE + 16 * i, n, bad_page);
+    for (int i = 0; i < PAGES; ++i) p.page[i] = table[min(stage * WIDE_STAGE + PART * i, max(n - 1, 0)) >> a.pool.page_shift];
     return p;
   };
-  // Load u of this wave is load (wave + WAVES u) of the stage: ROWS_LOAD rows, one tile's; from nowhere: the pool's first entries.
-  int from[PER];
+  struct Places {
+    int64_t at[PAGES];                                                       // where the parts lie (nowhere: the pool's first entries)
+    uint32_t there;                                                          // bit i: tile i is somewhere
+  };
+  auto places = [&](const Pages& pages, int stage) {
+    Places p;
+    p.there = 0;
+#pragma unroll
+    for (int i = 0; i < PAGES; ++i) {
+      const int entry = stage * WIDE_STAGE + PART * i, page = __builtin_amdgcn_readfirstlane(pages.page[i]);
+      const bool inside = page >= 0 && page < a.pool.n_pages, used = entry < n;
+      bad_page = bad_page || (used && !inside);
+      p.there |= used && inside ? (PAGES == 1 ? 15u : 1u << i) : 0u;
+      const int64_t row = (((int64_t)(used && inside ? page : 0) * a.pool.H_kv + hk) << a.pool.page_shift) + (entry & ((1 << a.pool.page_shift) - 1));
+      p.at[i] = row * ROW;
+    }
+    return p;
+  };
+  // Half of the waves load K, half V: load u of a wave is its matrix's load HALF u + wave % HALF, ROWS_LOAD rows of one tile.
+  constexpr int HALF = WAVES / 2, SPAN = HALF > NB ? HALF / NB : 1;
+  const int mine = wave % HALF;
+  const uint8_t* const pool = wave < HALF ? a.pool.k : a.pool.v;
+  const uint32_t lds_mine = lds + (wave < HALF ? 0 : WIDE_STAGE * ROW) + mine * 1024;
+  uint32_t from[PER];
 #pragma unroll
   for (int u = 0; u < PER; ++u) {
-    const int i = wave + WAVES * u, row = i % LOADS * ROWS_LOAD + lane / CHUNKS, chunk = lane % CHUNKS;
-    from[u] = row % 16 * ROW + (chunk ^ (i < LOADS ? k_turn(row) : v_turn(row))) * 16;
+    const int row = (HALF * u + mine) * ROWS_LOAD + lane / CHUNKS, chunk = lane % CHUNKS;
+    from[u] = row % PART * ROW + (chunk ^ (wave < HALF ? k_turn(row) : v_turn(row))) * 16;
   }
-  auto stage_in = [&](const Places& p, int buffer) {
+  auto load_in = [&](const Places& p, int buffer, int u) {
+    int64_t at = p.at[0];
+    if constexpr (PAGES > 1) {
+      at = p.at[HALF * u / NB];
 #pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      const int i = wave + WAVES * u, tile = i % LOADS * ROWS_LOAD / 16;
-      const int64_t at = tile == 0 ? p.at[0] : tile == 1 ? p.at[1] : tile == 2 ? p.at[2] : p.at[3];
-      load16_to_lds((i < LOADS ? a.pool.k : a.pool.v) + (at < 0 ? 0 : at) + from[u], lds + buffer * (2 * WIDE_STAGE * ROW) + i * 1024);
+      for (int i = 1; i < SPAN; ++i) at = mine / NB == i ? p.at[HALF * u / NB + i] : at;
     }
+    load16_to_lds_from(pool + at, from[u], lds_mine + buffer * (2 * WIDE_STAGE * ROW) + u * (HALF * 1024));
   };
-  // LDS places of this lane's operands, of the first tile
-  int k_at[NB], v_at[TILES];
-#pragma unroll
-  for (int f = 0; f < NB; ++f) k_at[f] = c * ROW + ((4 * f + g) ^ k_turn(c)) * 16;
-#pragma unroll
-  for (int j = 0; j < TILES; ++j) {
-    const int row = 4 * g + (c >> 2);
-    v_at[j] = WIDE_STAGE * ROW + row * ROW + ((2 * j + ((c & 3) >> 1)) ^ v_turn(row)) * 16 + (c & 1) * 8;
-  }
+  // LDS places of this lane's operands in the first tile: K's of product f is k_at ^ 64 f, V's of elements 16 j .. is v_at ^ 32 j
+  const uint32_t k_first = c * ROW + (g ^ k_turn(c)) * 16;
+  const uint32_t v_first = WIDE_STAGE * ROW + (4 * g + (c >> 2)) * ROW + (((c & 3) >> 1) ^ v_turn(4 * g + (c >> 2))) * 16 + (c & 1) * 8;
 
   // One stage, in LDS at `in`: all its scores, their weights, then the values, 32 entries at a time.  CAREFUL: a row may not see every
   // entry of it.
-  auto take = [&](auto careful, const char* in, int base, const Places& now) {
+  auto take = [&](auto careful, const char* in, int base, uint32_t now, auto request) {
     constexpr bool CAREFUL = decltype(careful)::value;
+    uint32_t k_at = k_first, v_at = v_first;
+    asm volatile("" : "+v"(k_at), "+v"(v_at));                               // an exclusive-or a read, not a register for each over the whole loop
     f32x4_t d[R][4];
     // A tile's operands are requested a tile ahead: the compiler, left to itself, reads each right before its use.
     uint4_t key[2][NB];
     auto read_keys = [&](int i) {
 #pragma unroll
-      for (int f = 0; f < NB; ++f) key[i & 1][f] = *reinterpret_cast<const uint4_t*>(in + i * 16 * ROW + k_at[f]);
+      for (int f = 0; f < NB; ++f) key[i & 1][f] = *reinterpret_cast<const uint4_t*>(in + i * 16 * ROW + (k_at ^ (64 * f)));
     };
     read_keys(0);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if (i < 3) read_keys(i + 1);
+      request(i);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int r = 0; r < R; ++r) d[r][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -118,7 +150,7 @@ template <int NB, int WAVES> __global__ __launch_bounds__(WAVES * 64, 2) void pa
     settle(d);
     float s[R][16];
     uint32_t seen[R] = {};
-    const bool there[4] = {now.at[0] >= 0, now.at[1] >= 0, now.at[2] >= 0, now.at[3] >= 0};
+    const bool there[4] = {(now & 1) != 0, (now & 2) != 0, (now & 4) != 0, (now & 8) != 0};
     if constexpr (CAREFUL) {
 #pragma unroll
       for (int r = 0; r < R; ++r) seen[r] = q.template seen<4>(a, r, base, g, n, past, there);
@@ -168,7 +200,7 @@ template <int NB, int WAVES> __global__ __launch_bounds__(WAVES * 64, 2) void pa
       auto read_values = [&](int j) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const uint2v_t w = __builtin_bit_cast(uint2v_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t)(values + i * 16 * ROW + v_at[j])));
+          const uint2v_t w = __builtin_bit_cast(uint2v_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t)(values + i * 16 * ROW + (v_at ^ (32 * j)))));
           ahead[j % AHEAD][2 * i] = w[0];
           ahead[j % AHEAD][2 * i + 1] = w[1];
         }
@@ -202,26 +234,48 @@ template <int NB, int WAVES> __global__ __launch_bounds__(WAVES * 64, 2) void pa
   // Stages that every row of the workgroup sees whole come first; from the first other one on, all steps are taken with care.  Code of
   // both in one loop would cost the ordinary steps their registers.
   const int group_sees = a.tree ? past : past + (int)(group_first / a.group) + 1;
-  Places now = places(s0), next = now;
+  Pages ahead = pages(s0);
+  Places next = places(ahead, s0);
+  uint32_t now = next.there;
+  ahead = pages(s0 + 1);
   int stage = s0;
-  if (s0 < s1) stage_in(now, 0);
-  auto begin = [&]() -> const char* {                                        // this stage is there, the next one on its way
-    const int buffer = (stage - s0) & 1;
-    if (stage + 1 < s1) next = places(stage + 1);
-    wide_barrier();                                                          // the other buffer is no longer read
-    if (stage + 1 < s1) stage_in(next, buffer ^ 1);
-    return wide_lds + buffer * (2 * WIDE_STAGE * ROW);
+  if (s0 < s1) {
+#pragma unroll
+    for (int u = 0; u < PER; ++u) load_in(next, 0, u);
+  }
+  auto begin = [&]() {                                                       // this stage is there, and the other buffer no longer read
+    next = places(ahead, stage + 1);
+    ahead = pages(stage + 2);                                                // requested a stage before they are needed
+    wide_barrier();
+    return (stage - s0) & 1;
+  };
+  // The next stage's loads (behind the last one: of entries that nothing uses), a quarter at a time: a burst of them holds a wave up for
+  // as long as its products take.
+  auto request = [&](int buffer, int quarter) {
+#pragma unroll
+    for (int u = 0; u < PER; ++u)
+      if (u * 4 / PER == quarter) load_in(next, buffer ^ 1, u);
   };
 #pragma unroll 1
-  for (; stage < s1 && (stage + 1) * WIDE_STAGE <= group_sees && now.at[0] >= 0 && now.at[1] >= 0 && now.at[2] >= 0 && now.at[3] >= 0; ++stage, now = next) {
-    const char* in = begin();
-    if (has_rows) take(std::false_type{}, in, stage * WIDE_STAGE, now);
+  for (; stage < s1 && (stage + 1) * WIDE_STAGE <= group_sees && now == 15; ++stage, now = next.there) {
+    const int buffer = begin();
+    if (has_rows)
+      take(std::false_type{}, wide_lds + buffer * (2 * WIDE_STAGE * ROW), stage * WIDE_STAGE, now, [&](int i) { request(buffer, i); });
+    else
+#pragma unroll
+      for (int i = 0; i < 4; ++i) request(buffer, i);
   }
+  q.look(a, b, m, past, first, rows, c);
 #pragma unroll 1
-  for (; stage < s1; ++stage, now = next) {
-    const char* in = begin();
-    if (stage * WIDE_STAGE < wave_hi) take(std::true_type{}, in, stage * WIDE_STAGE, now);
+  for (; stage < s1; ++stage, now = next.there) {
+    const int buffer = begin();
+    if (stage * WIDE_STAGE < wave_hi)
+      take(std::true_type{}, wide_lds + buffer * (2 * WIDE_STAGE * ROW), stage * WIDE_STAGE, now, [&](int i) { request(buffer, i); });
+    else
+#pragma unroll
+      for (int i = 0; i < 4; ++i) request(buffer, i);
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                         // no load outlives the workgroup's LDS
   settle(acc);
   paged_say(a, bad_page, lane);
 
@@ -243,7 +297,9 @@ template <int NB, int WAVES> __global__ __launch_bounds__(WAVES * 64, 2) void pa
 
 template <int NB, int WAVES> int32_t paged_launch_wide(const PagedAttnArgs& a, hipStream_t st) {
   const unsigned grid = a.row_groups > 1 ? (unsigned)((a.units + 7) / 8 * 8) * (unsigned)a.row_groups : (unsigned)a.units;
-  PHOTON_LAUNCH(KC_COARSE_ATTN, st, (paged_attn_wide_kernel<NB, WAVES>), dim3(grid), dim3(WAVES * 64), 2 * 2 * WIDE_STAGE * 64 * NB, st, a);
+  constexpr unsigned LDS = 2 * 2 * WIDE_STAGE * 64 * NB;
+  if ((1 << a.pool.page_shift) >= WIDE_STAGE) PHOTON_LAUNCH(KC_COARSE_ATTN, st, (paged_attn_wide_kernel<NB, WAVES, 1>), dim3(grid), dim3(WAVES * 64), LDS, st, a);
+  else PHOTON_LAUNCH(KC_COARSE_ATTN, st, (paged_attn_wide_kernel<NB, WAVES, 4>), dim3(grid), dim3(WAVES * 64), LDS, st, a);
   return check_launch("paged_attn_wide_kernel");
 }
 
