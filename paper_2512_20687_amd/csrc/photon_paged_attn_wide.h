@@ -7,12 +7,16 @@
 //   V     pairs of chunks likewise; ds_read_b64_tr_b16 hands a lane four entries of one element, as the contraction over entries takes
 //         them: the interleaving of the register kernel is the LDS's work here
 #pragma once
+#include <atomic>
+
 #include "photon_paged_attn.h"
 
 namespace photon {
 
 constexpr int WIDE_STAGE = 64;                 // entries of a stage
 constexpr int WIDE_TILES = 2;                  // row tiles of a wave
+
+constexpr int WIDE_VBUF = 3;                   // V is kept for a stage longer than K (see the loop)
 
 typedef short short4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) short4_t* lds_short4_t;
@@ -34,8 +38,9 @@ __device__ __forceinline__ void wide_barrier() { asm volatile("s_waitcnt vmcnt(0
 template <int NB, int WAVES, int PAGES> __global__ __launch_bounds__(WAVES * 64, 2) void paged_attn_wide_kernel(PagedAttnArgs a) {
   using Y = PagedTypes<bf16_t, bf16_t, NB>;
   constexpr int DP = Y::DP, TILES = Y::TILES, R = WIDE_TILES, ROW = 2 * DP, CHUNKS = ROW / 16;
+  constexpr int STAGE = WIDE_STAGE * ROW, VBUF = WIDE_VBUF;       // bytes of a stage's K, or V
   constexpr int LOADS = WIDE_STAGE * ROW / 1024, ROWS_LOAD = 1024 / ROW, PER = 2 * LOADS / WAVES;   // loads of a matrix; rows of one; a wave's, of both
-  extern __shared__ __align__(16) char wide_lds[];                           // [2 buffers][K, V][64][ROW]
+  extern __shared__ __align__(16) char wide_lds[];                           // K [2 buffers][64][ROW], then V [VBUF buffers][64][ROW]
   const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)wide_lds));
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
 
@@ -100,32 +105,33 @@ template <int NB, int WAVES, int PAGES> __global__ __launch_bounds__(WAVES * 64,
   constexpr int HALF = WAVES / 2, SPAN = HALF > NB ? HALF / NB : 1;
   const int mine = wave % HALF;
   const uint8_t* const pool = wave < HALF ? a.pool.k : a.pool.v;
-  const uint32_t lds_mine = lds + (wave < HALF ? 0 : WIDE_STAGE * ROW) + mine * 1024;
+  const uint32_t lds_mine = lds + (wave < HALF ? 0 : 2 * STAGE) + mine * 1024;
   uint32_t from[PER];
 #pragma unroll
   for (int u = 0; u < PER; ++u) {
     const int row = (HALF * u + mine) * ROWS_LOAD + lane / CHUNKS, chunk = lane % CHUNKS;
     from[u] = row % PART * ROW + (chunk ^ (wave < HALF ? k_turn(row) : v_turn(row))) * 16;
   }
-  auto load_in = [&](const Places& p, int buffer, int u) {
+  auto load_in = [&](const Places& p, int buffer, int u) {                     // buffer: of this wave's matrix
     int64_t at = p.at[0];
     if constexpr (PAGES > 1) {
       at = p.at[HALF * u / NB];
 #pragma unroll
       for (int i = 1; i < SPAN; ++i) at = mine / NB == i ? p.at[HALF * u / NB + i] : at;
     }
-    load16_to_lds_from(pool + at, from[u], lds_mine + buffer * (2 * WIDE_STAGE * ROW) + u * (HALF * 1024));
+    load16_to_lds_from(pool + at, from[u], lds_mine + buffer * STAGE + u * (HALF * 1024));
   };
   // LDS places of this lane's operands in the first tile: K's of product f is k_at ^ 64 f, V's of elements 16 j .. is v_at ^ 32 j
   const uint32_t k_first = c * ROW + (g ^ k_turn(c)) * 16;
-  const uint32_t v_first = WIDE_STAGE * ROW + (4 * g + (c >> 2)) * ROW + (((c & 3) >> 1) ^ v_turn(4 * g + (c >> 2))) * 16 + (c & 1) * 8;
+  const uint32_t v_first = (4 * g + (c >> 2)) * ROW + (((c & 3) >> 1) ^ v_turn(4 * g + (c >> 2))) * 16 + (c & 1) * 8;
 
-  // One stage, in LDS at `in`: all its scores, their weights, then the values, 32 entries at a time.  CAREFUL: a row may not see every
-  // entry of it.
-  auto take = [&](auto careful, const char* in, int base, uint32_t now, auto request) {
+  // A stage's scores and weights, its K in LDS at `in`.  CAREFUL: a row may not see every entry of it.
+  float s[R][16];
+  uint32_t seen[R] = {};
+  auto weigh = [&](auto careful, const char* in, int base, uint32_t now, auto request) {
     constexpr bool CAREFUL = decltype(careful)::value;
-    uint32_t k_at = k_first, v_at = v_first;
-    asm volatile("" : "+v"(k_at), "+v"(v_at));                               // an exclusive-or a read, not a register for each over the whole loop
+    uint32_t k_at = k_first;
+    asm volatile("" : "+v"(k_at));                                           // an exclusive-or a read, not a register for each over the whole loop
     f32x4_t d[R][4];
     // A tile's operands are requested a tile ahead: the compiler, left to itself, reads each right before its use.
     uint4_t key[2][NB];
@@ -148,14 +154,19 @@ template <int NB, int WAVES, int PAGES> __global__ __launch_bounds__(WAVES * 64,
       __builtin_amdgcn_sched_barrier(0);
     }
     settle(d);
-    float s[R][16];
-    uint32_t seen[R] = {};
-    const bool there[4] = {(now & 1) != 0, (now & 2) != 0, (now & 4) != 0, (now & 8) != 0};
     if constexpr (CAREFUL) {
+      const bool there[4] = {(now & 1) != 0, (now & 2) != 0, (now & 4) != 0, (now & 8) != 0};
 #pragma unroll
       for (int r = 0; r < R; ++r) seen[r] = q.template seen<4>(a, r, base, g, n, past, there);
     }
     paged_weights<CAREFUL, R, 4, TILES>(d, a.scale_log2e, seen, top, sum, acc, s);
+  };
+  // The values under those weights, V in LDS at `in`, 32 entries at a time.
+  auto add_values = [&](auto careful, const char* in, int base, uint32_t now) {
+    constexpr bool CAREFUL = decltype(careful)::value;
+    uint32_t v_at = v_first;
+    asm volatile("" : "+v"(v_at));
+    const bool there[4] = {(now & 1) != 0, (now & 2) != 0, (now & 4) != 0, (now & 8) != 0};
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const char* values = in + half * PAGED_STEP * ROW;
@@ -175,7 +186,7 @@ template <int NB, int WAVES, int PAGES> __global__ __launch_bounds__(WAVES * 64,
           bool bad = false;
 #pragma unroll
           for (int i = 0; i < CHUNKS / 2; ++i) {
-            const uint4_t x = *reinterpret_cast<const uint4_t*>(in + WIDE_STAGE * ROW + mine * ROW + (lane % 2 * (CHUNKS / 2) + i) * 16);
+            const uint4_t x = *reinterpret_cast<const uint4_t*>(in + mine * ROW + (lane % 2 * (CHUNKS / 2) + i) * 16);
 #pragma unroll
             for (int e = 0; e < 4; ++e) bad = bad || without_unbounded<bf16_t>(x[e]) != x[e];
           }
@@ -243,37 +254,59 @@ template <int NB, int WAVES, int PAGES> __global__ __launch_bounds__(WAVES * 64,
 #pragma unroll
     for (int u = 0; u < PER; ++u) load_in(next, 0, u);
   }
-  auto begin = [&]() {                                                       // this stage is there, and the other buffer no longer read
+  int k_buffer = 0, v_buffer = 0;                                            // this stage's
+  auto begin = [&]() {                                                       // this stage is there, and what it is not to use no longer read
     next = places(ahead, stage + 1);
     ahead = pages(stage + 2);                                                // requested a stage before they are needed
     wide_barrier();
-    return (stage - s0) & 1;
   };
   // The next stage's loads (behind the last one: of entries that nothing uses), a quarter at a time: a burst of them holds a wave up for
   // as long as its products take.
-  auto request = [&](int buffer, int quarter) {
+  auto request = [&](int quarter) {
+    const int buffer = wave < HALF ? k_buffer ^ 1 : v_buffer + 1 == VBUF ? 0 : v_buffer + 1;
 #pragma unroll
     for (int u = 0; u < PER; ++u)
-      if (u * 4 / PER == quarter) load_in(next, buffer ^ 1, u);
+      if (u * 4 / PER == quarter) load_in(next, buffer, u);
   };
+  auto end = [&]() {
+    ++stage;
+    k_buffer ^= 1;
+    v_buffer = v_buffer + 1 == VBUF ? 0 : v_buffer + 1;
+    now = next.there;
+  };
+  auto keys = [&]() { return wide_lds + k_buffer * STAGE; };
+  auto values = [&](int buffer) { return wide_lds + 2 * STAGE + buffer * STAGE; };
+  // Two waves that share a SIMD and do the same at the same time wait for each other: both for the matrix core, then both for the vector
+  // unit.  So the second half of a workgroup's waves adds a stage's values after the next barrier, when the first half is at its scores,
+  // and is at its weights when they are at their values.  Of two workgroups of four waves, which share a unit's SIMDs, so does the one.
+  const bool late = WAVES == 8 ? wave >= HALF : ((blockIdx.x >> 8) & 1) != 0;
 #pragma unroll 1
-  for (; stage < s1 && (stage + 1) * WIDE_STAGE <= group_sees && now == 15; ++stage, now = next.there) {
-    const int buffer = begin();
-    if (has_rows)
-      take(std::false_type{}, wide_lds + buffer * (2 * WIDE_STAGE * ROW), stage * WIDE_STAGE, now, [&](int i) { request(buffer, i); });
-    else
+  while (stage < s1 && (stage + 1) * WIDE_STAGE <= group_sees && now == 15) {
+    begin();
+    if (has_rows) {
+      if (late && stage > s0) add_values(std::false_type{}, values(v_buffer == 0 ? VBUF - 1 : v_buffer - 1), 0, 15);
+      weigh(std::false_type{}, keys(), 0, 15, request);
+      if (!late) add_values(std::false_type{}, values(v_buffer), 0, 15);
+    } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) request(buffer, i);
+      for (int i = 0; i < 4; ++i) request(i);
+    }
+    end();
   }
+  if (late && has_rows && stage > s0) add_values(std::false_type{}, values(v_buffer == 0 ? VBUF - 1 : v_buffer - 1), 0, 15);
   q.look(a, b, m, past, first, rows, c);
 #pragma unroll 1
-  for (; stage < s1; ++stage, now = next.there) {
-    const int buffer = begin();
-    if (stage * WIDE_STAGE < wave_hi)
-      take(std::true_type{}, wide_lds + buffer * (2 * WIDE_STAGE * ROW), stage * WIDE_STAGE, now, [&](int i) { request(buffer, i); });
-    else
+  while (stage < s1) {
+    begin();
+    const int base = stage * WIDE_STAGE;
+    if (base < wave_hi) {
+      weigh(std::true_type{}, keys(), base, now, request);
+      add_values(std::true_type{}, values(v_buffer), base, now);
+    } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) request(buffer, i);
+      for (int i = 0; i < 4; ++i) request(i);
+    }
+    end();
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                         // no load outlives the workgroup's LDS
   settle(acc);
@@ -295,12 +328,23 @@ template <int NB, int WAVES, int PAGES> __global__ __launch_bounds__(WAVES * 64,
   }
 }
 
-template <int NB, int WAVES> int32_t paged_launch_wide(const PagedAttnArgs& a, hipStream_t st) {
+template <int NB, int WAVES, int PAGES> int32_t paged_launch_wide_pages(const PagedAttnArgs& a, hipStream_t st) {
   const unsigned grid = a.row_groups > 1 ? (unsigned)((a.units + 7) / 8 * 8) * (unsigned)a.row_groups : (unsigned)a.units;
-  constexpr unsigned LDS = 2 * 2 * WIDE_STAGE * 64 * NB;
-  if ((1 << a.pool.page_shift) >= WIDE_STAGE) PHOTON_LAUNCH(KC_COARSE_ATTN, st, (paged_attn_wide_kernel<NB, WAVES, 1>), dim3(grid), dim3(WAVES * 64), LDS, st, a);
-  else PHOTON_LAUNCH(KC_COARSE_ATTN, st, (paged_attn_wide_kernel<NB, WAVES, 4>), dim3(grid), dim3(WAVES * 64), LDS, st, a);
+  constexpr unsigned LDS = (2 + WIDE_VBUF) * WIDE_STAGE * 64 * NB;
+  if constexpr (LDS > (64u << 10)) {                             // has to be allowed once on every device
+    static std::atomic<bool> allowed[64];
+    int device = 0;
+    if (hipGetDevice(&device) != hipSuccess || device < 0 || device >= 64 || !allowed[device].load(std::memory_order_relaxed)) {
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(paged_attn_wide_kernel<NB, WAVES, PAGES>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)LDS);
+      if (e != hipSuccess) return fail(PHOTON_ERR_HIP, "paged_attn_wide_kernel: %u bytes of LDS: %s", LDS, hipGetErrorString(e));
+      if (device >= 0 && device < 64) allowed[device].store(true, std::memory_order_relaxed);
+    }
+  }
+  PHOTON_LAUNCH(KC_COARSE_ATTN, st, (paged_attn_wide_kernel<NB, WAVES, PAGES>), dim3(grid), dim3(WAVES * 64), LDS, st, a);
   return check_launch("paged_attn_wide_kernel");
+}
+template <int NB, int WAVES> int32_t paged_launch_wide(const PagedAttnArgs& a, hipStream_t st) {
+  return (1 << a.pool.page_shift) >= WIDE_STAGE ? paged_launch_wide_pages<NB, WAVES, 1>(a, st) : paged_launch_wide_pages<NB, WAVES, 4>(a, st);
 }
 
 }  // namespace photon
