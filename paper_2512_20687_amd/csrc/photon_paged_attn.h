@@ -29,6 +29,7 @@ namespace photon {
 
 constexpr int PAGED_STEP = 32;                 // entries of a step
 constexpr int PAGED_WAVES = 4;                 // of a workgroup
+constexpr int64_t PAGED_MOST_ROWS = (1ll << 31) - 4096;   // that share a K/V head: row numbers, tiles' ends among them, are int32
 constexpr float PAGED_RAISE = 256.f;          // sum of a lane's eight weights of a step from which on the reference rises
 constexpr float PAGED_LOWEST = -FLT_MAX;       // a row's reference before it saw a score
 
@@ -215,11 +216,14 @@ __device__ __forceinline__ void add_unbounded(f32x4_t& acc, const f32x4_t& digit
   }
 }
 
-// Entries that count for sequence b, its queries, and the entries before theirs (less than 0: the first own ones are not there).
-__device__ __forceinline__ void paged_sequence(const PagedAttnArgs& a, int b, int& n, int& m, int& past) {
-  n = __builtin_amdgcn_readfirstlane(a.seq_len[b]);
+// Sequence b as its arrays say, then: the entries that count, its queries, and the entries before theirs (less than 0: the first own
+// ones are not there).  A kernel asks for the former before anything else and uses them behind its own loads of q.
+struct PagedCounts { int32_t len, fresh; };
+__device__ __forceinline__ PagedCounts paged_counts(const PagedAttnArgs& a, int b) { return PagedCounts{a.seq_len[b], a.n_new ? a.n_new[b] : a.T}; }
+__device__ __forceinline__ void paged_sequence(const PagedAttnArgs& a, const PagedCounts& counts, int& n, int& m, int& past) {
+  n = __builtin_amdgcn_readfirstlane(counts.len);
   n = n < 0 ? 0 : n > a.S_max ? a.S_max : n;
-  m = a.n_new ? __builtin_amdgcn_readfirstlane(a.n_new[b]) : a.T;
+  m = __builtin_amdgcn_readfirstlane(counts.fresh);
   m = m < 0 ? 0 : m > a.T ? a.T : m;
   past = n - m;
 }
@@ -242,8 +246,8 @@ __device__ __forceinline__ bool paged_unit(const PagedAttnArgs& a, int& row_grou
 }
 
 // Row `row` of stream (b, hk): its row of out.
-__device__ __forceinline__ int64_t paged_row(const PagedAttnArgs& a, int b, int hk, int64_t row) {
-  const int64_t t = row / a.group;
+__device__ __forceinline__ int64_t paged_row(const PagedAttnArgs& a, int b, int hk, int row) {
+  const int t = row / a.group;
   return ((int64_t)b * a.T + t) * a.H + hk * a.group + (row - t * a.group);
 }
 // Four elements of a row's result: to out, or with its reference and sum to the workspace.
@@ -261,14 +265,14 @@ __device__ __forceinline__ void paged_emit(const PagedAttnArgs& a, int64_t to, i
     st[1] = sum;
   }
 }
-// Where the 16 entries from `entry` on of a sequence of n lie; < 0: nowhere (behind the last, or a page outside the pool, which `bad`
-// remembers).
-__device__ __forceinline__ int64_t paged_place(const PagedAttnArgs& a, const int32_t* table, int hk, int entry, int n, bool& bad) {
-  if (entry >= n) return -1;
-  const int page = __builtin_amdgcn_readfirstlane(table[entry >> a.pool.page_shift]);
-  const bool there = page >= 0 && page < a.pool.n_pages;
-  bad = bad || !there;
-  return there ? page * a.pool.page_bytes + hk * a.pool.head_bytes + (int64_t)((entry & ((1 << a.pool.page_shift) - 1)) * a.pool.row_bytes) : -1;
+// Where the 16 entries from `entry` on of a sequence of n lie, in the page that the table gives; < 0: nowhere (behind the last, or a page
+// outside the pool, which `bad` remembers).
+__device__ __forceinline__ int64_t paged_place(const PagedAttnArgs& a, int page, int hk, int entry, int n, bool& bad) {
+  page = __builtin_amdgcn_readfirstlane(page);
+  const bool used = entry < n, inside = page >= 0 && page < a.pool.n_pages;
+  bad = bad || (used && !inside);
+  const int64_t row = (((int64_t)page * a.pool.H_kv + hk) << a.pool.page_shift) + (entry & ((1 << a.pool.page_shift) - 1));
+  return used && inside ? row * a.pool.row_bytes : -1;
 }
 __device__ __forceinline__ void paged_say(const PagedAttnArgs& a, bool bad, int lane) {
   if (bad && a.status && lane == 0) atomicOr(a.status, (int)PHOTON_STATUS_BAD_PAGE);
@@ -281,12 +285,11 @@ template <typename KV, typename T, int NB, int R> struct PagedRows {
   int limit[R];                                // entries below are seen (without a tree); set by look(), as the next
   uint64_t bits[R];                            // own entries that are seen (with one)
 
-  // Rows `first` .. of a stream that has `rows`: those behind the last are given its values and not stored.
-  __device__ __forceinline__ void load(const PagedAttnArgs& a, int b, int hk, int64_t first, int64_t rows, int c, int g) {
+  // Rows `first` .. of a stream; those behind its last are given that one's values.
+  __device__ __forceinline__ void load(const PagedAttnArgs& a, int b, int hk, int first, int c, int g) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const int64_t row = min(first + r * 16 + c, rows - 1);
-      const int t = (int)(row / a.group), h = hk * a.group + (int)(row - (int64_t)t * a.group);
+      const int row = min(first + r * 16 + c, a.T * a.group - 1), t = row / a.group, h = hk * a.group + (row - t * a.group);
       const T* from = (const T*)a.q + ((int64_t)b * a.T + t) * a.q_stride + (int64_t)h * a.pool.d_h;
       if constexpr (Y::F32) {
 #pragma unroll
@@ -317,10 +320,10 @@ template <typename KV, typename T, int NB, int R> struct PagedRows {
       }
     }
   }
-  __device__ __forceinline__ void look(const PagedAttnArgs& a, int b, int m, int past, int64_t first, int64_t rows, int c) {
+  __device__ __forceinline__ void look(const PagedAttnArgs& a, int b, int m, int past, int first, int rows, int c) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const int t = (int)(min(first + r * 16 + c, rows - 1) / a.group);
+      const int t = min(first + r * 16 + c, rows - 1) / a.group;
       limit[r] = past + t + 1;
       bits[r] = 0;
       if (a.tree) bits[r] = a.tree[(int64_t)b * a.T + t] & (m == 64 ? ~0ull : (1ull << m) - 1);
@@ -410,7 +413,8 @@ __device__ __forceinline__ void paged_weights(const f32x4_t (&d)[R][N], float sc
   for (int r = 0; r < R; ++r) sum[r] += s[r];
 }
 
-// R row tiles a wave, RW waves side by side over rows; the other PAGED_WAVES / RW deal the steps among themselves.
+// R row tiles a wave, RW waves side by side over rows; the KW waves of the same rows deal the steps among themselves.  Fewer waves lose even
+// where streams are many and short (256 x 16 streams of 1085 entries: 203 us, 215 with two waves, 231 with one).
 template <typename KV, typename T, int NB, int R, int RW>
 __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnArgs a) {
   using Y = PagedTypes<KV, T, NB>;
@@ -422,19 +426,31 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
 
   int row_group, hk, split, b;
   if (!paged_unit(a, row_group, hk, split, b)) return;
+  // What is needed first is asked for at once: lengths, q, and (where a wave's first step does not depend on lengths) its pages.
+  const PagedCounts counts = paged_counts(a, b);
+  const int32_t* table = a.pool.table + (int64_t)b * a.pool.max_pages;
+  struct Pages { int32_t page[2]; };                                         // of a step's tiles; behind `most` entries: the last one's
+  auto pages = [&](int step, int most) {
+    Pages p;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) p.page[i] = table[min(step * PAGED_STEP + 16 * i, most - 1) >> a.pool.page_shift];
+    return p;
+  };
+  Pages ahead = pages(kw, a.S_max);
+  __builtin_amdgcn_sched_barrier(0);
+  const int group_first = row_group * (RW * R * 16), first = group_first + rw * (R * 16);
+  PagedRows<KV, T, NB, R> q;
+  q.load(a, b, hk, first, c, g);
+  __builtin_amdgcn_sched_barrier(0);
   int n, m, past;
-  paged_sequence(a, b, n, m, past);
-  const int64_t rows = (int64_t)m * a.group;
-  const int64_t group_first = (int64_t)row_group * (RW * R * 16), first = group_first + rw * (R * 16);
+  paged_sequence(a, counts, n, m, past);
+  const int rows = m * a.group;
   if (group_first >= rows) return;
-  const int64_t group_last = min(group_first + RW * R * 16, rows) - 1;
-  const int hi = a.tree ? n : min(n, past + (int)(group_last / a.group) + 1);               // entries that a row of the workgroup sees
+  const int group_last = min(group_first + RW * R * 16, rows) - 1;
+  const int hi = a.tree ? n : min(n, past + group_last / a.group + 1);                     // entries that a row of the workgroup sees
   const int steps = hi <= 0 ? 0 : (hi + PAGED_STEP - 1) / PAGED_STEP;
   const int s0 = (int)((int64_t)steps * split / a.n_splits), s1 = (int)((int64_t)steps * (split + 1) / a.n_splits);
-  const int all_see = a.tree ? past : past + (int)(min(first, rows - 1) / a.group) + 1;    // entries that every row of the wave sees
-
-  PagedRows<KV, T, NB, R> q;
-  q.load(a, b, hk, first, rows, c, g);
+  const int all_see = a.tree ? past : past + min(first, rows - 1) / a.group + 1;           // entries that every row of the wave sees
 
   float top[R], sum[R];
   f32x4_t acc[R][TILES];
@@ -446,12 +462,15 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
     for (int j = 0; j < TILES; ++j) acc[r][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
 
-  const int32_t* table = a.pool.table + (int64_t)b * a.pool.max_pages;
   bool bad = false;
-  auto place = [&](int entry) { return paged_place(a, table, hk, entry, n, bad); };
+  auto places = [&](const Pages& p, int step, int64_t (&at)[2]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) at[i] = paged_place(a, p.page[i], hk, step * PAGED_STEP + 16 * i, n, bad);
+  };
   const int k_lane = c * a.pool.row_bytes, v_lane = 4 * g * a.pool.row_bytes + c * Y::V_BYTES;
   uint32_t kx[2][Y::K_WORDS], vx[8][Y::V_WORDS];
-  auto load_k = [&](const int64_t (&at)[2]) {                                      // from nowhere: the pool's first entries, in bounds, not used
+  // From nowhere: the pool's first entries, in bounds, not used.
+  auto load_k = [&](const int64_t (&at)[2]) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) load_keys<KV, NB>(a.pool.k + (at[i] < 0 ? 0 : at[i]) + k_lane, g, kx[i]);
   };
@@ -464,10 +483,11 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
   int step = s0 + kw;
   int64_t at[2] = {-1, -1};
   if (has_rows && step < s1) {
-    at[0] = place(step * PAGED_STEP);
-    at[1] = place(step * PAGED_STEP + 16);
+    if (s0 > 0) ahead = pages(step, n);
+    places(ahead, step, at);
     load_k(at);
     load_v(at);
+    ahead = pages(min(step + KW, steps - 1), n);                             // requested a step before they are needed
   }
   // One step; the next one's entries are requested as soon as their registers are free.  CAREFUL: a row may not see every entry of it.
   auto take = [&](auto careful) {
@@ -476,8 +496,8 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
     const int base = step * PAGED_STEP, next = step + KW;
     int64_t next_at[2] = {-1, -1};
     if (next < s1) {
-      next_at[0] = place(next * PAGED_STEP);
-      next_at[1] = place(next * PAGED_STEP + 16);
+      places(ahead, next, next_at);
+      ahead = pages(min(next + KW, steps - 1), n);
     }
     f32x4_t d[R][2];
 #pragma unroll
@@ -610,7 +630,7 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
   for (int r = 0; r < R; ++r) {
     const float l = over_row(sum[r], [](float x, float y) { return x + y; });
     const float mean = l == 0.f ? 0.f : 1.f / l;
-    const int64_t row = first + r * 16 + c;
+    const int row = first + r * 16 + c;
     if constexpr (KW == 1) {
       if (row < rows) {
 #pragma unroll
@@ -635,22 +655,21 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
       }
       __syncthreads();
       for (int x = tid; x < RW * 16 * (DP / 4); x += PAGED_WAVES * 64) {
-        const int d = x % (DP / 4) * 4, i = x / (DP / 4) % 16, of = x / (DP / 4) / 16 * KW;
-        const int64_t to = group_first + of / KW * (R * 16) + r * 16 + i;
+        const int d = x % (DP / 4) * 4, i = x / (DP / 4) % 16, of = x / (DP / 4) / 16;     // of: which of the waves side by side
+        const int to = group_first + of * (R * 16) + r * 16 + i;
         if (to >= rows) continue;
-        float w_top = PAGED_LOWEST, w_sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+        float w_top = PAGED_LOWEST, w_sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f}, weight[KW];
 #pragma unroll
-        for (int w = 0; w < KW; ++w) w_top = fmaxf(w_top, stats[of + w][i][0]);
-        float weight[KW];
+        for (int w = 0; w < KW; ++w) w_top = fmaxf(w_top, stats[of * KW + w][i][0]);
 #pragma unroll
         for (int w = 0; w < KW; ++w) {
-          weight[w] = stats[of + w][i][1] * fast_exp2(stats[of + w][i][0] - w_top);
+          weight[w] = stats[of * KW + w][i][1] * fast_exp2(stats[of * KW + w][i][0] - w_top);
           w_sum += weight[w];
         }
         const float inverse = w_sum == 0.f ? 0.f : 1.f / w_sum;
 #pragma unroll
         for (int w = 0; w < KW; ++w) {
-          const float4_t y = *reinterpret_cast<const float4_t*>(results + ((of + w) * 16 + i) * PITCH + d);
+          const float4_t y = *reinterpret_cast<const float4_t*>(results + ((of * KW + w) * 16 + i) * PITCH + d);
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[e] = fmaf(y[e], weight[w] * inverse, o[e]);
         }
@@ -660,28 +679,41 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
   }
 }
 
-// The splits' results of a row, in order, DP / 4 lanes to a row.
-template <typename T, int NB> __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
-  constexpr int DP = 32 * NB, LANES = DP / 4;
-  const int64_t to = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
-  if (to >= (int64_t)a.Bt * a.T * a.H) return;
-  const int d = threadIdx.x % LANES * 4;
+// The splits' results of a row.  DP / 4 lanes hold a row's elements; with many splits a workgroup's SIDE groups of lanes take every
+// SIDE-th one, and their results are put together in order (16 streams of 512 entries in 64 splits: 12 us in all, 24 with one group).
+template <typename T, int NB, int SIDE> __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
+  constexpr int DP = 32 * NB, LANES = DP / 4, ROWS = 256 / (LANES * SIDE);
+  __shared__ __align__(16) float part[SIDE > 1 ? 256 * 4 : 4];
+  const int lane = threadIdx.x % LANES, side = threadIdx.x / LANES % SIDE, d = lane * 4;
+  const int64_t to = (int64_t)blockIdx.x * ROWS + threadIdx.x / (LANES * SIDE);
   const int64_t token = to / a.H;
   const int b = (int)(token / a.T), t = (int)(token - (int64_t)b * a.T);
-  int m = a.n_new ? a.n_new[b] : a.T;
-  if (t >= m) return;
+  if (to >= (int64_t)a.Bt * a.T * a.H || t >= (a.n_new ? a.n_new[b] : a.T)) return;    // with SIDE > 1 ROWS is 1: the whole workgroup's
   const float* values = a.ws + to * a.n_splits * DP + d;
-  const float* stats = a.ws + (int64_t)a.Bt * a.T * a.H * a.n_splits * DP + to * a.n_splits * 2;
+  const float2_native* stats = reinterpret_cast<const float2_native*>(a.ws + (int64_t)a.Bt * a.T * a.H * a.n_splits * DP) + to * a.n_splits;
   float top = PAGED_LOWEST, sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < a.n_splits; ++s) top = fmaxf(top, stats[2 * s]);
-  for (int s = 0; s < a.n_splits; ++s) sum += stats[2 * s + 1] * fast_exp2(stats[2 * s] - top);
+#pragma unroll 8
+  for (int s = 0; s < a.n_splits; ++s) top = fmaxf(top, stats[s].x);
+#pragma unroll 8
+  for (int s = 0; s < a.n_splits; ++s) sum += stats[s].y * fast_exp2(stats[s].x - top);
   const float inverse = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll 4
-  for (int s = 0; s < a.n_splits; ++s) {
+  for (int s = side; s < a.n_splits; s += SIDE) {
     const float4_t y = *reinterpret_cast<const float4_t*>(values + (int64_t)s * DP);
-    const float w = stats[2 * s + 1] * fast_exp2(stats[2 * s] - top) * inverse;
+    const float w = stats[s].y * fast_exp2(stats[s].x - top) * inverse;
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = fmaf(y[e], w, o[e]);
+  }
+  if constexpr (SIDE > 1) {
+    *reinterpret_cast<float4_t*>(part + threadIdx.x * 4) = float4_t{o[0], o[1], o[2], o[3]};
+    __syncthreads();
+    if (side != 0) return;
+#pragma unroll
+    for (int s = 1; s < SIDE; ++s) {
+      const float4_t y = *reinterpret_cast<const float4_t*>(part + (s * LANES + lane) * 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += y[e];
+    }
   }
   if (d < a.pool.d_h) store_result4<T>((T*)a.out + to * a.pool.d_h, d, a.pool.d_h, a.out_pieces, o);
 }

@@ -4,15 +4,19 @@
 namespace photon {
 namespace {
 
-// Workgroups over the entries of a stream, and the fewest steps that are worth one.
+// Workgroups over the entries of a stream: as many as the chip holds at once (two a unit; one where a workgroup's registers fill it), but
+// none with fewer than two steps (wide: eight) a wave, and none where that leaves fewer than four: the merge is a launch.  Microseconds:
+// 16 streams of 2048 entries of 64 bf16 in 1, 2, 4, 8, 16 workgroups 19.9, 15.1, 11.4, 10.3, 11.0; of 512 in 1, 2, 4 8.5, 9.4, 8.4; 128 of 8192 in
+// 2, 4, 8 55, 46, 57; 32 of 32749 of 128 in 4, 8, 16 169, 101, 102; 256 rows over 128 streams of 4096 in 1, 2, 4 181, 128, 145.
 int paged_auto_splits(int Bt, int T, int H, int H_kv, int64_t S_max, bool f32_rows, photon_dtype kv_dt) {
   const int64_t rows = (int64_t)T * (H / H_kv);
   const PagedTile tile = paged_tile(rows, f32_rows, kv_dt);
   const int64_t groups = (int64_t)Bt * H_kv * ((rows + tile.rows() - 1) / tile.rows());
   const int64_t steps = (S_max + PAGED_STEP - 1) / PAGED_STEP;
-  int64_t splits = (tile.wide && tile.waves == 8 ? 256 : 512) / groups;
-  const int64_t most = tile.wide ? steps / 8 : steps * tile.waves / (4 * PAGED_WAVES);
+  int64_t splits = (tile.tiles == 1 ? 512 : 256) / groups;
+  const int64_t most = tile.wide ? steps / 8 : steps * tile.waves / (2 * PAGED_WAVES);
   splits = splits > most ? most : splits;
+  if (!tile.wide && most < 4) splits = 1;
   return (int)(splits < 1 ? 1 : splits > 256 ? 256 : splits);
 }
 int paged_most_splits(const photon_paged_cache* c, int Bt, int T, int H, int64_t S_max) {   // of either dtype of rows
@@ -20,10 +24,13 @@ int paged_most_splits(const photon_paged_cache* c, int Bt, int T, int H, int64_t
   return a > b ? a : b;
 }
 
+constexpr int MANY_SPLITS = 9;            // from which on a row's are merged by all lanes of a workgroup
+
 template <typename T, int NB> int32_t launch_merge(const PagedAttnArgs& a, hipStream_t st) {
   const int64_t rows = (int64_t)a.Bt * a.T * a.H;
   constexpr int per = 256 / (8 * NB);
-  PHOTON_LAUNCH(KC_COARSE_MERGE, st, (paged_merge_kernel<T, NB>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st, a);
+  if (a.n_splits >= MANY_SPLITS && rows <= (int64_t)0xffffffff / 256) PHOTON_LAUNCH(KC_COARSE_MERGE, st, (paged_merge_kernel<T, NB, per>), dim3((unsigned)rows), dim3(256), 0, st, a);
+  else PHOTON_LAUNCH(KC_COARSE_MERGE, st, (paged_merge_kernel<T, NB, 1>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st, a);
   return check_launch("paged_merge_kernel");
 }
 template <typename T> int32_t launch_merge_t(const PagedAttnArgs& a, hipStream_t st) {
@@ -84,8 +91,9 @@ extern "C" int32_t photon_paged_attn(const photon_paged_cache* cache, const void
   a.q_stride = q_stride; a.S_max = (int32_t)S_max; a.Bt = Bt; a.T = T; a.H = H; a.group = H / cache->H_kv; a.n_splits = n_splits;
   const int64_t rows = (int64_t)T * a.group;
   const PagedTile tile = paged_tile(rows, f32, cache->kv_dt);
+  PHOTON_REQUIRE(rows <= PAGED_MOST_ROWS, PHOTON_ERR_UNSUPPORTED, "%s: T=%d queries of %d heads a K/V head are too many", __func__, T, a.group);
   const int64_t groups = (rows + tile.rows() - 1) / tile.rows(), units = (int64_t)Bt * cache->H_kv * n_splits;
-  PHOTON_REQUIRE((units + 7) * groups <= (int64_t)0xffffffff / 512, PHOTON_ERR_UNSUPPORTED,
+  PHOTON_REQUIRE((units + 7) * groups <= (int64_t)0xffffffff / 512 && (int64_t)Bt * T * H <= (int64_t)0xffffffff / 32, PHOTON_ERR_UNSUPPORTED,
                  "%s: Bt=%d, T=%d, H=%d, n_splits=%d are too many workgroups", __func__, Bt, T, H, n_splits);
   a.row_groups = (int32_t)groups; a.units = (int32_t)units;
   a.scale_log2e = scale * LOG2E;

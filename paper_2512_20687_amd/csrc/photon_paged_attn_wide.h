@@ -47,19 +47,17 @@ template <int NB, int WAVES, int PAGES> __global__ __launch_bounds__(WAVES * 64,
   int row_group, hk, split, b;
   if (!paged_unit(a, row_group, hk, split, b)) return;
   int n, m, past;
-  paged_sequence(a, b, n, m, past);
-  const int64_t rows = (int64_t)m * a.group;
-  const int64_t group_first = (int64_t)row_group * (WAVES * R * 16), first = group_first + wave * (R * 16);
+  paged_sequence(a, paged_counts(a, b), n, m, past);
+  const int rows = m * a.group, group_first = row_group * (WAVES * R * 16), first = group_first + wave * (R * 16);
   if (group_first >= rows) return;
-  const int64_t group_last = min(group_first + WAVES * R * 16, rows) - 1, last = min(first + R * 16, rows) - 1;
-  const int hi = a.tree ? n : min(n, past + (int)(group_last / a.group) + 1);
+  const int group_last = min(group_first + WAVES * R * 16, rows) - 1, last = min(first + R * 16, rows) - 1;
+  const int hi = a.tree ? n : min(n, past + group_last / a.group + 1);
   const int stages = hi <= 0 ? 0 : (hi + WIDE_STAGE - 1) / WIDE_STAGE;
   const int s0 = (int)((int64_t)stages * split / a.n_splits), s1 = (int)((int64_t)stages * (split + 1) / a.n_splits);
   const bool has_rows = first < rows;
-  const int wave_hi = !has_rows ? 0 : a.tree ? n : min(n, past + (int)(last / a.group) + 1);
+  const int wave_hi = !has_rows ? 0 : a.tree ? n : min(n, past + last / a.group + 1);
 
   PagedRows<bf16_t, bf16_t, NB, R> q;
-  q.load(a, b, hk, first, rows, c, g);
   float top[R], sum[R];
   f32x4_t acc[R][TILES];
 #pragma unroll
@@ -133,26 +131,35 @@ template <int NB, int WAVES, int PAGES> __global__ __launch_bounds__(WAVES * 64,
     uint32_t k_at = k_first;
     asm volatile("" : "+v"(k_at));                                           // an exclusive-or a read, not a register for each over the whole loop
     f32x4_t d[R][4];
-    // A tile's operands are requested a tile ahead: the compiler, left to itself, reads each right before its use.
+    // Two tiles side by side: a product whose sum the next but one continues waits for it, of four sums none does.  Operands of the
+    // next two are requested as those of these are used up: the compiler, left to itself, reads each right before its use.
     uint4_t key[2][NB];
-    auto read_keys = [&](int i) {
+    auto read_keys = [&](int i, int f) {
 #pragma unroll
-      for (int f = 0; f < NB; ++f) key[i & 1][f] = *reinterpret_cast<const uint4_t*>(in + i * 16 * ROW + (k_at ^ (64 * f)));
+      for (int t = 0; t < 2; ++t) key[t][f] = *reinterpret_cast<const uint4_t*>(in + (i + t) * 16 * ROW + (k_at ^ (64 * f)));
     };
-    read_keys(0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (i < 3) read_keys(i + 1);
-      request(i);
-      __builtin_amdgcn_sched_barrier(0);
+    for (int f = 0; f < NB; ++f) read_keys(0, f);
 #pragma unroll
-      for (int r = 0; r < R; ++r) d[r][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < 4; i += 2) {
 #pragma unroll
-      for (int f = 0; f < NB; ++f)
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int r = 0; r < R; ++r) d[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(key[i & 1][f]), q.operand(r, 0, f), d[r][i], 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
+        for (int r = 0; r < R; ++r) d[r][i + t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int f = 0; f < NB; ++f) {
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+            d[r][i + t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(key[t][f]), q.operand(r, 0, f), d[r][i + t], 0, 0, 0);
+        if (i == 0) read_keys(2, f);
+        if (f % 2 == 0 && f / 2 < 2) request(i + f / 2);
+      }
+      if (NB < 4) request(i + 1);
     }
+    __builtin_amdgcn_sched_barrier(0);
     settle(d);
     if constexpr (CAREFUL) {
       const bool there[4] = {(now & 1) != 0, (now & 2) != 0, (now & 4) != 0, (now & 8) != 0};
@@ -206,45 +213,53 @@ template <int NB, int WAVES, int PAGES> __global__ __launch_bounds__(WAVES * 64,
         p[r][0] = as_bf16x8(high);
         p[r][1] = as_bf16x8(low);
       }
-      constexpr int AHEAD = 2;                                               // operands requested ahead
-      uint4_t ahead[AHEAD];
+      constexpr int SIDE = 2;                                                // operands side by side, as above, and as many requested ahead
+      uint4_t ahead[SIDE];
       auto read_values = [&](int j) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const uint2v_t w = __builtin_bit_cast(uint2v_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t)(values + i * 16 * ROW + (v_at ^ (32 * j)))));
-          ahead[j % AHEAD][2 * i] = w[0];
-          ahead[j % AHEAD][2 * i + 1] = w[1];
-        }
+        for (int t = 0; t < SIDE; ++t)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint2v_t w = __builtin_bit_cast(uint2v_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t)(values + i * 16 * ROW + (v_at ^ (32 * (j + t))))));
+            ahead[t][2 * i] = w[0];
+            ahead[t][2 * i + 1] = w[1];
+          }
       };
+      read_values(0);
 #pragma unroll
-      for (int j = 0; j < AHEAD && j < TILES; ++j) read_values(j);
+      for (int j = 0; j < TILES; j += SIDE) {
+        uint4_t value[SIDE];
 #pragma unroll
-      for (int j = 0; j < TILES; ++j) {
-        uint4_t value = ahead[j % AHEAD];
-        if (j + AHEAD < TILES) read_values(j + AHEAD);
+        for (int t = 0; t < SIDE; ++t) value[t] = ahead[t];
+        if (j + SIDE < TILES) read_values(j + SIDE);
         __builtin_amdgcn_sched_barrier(6);                                   // arithmetic may pass
         if constexpr (CAREFUL) {
-          value &= keep;
-          if (some) {
 #pragma unroll
-            for (int r = 0; r < R; ++r)
-              add_unbounded(acc[r][j], __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(unbounded_codes(value)), as_bf16x8(seen_operand(seen[r] >> (8 * half))),
-                                                                               f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0));
+          for (int t = 0; t < SIDE; ++t) {
+            value[t] &= keep;
+            if (some) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) value[i] = without_unbounded<bf16_t>(value[i]);
+              for (int r = 0; r < R; ++r)
+                add_unbounded(acc[r][j + t], __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(unbounded_codes(value[t])), as_bf16x8(seen_operand(seen[r] >> (8 * half))),
+                                                                                     f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0));
+#pragma unroll
+              for (int i = 0; i < 4; ++i) value[t][i] = without_unbounded<bf16_t>(value[t][i]);
+            }
           }
         }
 #pragma unroll
         for (int part = 1; part >= 0; --part)
 #pragma unroll
-          for (int r = 0; r < R; ++r) acc[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(value), p[r][part], acc[r][j], 0, 0, 0);
+          for (int t = 0; t < SIDE; ++t)
+#pragma unroll
+            for (int r = 0; r < R; ++r) acc[r][j + t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(value[t]), p[r][part], acc[r][j + t], 0, 0, 0);
       }
     }
   };
 
   // Stages that every row of the workgroup sees whole come first; from the first other one on, all steps are taken with care.  Code of
   // both in one loop would cost the ordinary steps their registers.
-  const int group_sees = a.tree ? past : past + (int)(group_first / a.group) + 1;
+  const int group_sees = a.tree ? past : past + group_first / a.group + 1;
   Pages ahead = pages(s0);
   Places next = places(ahead, s0);
   uint32_t now = next.there;
@@ -254,6 +269,7 @@ template <int NB, int WAVES, int PAGES> __global__ __launch_bounds__(WAVES * 64,
 #pragma unroll
     for (int u = 0; u < PER; ++u) load_in(next, 0, u);
   }
+  q.load(a, b, hk, first, c, g);                                        // behind the first stage's requests: one latency for both
   int k_buffer = 0, v_buffer = 0;                                            // this stage's
   auto begin = [&]() {                                                       // this stage is there, and what it is not to use no longer read
     next = places(ahead, stage + 1);
@@ -317,7 +333,7 @@ template <int NB, int WAVES, int PAGES> __global__ __launch_bounds__(WAVES * 64,
   for (int r = 0; r < R; ++r) {
     const float l = over_row(sum[r], [](float x, float y) { return x + y; });
     const float mean = l == 0.f ? 0.f : 1.f / l;
-    const int64_t row = first + r * 16 + c;
+    const int row = first + r * 16 + c;
     if (row >= rows) continue;
     const int64_t to = paged_row(a, b, hk, row);
 #pragma unroll
