@@ -485,6 +485,7 @@ class PagedCache:
         self._c = _PagedCache(k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), shape[0], shape[2], page_table.shape[1], shape[1], d_h,
                               _dt(k_pages))
         self._ref = C.byref(self._c)
+        self._lib = load_library()
 
 
 def _paged_status(status: Optional[torch.Tensor]) -> Optional[int]:
@@ -495,12 +496,11 @@ def _paged_status(status: Optional[torch.Tensor]) -> Optional[int]:
     return status.data_ptr()
 
 
-def _paged_rows(t: torch.Tensor, Bt: int, d_h: int, name: str) -> int:
+def _paged_rows(t: torch.Tensor, shape, Bt: int, d_h: int, name: str) -> int:
     """The stride of rows [Bt, T, heads, d_h] in fp32 or bf16."""
-    shape = t.shape
     if len(shape) != 4 or shape[0] != Bt or shape[3] != d_h or (t.dtype is not torch.float32 and t.dtype is not torch.bfloat16):
         raise PhotonError(-1, f"{name} must be fp32 or bf16 rows [{Bt}, T, heads, {d_h}], not {tuple(shape)} {t.dtype}")
-    return _mx_row_stride(t)
+    return shape[2] * d_h if t.is_contiguous() else _mx_row_stride(t)
 
 
 def photon_paged_cache_write(k, v, cache: PagedCache, start=None, n_new=None, position=None, q=None, q_out=None, rope_theta: float = 0.0,
@@ -508,36 +508,38 @@ def photon_paged_cache_write(k, v, cache: PagedCache, start=None, n_new=None, po
     """Rows k, v [Bt, T, H_kv, d_h] (views of a wider matrix included) become the entries start[b] .. of the cache, K rotated to its
     position (int32 [Bt, T], or the entry's own number); q [Bt, T, H, d_h] is rotated into q_out.  start, n_new int32 [Bt] or None
     (0, T); status: int32 word that receives PHOTON_STATUS_CACHE_FULL and _BAD_PAGE."""
-    Bt, d_h, dtype = cache.Bt, cache.d_h, k.dtype
-    stride = _paged_rows(k, Bt, d_h, "k")
-    T = k.shape[1]
-    if v.shape != k.shape or v.dtype is not dtype or k.shape[2] != cache.H_kv:
+    Bt, d_h, dtype, shape = cache.Bt, cache.d_h, k.dtype, k.shape
+    stride = _paged_rows(k, shape, Bt, d_h, "k")
+    T = shape[1]
+    if v.shape != shape or v.dtype is not dtype or shape[2] != cache.H_kv:
         raise PhotonError(-1, f"k and v must be rows of {cache.H_kv} heads of one dtype")
-    if v.stride() != k.stride() and _mx_row_stride(v) != stride:
+    if _paged_rows(v, shape, Bt, d_h, "v") != stride:
         raise PhotonError(-1, f"k and v rows must have one stride: {stride} and {_mx_row_stride(v)}")
     if (q is None) != (q_out is None):
         raise PhotonError(-1, "q and q_out go together")
-    H, q_stride, out_stride = 0, 0, 0
+    H, q_stride, out_stride, q_at, out_at = 0, 0, 0, None, None
     if q is not None:
-        if q.dtype is not dtype or q_out.dtype is not dtype or q_out.shape != q.shape or q.shape[1] != T:
+        q_shape = q.shape
+        if q.dtype is not dtype or q_out.dtype is not dtype or q_out.shape != q_shape or len(q_shape) != 4 or q_shape[1] != T:
             raise PhotonError(-1, "q and q_out must be rows [Bt, T, H, d_h] of k's dtype")
-        H, q_stride, out_stride = q.shape[2], _paged_rows(q, Bt, d_h, "q"), _paged_rows(q_out, Bt, d_h, "q_out")
+        H, q_stride, out_stride = q_shape[2], _paged_rows(q, q_shape, Bt, d_h, "q"), _paged_rows(q_out, q_shape, Bt, d_h, "q_out")
+        q_at, out_at = q.data_ptr(), q_out.data_ptr()
     if position is not None and (position.dtype is not torch.int32 or tuple(position.shape) != (Bt, T) or not position.is_contiguous()):
         raise PhotonError(-1, f"position must be a contiguous int32 tensor [{Bt}, {T}]")
-    _mx_call(load_library().photon_paged_cache_write, (k, v, *cache._tensors, q, q_out, start, n_new, position, status), cache._ref, k.data_ptr(),
-             v.data_ptr(), stride, None if q is None else q.data_ptr(), q_stride, None if q is None else q_out.data_ptr(), out_stride,
-             _mx_counts(start, Bt, "start"), _mx_counts(n_new, Bt, "n_new"), None if position is None else position.data_ptr(),
-             _paged_status(status), Bt, T, H, rope_theta, PHOTON_F32 if dtype is torch.float32 else PHOTON_BF16)
+    _mx_call(cache._lib.photon_paged_cache_write, (k, v, *cache._tensors, q, q_out, start, n_new, position, status), cache._ref, k.data_ptr(),
+             v.data_ptr(), stride, q_at, q_stride, out_at, out_stride, _mx_counts(start, Bt, "start"), _mx_counts(n_new, Bt, "n_new"),
+             None if position is None else position.data_ptr(), _paged_status(status), Bt, T, H, rope_theta,
+             PHOTON_F32 if dtype is torch.float32 else PHOTON_BF16)
 
 
 def photon_paged_cache_move(cache: PagedCache, start, source, n=None, status=None) -> None:
     """Entry start[b] + i of every sequence becomes what entry start[b] + source[b, i] was, i < n[b]; source int32 [Bt, T], T <= 64;
     start, n int32 [Bt] or None (0, T)."""
-    Bt = cache.Bt
-    if source.dtype is not torch.int32 or source.dim() != 2 or source.shape[0] != Bt or not source.is_contiguous():
+    Bt, shape = cache.Bt, source.shape
+    if source.dtype is not torch.int32 or len(shape) != 2 or shape[0] != Bt or not source.is_contiguous():
         raise PhotonError(-1, f"source must be a contiguous int32 tensor [{Bt}, T]")
-    _mx_call(load_library().photon_paged_cache_move, (source, *cache._tensors, start, n, status), cache._ref, _mx_counts(start, Bt, "start"),
-             source.data_ptr(), _mx_counts(n, Bt, "n"), _paged_status(status), Bt, source.shape[1])
+    _mx_call(cache._lib.photon_paged_cache_move, (source, *cache._tensors, start, n, status), cache._ref, _mx_counts(start, Bt, "start"),
+             source.data_ptr(), _mx_counts(n, Bt, "n"), _paged_status(status), Bt, shape[1])
 
 
 def photon_paged_attn_workspace_bytes(cache: PagedCache, Bt: int, T: int, H: int, S_max: Optional[int] = None, n_splits: int = 0) -> int:
@@ -548,16 +550,16 @@ def photon_paged_attn(q, cache: PagedCache, seq_len, out, n_new=None, tree=None,
                       n_splits: int = 0, workspace: Optional[torch.Tensor] = None, status=None):
     """q (rows one stride apart), out (contiguous) [Bt, T, H, d_h] fp32 or bf16; seq_len int32 [Bt], the T (n_new[b]) queries' own
     entries counted; tree int64 [Bt, T]: bit j of a query's word where it sees own entry j (None: those up to its own); returns out."""
-    Bt, d_h, dtype = cache.Bt, cache.d_h, q.dtype
-    stride = _paged_rows(q, Bt, d_h, "q")
-    if out.shape != q.shape or out.dtype is not dtype or not out.is_contiguous():
+    Bt, d_h, dtype, shape = cache.Bt, cache.d_h, q.dtype, q.shape
+    stride = _paged_rows(q, shape, Bt, d_h, "q")
+    if out.shape != shape or out.dtype is not dtype or not out.is_contiguous():
         raise PhotonError(-1, "out must be contiguous, of q's shape and dtype")
-    T, H = q.shape[1:3]
+    T, H = shape[1], shape[2]
     if seq_len is None or (workspace is not None and not workspace.is_contiguous()):
         raise PhotonError(-1, "seq_len is missing, or workspace is not contiguous")
     if tree is not None and (tree.dtype is not torch.int64 or tuple(tree.shape) != (Bt, T) or not tree.is_contiguous()):
         raise PhotonError(-1, f"tree must be a contiguous int64 tensor [{Bt}, {T}]")
-    _mx_call(load_library().photon_paged_attn, (q, *cache._tensors, seq_len, n_new, tree, out, workspace, status), cache._ref, q.data_ptr(), stride,
+    _mx_call(cache._lib.photon_paged_attn, (q, *cache._tensors, seq_len, n_new, tree, out, workspace, status), cache._ref, q.data_ptr(), stride,
              _mx_counts(seq_len, Bt, "seq_len"), _mx_counts(n_new, Bt, "n_new"), None if tree is None else tree.data_ptr(), out.data_ptr(),
              _paged_status(status), Bt, T, H, cache.S_max if S_max is None else S_max, 1.0 / math.sqrt(d_h) if scale is None else scale, n_splits,
              None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel() * workspace.element_size(),

@@ -97,10 +97,33 @@ __global__ __launch_bounds__(256) void paged_write_kernel(WriteArgs a, RopeTable
   __shared__ float2_native angle[ROPE_ROWS][MOST_PAIRS];
   __shared__ int64_t place[ROPE_ROWS];                                       // byte offset of the entry of head 0; -1: none
   const int b = blockIdx.z, tid = threadIdx.x, t0 = blockIdx.x * a.rows;
+  const int pieces = a.half / VEC, x = blockIdx.y * blockDim.x + tid;
+  const int q_heads = a.q ? a.H : 0, H_kv = a.pool.H_kv, d_h = a.pool.d_h, heads = q_heads + 2 * H_kv;
+  const int head = min(x / pieces, heads - 1), c = (x - x / pieces * pieces) * VEC;         // threads behind the last head only help with the table
+  const int kind = head < q_heads ? 0 : head < q_heads + H_kv ? 1 : 2;       // q, K, V
+  const int h = kind == 0 ? head : kind == 1 ? head - q_heads : head - q_heads - H_kv;
+  const int64_t stride = kind == 0 ? a.q_stride : a.row_stride;
+  const T* from = (const T*)(kind == 0 ? a.q : kind == 1 ? a.k : a.v) + ((int64_t)b * a.T + t0) * stride + (int64_t)h * d_h + c;
+  const bool pair = c + a.half < d_h;                                        // an odd head's last element has no partner
+  constexpr int AT_ONCE = 4;                                                 // rows in flight
+  float lo[AT_ONCE][VEC], hi[AT_ONCE][VEC];
+  auto request = [&](int r0, int rows) {
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const int r = min(r0 + u, rows - 1);
+      load_piece<T, VEC>(from + r * stride, lo[u]);
+      load_piece<T, VEC>(from + r * stride + (pair ? a.half : 0), hi[u]);
+    }
+  };
+  // The first rows are on their way while places and angles are found out, and counts, too, where most workgroups will have rows (64
+  // prompts of 1 .. 133 rows: 42 us, 53 with all of the padding's rows requested).
+  const bool early = a.n_new == nullptr || a.T <= AT_ONCE;
+  if (early) request(0, min(a.rows, a.T - t0));
   int m = a.n_new ? a.n_new[b] : a.T;
   m = m < 0 ? 0 : m > a.T ? a.T : m;
   const int rows = min(a.rows, m - t0);
   if (rows <= 0) return;
+  if (!early) request(0, rows);
   const int start = a.start ? a.start[b] : 0;
   if (tid < rows) {
     const int64_t entry = (int64_t)start + t0 + tid;
@@ -117,39 +140,25 @@ __global__ __launch_bounds__(256) void paged_write_kernel(WriteArgs a, RopeTable
     if (bad && a.status && blockIdx.y == 0) atomicOr(a.status, bad);
   }
   if (a.rotate) {
-    for (int x = tid; x < rows * a.half; x += blockDim.x) {
-      const int r = x / a.half, i = x - r * a.half;
+    for (int y = tid; y < rows * a.half; y += blockDim.x) {
+      const int r = y / a.half, i = y - r * a.half;
       const int position = a.position ? a.position[(int64_t)b * a.T + t0 + r] : (int)((uint32_t)start + t0 + r);
       const uint64_t phase = (uint64_t)(int64_t)position * rope.turns[i];
       // the nearest quarter turn is taken off before the phase becomes a float: what is left is at most an eighth
       const uint32_t turn = (uint32_t)(phase >> 32), quarter = (turn + 0x20000000u) >> 30;
-      float s, c;
-      sincospif((float)(int32_t)(turn - (quarter << 30)) * 0x1p-31f, &s, &c);
-      const float cs = quarter & 1 ? -s : c, sn = quarter & 1 ? c : s;
-      angle[r][i] = quarter & 2 ? float2_native{-cs, -sn} : float2_native{cs, sn};
+      float sn, cs;
+      sincospif((float)(int32_t)(turn - (quarter << 30)) * 0x1p-31f, &sn, &cs);
+      const float co = quarter & 1 ? -sn : cs, si = quarter & 1 ? cs : sn;
+      angle[r][i] = quarter & 2 ? float2_native{-co, -si} : float2_native{co, si};
     }
   }
   __syncthreads();
-  const int pieces = a.half / VEC, x = blockIdx.y * blockDim.x + tid;
-  const int head = x / pieces, c = (x - head * pieces) * VEC;
-  const int q_heads = a.q ? a.H : 0, H_kv = a.pool.H_kv, d_h = a.pool.d_h;
-  if (head >= q_heads + 2 * H_kv) return;
-  const int kind = head < q_heads ? 0 : head < q_heads + H_kv ? 1 : 2;       // q, K, V
-  const int h = kind == 0 ? head : kind == 1 ? head - q_heads : head - q_heads - H_kv;
-  const int64_t stride = kind == 0 ? a.q_stride : a.row_stride;
-  const T* from = (const T*)(kind == 0 ? a.q : kind == 1 ? a.k : a.v) + ((int64_t)b * a.T + t0) * stride + (int64_t)h * d_h + c;
+  if (x / pieces >= heads) return;
   T* q_to = (T*)a.q_out + ((int64_t)b * a.T + t0) * a.q_out_stride + (int64_t)h * d_h + c;
   uint8_t* pool = (kind == 1 ? a.pool.k : a.pool.v) + h * a.pool.head_bytes;
-  const bool pair = c + a.half < d_h;                                        // an odd head's last element has no partner
-  constexpr int AT_ONCE = 4;                                                 // rows in flight
+  const int d_p = a.pool.row_bytes / (int)sizeof(KV);
   for (int r0 = 0; r0 < rows; r0 += AT_ONCE) {
-    float lo[AT_ONCE][VEC], hi[AT_ONCE][VEC];
-#pragma unroll
-    for (int u = 0; u < AT_ONCE; ++u) {
-      const int r = min(r0 + u, rows - 1);
-      load_piece<T, VEC>(from + r * stride, lo[u]);
-      load_piece<T, VEC>(from + r * stride + (pair ? a.half : 0), hi[u]);
-    }
+    if (r0 > 0) request(r0, rows);
 #pragma unroll
     for (int u = 0; u < AT_ONCE; ++u) {
       const int r = r0 + u;
@@ -169,7 +178,6 @@ __global__ __launch_bounds__(256) void paged_write_kernel(WriteArgs a, RopeTable
         store_piece<KV, VEC>(to + c, lo[u]);
         if (pair) store_piece<KV, VEC>(to + c + a.half, hi[u]);
         // the columns behind a head's elements: VEC divides 32 and, where it is not 1, d_h
-        const int d_p = a.pool.row_bytes / (int)sizeof(KV);
         const float zero[VEC] = {};
         for (int e = d_h + c; e < d_p; e += pieces * VEC) store_piece<KV, VEC>(to + e, zero);
       }
@@ -293,10 +301,18 @@ extern "C" int32_t photon_paged_cache_write(const photon_paged_cache* cache, con
   a.T = T; a.H = q ? H : 0; a.rows = 1; a.half = (d_h + 1) / 2; a.rotate = rope_theta != 0.f;
   RopeTable rope;
   if (a.rotate) {
-    // theta^(-2i/d_h) / (2 pi): products in extended precision, within 2^-29 turns of the angle at every 32-bit position
+    // theta^(-2i/d_h) / (2 pi) as fractions of 2^128, one a product of the one before with theta^(-2/d_h) as a fraction of 2^64, which is
+    // within 2^-65: within 2^-29 turns of the angle at every 32-bit position.
     const long double ratio = powl((long double)rope_theta, -2.0L / d_h);
-    long double f = 0.15915494309189533576888376337251436L;
-    for (int i = 0; i < a.half; ++i, f *= ratio) rope.turns[i] = (uint64_t)ldexpl(f, 64);
+    const uint64_t r = ratio < 1.0L ? (uint64_t)ldexpl(ratio, 64) : 0;       // 0: all alike
+    uint64_t high = 0x28be60db9391054aull, low = 0x7f09d5f47d4d3770ull;      // 1 / (2 pi)
+    for (int i = 0; i < a.half; ++i) {
+      rope.turns[i] = high + (low >> 63);
+      if (r == 0) continue;
+      const unsigned __int128 next = (unsigned __int128)high * r + (uint64_t)(((unsigned __int128)low * r) >> 64);
+      high = (uint64_t)(next >> 64);
+      low = (uint64_t)next;
+    }
   }
   // Elements of a piece: they divide half a head (so pairs are whole pieces) and are aligned in every row that a piece is read from.
   const auto whole = [&](int vec) {

@@ -1,0 +1,156 @@
+"""Attention over the paged K/V cache where many rows share a K/V head (bf16 rows and pages take entries through LDS there), and what all
+of its kernels have to survive: pages that are not there, far scores, large values, scales of any kind, more splits than steps.
+
+Tolerances as in tests/test_gpu_paged_attn.py."""
+import numpy as np
+import pytest
+import torch
+
+import paged_plain as plain
+from test_gpu_paged_attn import BAD_PAGE, KV, check, filled, i32, i64, trees
+from util import require_gpu
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ph():
+    require_gpu()
+    import paper_2512_20687_amd as m
+    m.load_library()
+    return m
+
+
+def attend(ph, q, cache, lengths, splits=1, **kw):
+    Bt, T, H, _ = q.shape
+    out = torch.full_like(q, 5.0)
+    ws = torch.full((ph.photon_paged_attn_workspace_bytes(cache, Bt, T, H, None, splits) + 16,), 255, dtype=torch.uint8, device="cuda")
+    ph.photon_paged_attn(q, cache, i32(lengths), out, n_splits=splits, workspace=ws, **kw)
+    return out
+
+
+def queries(rng, shape, rows):
+    return torch.from_numpy(rng.standard_normal(shape).astype(np.float32)).to(rows).cuda()
+
+
+@pytest.mark.parametrize("P", [16, 32, 64, 256])
+@pytest.mark.parametrize("d_h", [20, 64, 100, 128])
+@pytest.mark.parametrize("T,H,H_kv,new,tree", [(66, 2, 2, [66, 40], False), (130, 4, 2, [130, 127], False), (33, 4, 1, [33, 17], False), (64, 4, 1, [64, 35], True), (40, 8, 1, [40, 39], True)])
+def test_many_rows(ph, P, d_h, T, H, H_kv, new, tree):
+    """65 rows to 320, workgroups with waves that have none, entries that end inside a stage, pages smaller and larger than one."""
+    rng = np.random.default_rng(P + d_h + T)
+    lengths = [new[0] + 217, new[1]]
+    table, n_pages = plain.table_of(rng, lengths, P)
+    pools = [filled(rng, n_pages, H_kv, d_h, P, "bf16", table, lengths) for _ in range(2)]
+    cache = ph.PagedCache(pools[0].cuda(), pools[1].cuda(), i32(table), d_h)
+    q = queries(rng, (2, T, H, d_h), torch.bfloat16)
+    masks = trees(rng, 2, T) if tree else None
+    for splits in (1, 2, 5):
+        check(attend(ph, q, cache, lengths, splits, n_new=i32(new), tree=i64(masks)), q, pools, table, lengths, new, d_h, masks, fill=5.0)
+
+
+@pytest.mark.parametrize("rows,kv", [(torch.bfloat16, "bf16"), (torch.float32, "bf16"), (torch.bfloat16, "e4m3"), (torch.float32, "f32")])
+@pytest.mark.parametrize("T,H,H_kv,P", [(1, 4, 2, 16), (9, 4, 2, 32), (48, 4, 2, 16), (48, 4, 2, 64), (150, 2, 1, 64), (150, 2, 1, 16)])
+def test_pages_that_are_missing_along_a_sequence(ph, rows, kv, T, H, H_kv, P):
+    """Missing pages at the beginning, in the middle, among the queries' own entries: skipped, and everything behind them is seen."""
+    rng = np.random.default_rng(T + P)
+    d_h, n = 64, 600
+    table, n_pages = plain.table_of(rng, [n], P)
+    pools = [filled(rng, n_pages, H_kv, d_h, P, kv, table, [n]) for _ in range(2)]
+    wrong = table.copy()
+    pages = (n + P - 1) // P
+    for at, page in ((0, -1), (pages // 2, n_pages), (pages // 2 + 1, 2 ** 31 - 1), (pages - 2, -(2 ** 31))):
+        wrong[0, at] = page
+    cache = ph.PagedCache(pools[0].cuda(), pools[1].cuda(), i32(wrong), d_h)
+    q = queries(rng, (1, T, H, d_h), rows)
+    there = np.repeat((wrong[0] >= 0) & (wrong[0] < n_pages), P)[:n]
+    k, v = (plain.entries(plain.values(p), table[0], n, d_h) for p in pools)
+    x = q.float().cpu().numpy()
+    for splits in (1, 3):
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        out = attend(ph, q, cache, [n], splits, status=status).float().cpu().numpy()
+        assert int(status) == BAD_PAGE
+        for t in range(0, T, 7):
+            ref, size = plain.attended(x[0, t], k, v, plain.seen(n, T, t) & there, d_h ** -0.5)
+            bound = 1e-5 * max(size.max(), 1e-30) if rows == torch.float32 else 2.0 ** -8 * np.abs(ref) + 2.0 ** -15 * size
+            assert (np.abs(out[0, t] - ref) <= bound).all(), t
+    # no page at all: zeros
+    none = ph.PagedCache(pools[0].cuda(), pools[1].cuda(), i32(np.full_like(table, -1)), d_h)
+    assert not attend(ph, q, none, [n], 2).any()
+
+
+@pytest.mark.parametrize("rows,kv", [(torch.bfloat16, "bf16"), (torch.float32, "bf16"), (torch.float32, "f32"), (torch.bfloat16, "e4m3")])
+@pytest.mark.parametrize("T", [1, 20, 70])
+@pytest.mark.parametrize("scale", [0.0, -0.3, 1.0, 2.5])
+def test_scales(ph, rows, kv, T, scale):
+    rng = np.random.default_rng(T)
+    d_h, lengths = 32, [300]
+    table, n_pages = plain.table_of(rng, lengths, 16)
+    pools = [filled(rng, n_pages, 1, d_h, 16, kv, table, lengths) for _ in range(2)]
+    cache = ph.PagedCache(pools[0].cuda(), pools[1].cuda(), i32(table), d_h)
+    q = queries(rng, (1, T, 1, d_h), rows)
+    for splits in (1, 3):
+        check(attend(ph, q, cache, lengths, splits, scale=scale), q, pools, table, lengths, [T], d_h, scale=scale)
+
+
+@pytest.mark.parametrize("rows,kv", [(torch.bfloat16, "bf16"), (torch.float32, "bf16"), (torch.float32, "f32")])
+@pytest.mark.parametrize("T", [3, 70])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_far_scores(ph, rows, kv, T, sign):
+    """Scores of 10^30 of either sign that rise along the sequence: the greatest one's V, and no NaN.  Neighbours are 2^-7 of 10^30 apart."""
+    n, d_h = 200, 64
+    k = torch.zeros((13, 1, 16, d_h))
+    k[..., 0] = sign * (1 + torch.arange(13 * 16).reshape(13, 1, 16) // 4 * 4 / 128.0)
+    v = torch.randn((13, 1, 16, d_h), generator=torch.Generator().manual_seed(1)).to(KV[kv])
+    q = torch.zeros((1, T, 1, d_h))
+    q[..., 0] = 1e30
+    table = np.arange(13, dtype=np.int32)[None]
+    cache = ph.PagedCache(k.to(KV[kv]).cuda(), v.cuda(), i32(table), d_h)
+    out = attend(ph, q.to(rows).cuda(), cache, [n], 1)
+    ks, vs = (plain.entries(plain.values(p), table[0], n, d_h) for p in (k.to(KV[kv]), v))
+    for t in (0, T - 1):
+        ref, a = plain.attended(q[0, t].to(rows).float().numpy(), ks, vs, plain.seen(n, T, t), d_h ** -0.5)
+        bound = 2.0 ** -14 * a + (0 if rows == torch.float32 else 2.0 ** -8 * np.abs(ref))
+        assert (np.abs(out[0, t].float().cpu().numpy() - ref) <= bound).all(), t
+
+
+@pytest.mark.parametrize("rows,kv", [(torch.bfloat16, "bf16"), (torch.float32, "bf16"), (torch.float32, "f32")])
+@pytest.mark.parametrize("T", [1, 17, 70])
+def test_large_values(ph, rows, kv, T):
+    """V whose absolute sum is near fp32's end, 150 entries of up to 2^120.8: finite, and as exact as elsewhere."""
+    rng = np.random.default_rng(T)
+    d_h, lengths = 64, [150]
+    table, n_pages = plain.table_of(rng, lengths, 32)
+    pools = [filled(rng, n_pages, 1, d_h, 32, kv, table, lengths) for _ in range(2)]
+    pools[1] = (pools[1].float() * 2.0 ** 118.5).to(KV[kv])
+    cache = ph.PagedCache(pools[0].cuda(), pools[1].cuda(), i32(table), d_h)
+    q = queries(rng, (1, T, 1, d_h), rows)
+    for splits in (1, 2):
+        check(attend(ph, q, cache, lengths, splits), q, pools, table, lengths, [T], d_h)
+
+
+def test_more_splits_than_steps(ph):
+    rng = np.random.default_rng(3)
+    lengths = [70, 1, 0]
+    for rows, kv, T in ((torch.bfloat16, "bf16", 1), (torch.float32, "f32", 3), (torch.bfloat16, "bf16", 70)):
+        new = [T, 1, 1]
+        table, n_pages = plain.table_of(rng, [max(n, 1) for n in lengths], 16)
+        pools = [filled(rng, n_pages, 2, 64, 16, kv, table, lengths) for _ in range(2)]
+        cache = ph.PagedCache(pools[0].cuda(), pools[1].cuda(), i32(table), 64)
+        q = queries(rng, (3, T, 4, 64), rows)
+        for splits in (8, 9, 100, 1024):
+            check(attend(ph, q, cache, lengths, splits, n_new=i32(new)), q, pools, table, lengths, new, 64, fill=5.0)
+
+
+def test_a_longer_bound_changes_no_bit_of_one_split(ph):
+    """S_max bounds the lengths: it chooses splits, nothing else."""
+    rng = np.random.default_rng(5)
+    lengths = [333, 20]
+    table, n_pages = plain.table_of(rng, lengths, 16, width=64)
+    pools = [filled(rng, n_pages, 2, 64, 16, "bf16", table, lengths) for _ in range(2)]
+    cache = ph.PagedCache(pools[0].cuda(), pools[1].cuda(), i32(table), 64)
+    for T in (1, 40):
+        q = queries(rng, (2, T, 4, 64), torch.bfloat16)
+        new = [T, min(T, 20)]
+        a, b = (attend(ph, q, cache, lengths, 1, S_max=s, n_new=i32(new)) for s in (333, 1024))
+        assert torch.equal(a, b)
