@@ -276,7 +276,7 @@ PHOTON_API int32_t photon_paged_cache_move(const photon_paged_cache* cache, cons
  *   seq_len  [Bt] int32, device; values outside [0, S_max] count as the nearer end.  Own entries before entry 0 are not there
  *   n_new    [Bt] int32, device, or NULL: T; queries past n_new[b] are skipped, their rows of out left as they were
  *   tree     [Bt][T] uint64, device, or NULL.  T <= 64 with it; bits n_new[b] and up count for nothing
- *   out      [Bt, T, H, d_h] dt
+ *   out      [Bt, T, H, d_h] dt; may not share memory with q
  *   status   NULL, or a device word that PHOTON_STATUS_BAD_PAGE is ORed into
  *   S_max    the most entries that a sequence has, at most max_pages * page_size (a bound that is close chooses better splits)
  * Scores, softmax, weights and sums are in fp32 for either dt; a bf16 result is rounded once.  Entries that a query does not see

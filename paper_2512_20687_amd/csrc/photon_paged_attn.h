@@ -544,7 +544,7 @@ __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnA
           unbounded = unbounded || without_unbounded<KV>(vx[i][w]) != vx[i][w];
         }
       }
-      some = m > 1 && __builtin_amdgcn_ballot_w64(unbounded) != 0;
+      some = (m > 1 || a.tree) && __builtin_amdgcn_ballot_w64(unbounded) != 0;   // a node need not see itself
     }
     if constexpr (Y::F32 && CAREFUL) {
       if (some) {

@@ -187,7 +187,7 @@ template <int NB, int WAVES, int PAGES> __global__ __launch_bounds__(WAVES * 64,
           const bool tile = there[2 * half + i / 2];
           keep[i] = (entry < n && tile ? 0xffffu : 0u) | (entry + 1 < n && tile ? 0xffff0000u : 0u);
         }
-        if (m > 1) {
+        if (m > 1 || a.tree) {                                                // a node need not see itself
           const int mine = half * PAGED_STEP + lane / 2;                     // entry of the stage that this lane looks at, half of its row
           const bool used = base + mine < n && (lane < 32 ? there[2 * half] : there[2 * half + 1]);
           bool bad = false;

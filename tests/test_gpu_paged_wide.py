@@ -154,3 +154,23 @@ def test_a_longer_bound_changes_no_bit_of_one_split(ph):
         new = [T, min(T, 20)]
         a, b = (attend(ph, q, cache, lengths, 1, S_max=s, n_new=i32(new)) for s in (333, 1024))
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("rows,kv", [(torch.bfloat16, "bf16"), (torch.float32, "bf16"), (torch.float32, "f32"), (torch.bfloat16, "e4m3")])
+@pytest.mark.parametrize("H", [2, 80])
+@pytest.mark.parametrize("new", [1, 3])
+def test_nodes_that_do_not_see_themselves(ph, rows, kv, H, new):
+    """Masks of zero: the entries before the tree's, whatever the own ones hold; and nothing, where there are none before."""
+    rng = np.random.default_rng(H + new)
+    d_h, P = 64, 16
+    for n in (new + 90, new):
+        table, n_pages = plain.table_of(rng, [n], P)
+        pools = [filled(rng, n_pages, 1, d_h, P, kv, table, [n]) for _ in range(2)]
+        for p in pools:
+            for j in range(n - new, n):
+                p[int(table[0, j // P]), 0, j % P] = 255 if kv == "e4m3" else float("nan")
+        cache = ph.PagedCache(pools[0].cuda(), pools[1].cuda(), i32(table), d_h)
+        q = queries(rng, (1, new, H, d_h), rows)
+        masks = np.zeros((1, new), np.uint64)
+        for splits in (1, 2):
+            check(attend(ph, q, cache, [n], splits, tree=i64(masks)), q, pools, table, [n], [new], d_h, masks)
