@@ -15,6 +15,11 @@
 // so that neither the weights nor V change lanes, nothing goes through LDS, and a row's shrinking factor is in the lane that needs
 // it.  fp32 pages: the same with 16x16x4 fp32 products, in which V needs no interleaving.
 //
+// What bounds it.  Up to 64 rows the entries, once streams fill the chip: 256 x 16 ragged streams of up to 2048 entries of 64 (fp32 rows, bf16
+// pages, 1139 MB) 200 us, 5.7 TB/s; 8 x 4 streams of 32749 entries of 128 under 8 heads (537 MB) 101 us, 5.3 TB/s with the merge.  Few and
+// short streams take the chain of one: counts, page, entries, two products, the waves' and the splits' merges (16 streams of 2048 fp32
+// entries, 16.8 MB: 12.0 us in two launches, of which the merge is 3).
+//
 // Precision.  Products of bf16 and E4M3 entries (which bf16 holds exactly) run on the bf16 matrix cores.  fp32 queries enter as three
 // bf16 parts, weights as two parts (17 bits; the result is rounded to 9) for bf16 rows and as three for fp32 rows.
 #pragma once
@@ -47,7 +52,12 @@ struct PagedAttnArgs {
   bool q_pieces, out_pieces;                   // rows of q, of out: aligned to 4 elements
 };
 
-// How the rows that share a K/V head are taken: row tiles of a wave, waves side by side over rows, and by which kernel.
+// How the rows that share a K/V head are taken: row tiles of a wave, waves side by side over rows, and by which kernel.  Microseconds, 32
+// streams of 3000 entries / 256 of 4096: 24 rows (128 bf16) in one wave of two tiles 21.6 / 99, in two workgroups of one tile 20.5 / 111; 64
+// rows by two waves 27.6 / 133, by one in two workgroups 25.8 / 142; 128 rows over E4M3 pages by four waves 35.5 / 205, by two in two
+// workgroups 34.3 / 221: fewer reads of the entries win once the chip is full.  The wide kernel takes 64 rows of 256 streams of 4096 in 119
+// where this one takes 130, but 52 rows of 16 streams of 3000 in 30.9, this one in 24.0: it begins where its waves have rows.  Its eight waves
+// instead of four for up to 128 rows cost ragged streams dear (1024 of up to 1000 entries of 32: 71 us, 50), gain 2 us in 36 at best.
 struct PagedTile {
   int tiles, waves;
   bool wide;                                   // photon_paged_attn_wide.h's
@@ -414,7 +424,7 @@ __device__ __forceinline__ void paged_weights(const f32x4_t (&d)[R][N], float sc
 }
 
 // R row tiles a wave, RW waves side by side over rows; the KW waves of the same rows deal the steps among themselves.  Fewer waves lose even
-// where streams are many and short (256 x 16 streams of 1085 entries: 203 us, 215 with two waves, 231 with one).
+// where streams are many (256 x 16 ragged streams of up to 2048 entries of 64 fp32-row bf16 pages: 206 us, 215 with two waves, 231 with one).
 template <typename KV, typename T, int NB, int R, int RW>
 __global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnArgs a) {
   using Y = PagedTypes<KV, T, NB>;

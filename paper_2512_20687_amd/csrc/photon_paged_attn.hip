@@ -6,8 +6,9 @@ namespace {
 
 // Workgroups over the entries of a stream: as many as the chip holds at once (two a unit; one where a workgroup's registers fill it), but
 // none with fewer than two steps (wide: eight) a wave, and none where that leaves fewer than four: the merge is a launch.  Microseconds:
-// 16 streams of 2048 entries of 64 bf16 in 1, 2, 4, 8, 16 workgroups 19.9, 15.1, 11.4, 10.3, 11.0; of 512 in 1, 2, 4 8.5, 9.4, 8.4; 128 of 8192 in
-// 2, 4, 8 55, 46, 57; 32 of 32749 of 128 in 4, 8, 16 169, 101, 102; 256 rows over 128 streams of 4096 in 1, 2, 4 181, 128, 145.
+// 16 streams of 2048 entries of 64 bf16 in 1, 2, 4, 8, 16 workgroups 16.7, 13.4, 10.5, 9.0, 8.3; of 512 in 1, 2, 4 7.5, 8.8, 8.1; 128 of
+// 8192 in 2, 4, 8 45.5, 45.0, 48.1; 32 of 32749 of 128 in 4, 8, 16 127, 99, 100; 256 rows over 128 streams of 4096 in 1, 2, 4 181, 125, 150;
+// 2048 rows over 16 of 8191 in 1, 2, 4 326, 196, 212.
 int paged_auto_splits(int Bt, int T, int H, int H_kv, int64_t S_max, bool f32_rows, photon_dtype kv_dt) {
   const int64_t rows = (int64_t)T * (H / H_kv);
   const PagedTile tile = paged_tile(rows, f32_rows, kv_dt);

@@ -1,12 +1,13 @@
 """Per-kernel throughput of the hot path's entry points at the shapes of the
 benchmark configurations, each against the roofline that bounds it.
 
-    python -m paper_2512_20687_amd.kernel_bench [--only copy,module,probe,a1,a2,mx,a3,encoder,prefill,schedules,storage,linear]
+    python -m paper_2512_20687_amd.kernel_bench [--only copy,module,probe,a1,a2,mx,paged,a3,encoder,prefill,schedules,storage,linear]
 
 Prints one JSON object per line: a streaming-read ceiling (a trivial read-only
 kernel over 2 GiB), the chunker GEMM (bf16 MFMA peak), the coarse decode
 attention at the configuration-3 shape and over a flat 131072-key cache (HBM
-peak), the 4-bit cache written, read back and attended over (HBM peak), chunk-local attention in tile mode (HBM peak), the encoders' whole-sequence causal
+peak), the 4-bit cache written, read back and attended over (HBM peak), the paged
+cache likewise (HBM peak; many queries: bf16 MFMA peak), chunk-local attention in tile mode (HBM peak), the encoders' whole-sequence causal
 attention (bf16 MFMA peak on the causal half's flops), whole steps and prefills with
 the coarse cache in its three types, and the few-row linear maps of one block (HBM
 peak on weight bytes).  Inputs are seeded and synthetic,
@@ -171,6 +172,45 @@ def bench_mx():
                           warm=len(caches))
             _emit("mxfp4_attn_kernel" + (" + mxfp4_merge_kernel" if n > 1 else ""),
                   f"{what}: Bt={Bt} H={H} H_kv={H_kv} S={S} d_h={d_h} {str(dtype)[6:]} splits={n}", us, bytes_=nbytes)
+        del caches, q, out, ws
+        torch.cuda.empty_cache()
+
+
+def bench_paged():
+    """The paged cache: rows of a prompt and of a step appended, attention of one query, a drafted tree and a piece of a prompt per sequence."""
+    def sets(nbytes):
+        return max(1, -(-(1 << 30) // nbytes))                # so many take turns
+
+    def make(Bt, H, d_h, S, P, dtype):
+        pages = -(-S // P)
+        table = torch.randperm(Bt * pages, device="cuda").to(torch.int32).view(Bt, pages)
+        return ph.PagedCache(*(torch.randn((Bt * pages, H, P, ph.photon_kv_row_elems(d_h)), device="cuda").to(dtype) for _ in range(2)), table, d_h)
+
+    for Bt, T, H, d_h, dtype, what in ((4, 8192, 32, 64, torch.bfloat16, "cfg3 prompt"), (4, 1, 32, 64, torch.float32, "cfg3 append"),
+                                       (256, 1, 16, 64, torch.float32, "cfg4 append")):
+        rows, entries = Bt * T * H * d_h * (4 if dtype == torch.float32 else 2), Bt * T * H * d_h * 2
+        n = min(64, sets(4 * rows + 2 * entries))
+        data = [[torch.randn((Bt, T, H, d_h), device="cuda").to(dtype) for _ in range(3)] for _ in range(n)]
+        caches = [make(Bt, H, d_h, max(T, 64), 64, torch.bfloat16) for _ in range(n)]
+
+        def append(i):
+            k, v, q = data[i % n]
+            ph.photon_paged_cache_write(k, v, caches[i % n], q=q, q_out=q, rope_theta=1e4)
+
+        _emit("paged_write_kernel", f"{what}: Bt={Bt} T={T} H={H} d_h={d_h} {str(dtype)[6:]} rows", _time_us(append, max(20, 2 * n), warm=n), bytes_=4 * rows + 2 * entries)
+        del data, caches
+    f32, bf16 = torch.float32, torch.bfloat16
+    for Bt, T, H, H_kv, d_h, S, dtype, kv, what in ((4, 1, 32, 32, 64, 8320, f32, bf16, "cfg3"), (256, 1, 16, 16, 64, 2112, f32, bf16, "cfg4"),
+                                                    (4, 1, 32, 32, 64, 8320, f32, f32, "cfg3"), (8, 1, 32, 4, 128, 32768, bf16, bf16, "grouped heads"),
+                                                    (16, 64, 32, 8, 128, 4096, bf16, bf16, "64 nodes"), (2, 512, 32, 8, 128, 8192, bf16, bf16, "piece of a prompt")):
+        nbytes = 2 * Bt * H_kv * S * d_h * (4 if kv is f32 else 2)
+        caches = [make(Bt, H_kv, d_h, S, 64, kv) for _ in range(sets(nbytes))]
+        q = torch.randn((Bt, T, H, d_h), device="cuda").to(dtype)
+        out, lens = torch.empty_like(q), torch.full((Bt,), S, dtype=torch.int32, device="cuda")
+        ws = torch.empty(max(16, ph.photon_paged_attn_workspace_bytes(caches[0], Bt, T, H, S)), dtype=torch.uint8, device="cuda")
+        us = _time_us(lambda i: ph.photon_paged_attn(q, caches[i % len(caches)], lens, out, S_max=S, workspace=ws), 4 * max(15, len(caches)), warm=len(caches))
+        work = dict(flops=4 * d_h * Bt * H * (T * (S - T) + T * (T + 1) // 2)) if T > 1 else dict(bytes_=nbytes)
+        _emit("paged attention, merge included", f"{what}: Bt={Bt} T={T} H={H} H_kv={H_kv} S={S} d_h={d_h} {str(dtype)[6:]} rows, {str(kv)[6:]} pages", us, **work)
         del caches, q, out, ws
         torch.cuda.empty_cache()
 
@@ -469,7 +509,7 @@ def bench_linear():
             del ws
 
 
-ALL = {"copy": bench_copy, "module": bench_module, "probe": bench_probe, "a1": bench_a1, "a2": bench_a2, "mx": bench_mx, "a3": bench_a3, "encoder": bench_encoder_attn, "prefill": bench_prefill, "schedules": bench_schedules, "storage": bench_storage, "linear": bench_linear}
+ALL = {"copy": bench_copy, "module": bench_module, "probe": bench_probe, "a1": bench_a1, "a2": bench_a2, "mx": bench_mx, "paged": bench_paged, "a3": bench_a3, "encoder": bench_encoder_attn, "prefill": bench_prefill, "schedules": bench_schedules, "storage": bench_storage, "linear": bench_linear}
 
 
 def main(argv=None):
