@@ -425,8 +425,14 @@ __device__ __forceinline__ void paged_weights(const f32x4_t (&d)[R][N], float sc
 
 // R row tiles a wave, RW waves side by side over rows; the KW waves of the same rows deal the steps among themselves.  Fewer waves lose even
 // where streams are many (256 x 16 ragged streams of up to 2048 entries of 64 fp32-row bf16 pages: 206 us, 215 with two waves, 231 with one).
+// Two waves a SIMD are asked for wherever their registers suffice: left to itself, the compiler moves sums to accumulation registers and back
+// and then fits one (13 nodes over E4M3 pages, 1024 streams of up to 1000 entries: 21.3 us, now 17.8; 512 rows over fp32 pages, 256 streams of
+// 4096: 1439 us, now 1306).  Two tiles of 128 elements with fp32 rows or pages spill 130 registers and more at two waves (512 rows, 32
+// streams of 2000: 84 us, 54 at one).
+constexpr bool paged_two_waves(int d_p, int tiles, bool f32) { return !(d_p == 128 && tiles == 2 && f32); }
+
 template <typename KV, typename T, int NB, int R, int RW>
-__global__ __launch_bounds__(PAGED_WAVES * 64) void paged_attn_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(PAGED_WAVES * 64, paged_two_waves(32 * NB, R, sizeof(KV) == 4 || sizeof(T) == 4) ? 2 : 1) void paged_attn_kernel(PagedAttnArgs a) {
   using Y = PagedTypes<KV, T, NB>;
   constexpr int DP = Y::DP, TILES = Y::TILES, KW = PAGED_WAVES / RW, PITCH = DP + 4;
   __shared__ __align__(16) float results[KW > 1 ? PAGED_WAVES * 16 * PITCH : 4];

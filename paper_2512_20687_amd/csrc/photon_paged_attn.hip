@@ -9,19 +9,24 @@ namespace {
 // 16 streams of 2048 entries of 64 bf16 in 1, 2, 4, 8, 16 workgroups 16.7, 13.4, 10.5, 9.0, 8.3; of 512 in 1, 2, 4 7.5, 8.8, 8.1; 128 of
 // 8192 in 2, 4, 8 45.5, 45.0, 48.1; 32 of 32749 of 128 in 4, 8, 16 127, 99, 100; 256 rows over 128 streams of 4096 in 1, 2, 4 181, 125, 150;
 // 2048 rows over 16 of 8191 in 1, 2, 4 326, 196, 212.
-int paged_auto_splits(int Bt, int T, int H, int H_kv, int64_t S_max, bool f32_rows, photon_dtype kv_dt) {
+int paged_auto_splits(int Bt, int T, int H, int H_kv, int d_p, int64_t S_max, bool f32_rows, photon_dtype kv_dt) {
   const int64_t rows = (int64_t)T * (H / H_kv);
   const PagedTile tile = paged_tile(rows, f32_rows, kv_dt);
   const int64_t groups = (int64_t)Bt * H_kv * ((rows + tile.rows() - 1) / tile.rows());
   const int64_t steps = (S_max + PAGED_STEP - 1) / PAGED_STEP;
   int64_t splits = (tile.tiles == 1 ? 512 : 256) / groups;
+  // Two tiles a wave leave more to merge: their second workgroup a unit has to have 32 steps a wave (128 rows over E4M3 pages, 256 streams of
+  // 4096 entries: 194 us with one split, 144 with two; 32 streams of 3000 in 8, 16: 34, 44).
+  const bool held = tile.tiles == 2 && !tile.wide && paged_two_waves(d_p, 2, f32_rows || kv_dt == PHOTON_F32);
+  if (held && steps * tile.waves / PAGED_WAVES / 32 >= 512 / groups) splits = 512 / groups;
   const int64_t most = tile.wide ? steps / 8 : steps * tile.waves / (2 * PAGED_WAVES);
   splits = splits > most ? most : splits;
   if (!tile.wide && most < 4) splits = 1;
   return (int)(splits < 1 ? 1 : splits > 256 ? 256 : splits);
 }
 int paged_most_splits(const photon_paged_cache* c, int Bt, int T, int H, int64_t S_max) {   // of either dtype of rows
-  const int a = paged_auto_splits(Bt, T, H, c->H_kv, S_max, false, c->kv_dt), b = paged_auto_splits(Bt, T, H, c->H_kv, S_max, true, c->kv_dt);
+  const int d_p = kv_row_elems(c->d_h);
+  const int a = paged_auto_splits(Bt, T, H, c->H_kv, d_p, S_max, false, c->kv_dt), b = paged_auto_splits(Bt, T, H, c->H_kv, d_p, S_max, true, c->kv_dt);
   return a > b ? a : b;
 }
 
@@ -81,7 +86,7 @@ extern "C" int32_t photon_paged_attn(const photon_paged_cache* cache, const void
   PHOTON_REQUIRE(seq_len != nullptr, PHOTON_ERR_INVALID_ARG, "%s: seq_len is null", __func__);
   PHOTON_REQUIRE(q_stride >= (int64_t)H * d_h, PHOTON_ERR_INVALID_ARG, "%s: q_stride=%lld is less than a row of %d heads of %d", __func__, (long long)q_stride, H, d_h);
   const bool f32 = dt == PHOTON_F32;
-  if (n_splits == 0) n_splits = paged_auto_splits(Bt, T, H, cache->H_kv, S_max, f32, cache->kv_dt);
+  if (n_splits == 0) n_splits = paged_auto_splits(Bt, T, H, cache->H_kv, kv_row_elems(d_h), S_max, f32, cache->kv_dt);
   if (n_splits > 1) {
     const size_t need = workspace_bytes_of(cache, Bt, T, H, n_splits);
     PHOTON_REQUIRE(workspace != nullptr && aligned16(workspace) && workspace_bytes >= need, PHOTON_ERR_WORKSPACE,
