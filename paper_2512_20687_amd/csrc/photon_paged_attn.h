@@ -52,20 +52,28 @@ struct PagedAttnArgs {
   bool q_pieces, out_pieces;                   // rows of q, of out: aligned to 4 elements
 };
 
-// How the rows that share a K/V head are taken: row tiles of a wave, waves side by side over rows, and by which kernel.  Microseconds, 32
-// streams of 3000 entries / 256 of 4096: 24 rows (128 bf16) in one wave of two tiles 21.6 / 99, in two workgroups of one tile 20.5 / 111; 64
-// rows by two waves 27.6 / 133, by one in two workgroups 25.8 / 142; 128 rows over E4M3 pages by four waves 35.5 / 205, by two in two
-// workgroups 34.3 / 221: fewer reads of the entries win once the chip is full.  The wide kernel takes 64 rows of 256 streams of 4096 in 119
-// where this one takes 130, but 52 rows of 16 streams of 3000 in 30.9, this one in 24.0: it begins where its waves have rows.  Its eight waves
-// instead of four for up to 128 rows cost ragged streams dear (1024 of up to 1000 entries of 32: 71 us, 50), gain 2 us in 36 at best.
+// How the rows that share a K/V head are taken: row tiles of a wave, waves side by side over rows, and by which kernel.  While the chip holds all
+// workgroups of 32 rows at once (512: two a unit), these win whatever the rows: all four waves go along the entries.  From there on entries are to
+// be read fewer times: by workgroups of 64 rows, or the wide kernel's of 128 and 256, where rows and pages are bf16.  Microseconds, bf16
+// rows (32-row workgroups / 64-row ones / wide):
+//   84 rows, 16 x 8 ragged streams of up to 3000 entries of 128    E4M3 pages 39 / 63     bf16 pages 50 / - / 62
+//   128 rows, 8 streams of 3000                                    E4M3 18 / 24           bf16 20 / - / 31
+//   512 rows, 4 x 8 streams of 3000                                E4M3 55 / 66           bf16 72 / - / 71
+//   48 rows, 64 x 8 ragged streams of up to 1000                   E4M3 41 / 34           bf16 56 / 44
+//   512 rows, 32 x 8 streams of 4096                               E4M3 509 / 484         bf16 - / - / 395
+// The wide kernel's eight waves instead of four for up to 128 rows cost ragged streams dear (1024 of up to 1000 entries of 32: 71 us, 50) and
+// gain 2 us in 36 at best.  24 rows in two workgroups of one tile: 20.4 us for 32 streams of 3000 (in one of two tiles 21.3), but 110 for 256 of
+// 4096 (98).
 struct PagedTile {
   int tiles, waves;
   bool wide;                                   // photon_paged_attn_wide.h's
   int rows() const { return 16 * tiles * waves; }
 };
-inline PagedTile paged_tile(int64_t rows, bool f32_rows, photon_dtype kv_dt) {
-  if (rows > 64 && !f32_rows && kv_dt == PHOTON_BF16) return PagedTile{2, rows <= 128 ? 4 : 8, true};
-  return rows <= 16 ? PagedTile{1, 1, false} : rows <= 32 ? PagedTile{2, 1, false} : rows <= 64 ? PagedTile{2, 2, false} : PagedTile{2, 4, false};
+inline PagedTile paged_tile(int64_t rows, int64_t streams, bool f32_rows, photon_dtype kv_dt) {
+  if (rows <= 16) return PagedTile{1, 1, false};
+  if (streams * ((rows + 31) / 32) <= 512) return PagedTile{2, 1, false};
+  if (rows <= 64 || f32_rows || kv_dt != PHOTON_BF16) return PagedTile{2, 2, false};
+  return PagedTile{2, rows <= 128 ? 4 : 8, true};
 }
 
 // Launches over the tile of rows that `a` calls for; one translation unit per page type.
@@ -435,7 +443,7 @@ template <typename KV, typename T, int NB, int R, int RW>
 __global__ __launch_bounds__(PAGED_WAVES * 64, paged_two_waves(32 * NB, R, sizeof(KV) == 4 || sizeof(T) == 4) ? 2 : 1) void paged_attn_kernel(PagedAttnArgs a) {
   using Y = PagedTypes<KV, T, NB>;
   constexpr int DP = Y::DP, TILES = Y::TILES, KW = PAGED_WAVES / RW, PITCH = DP + 4;
-  __shared__ __align__(16) float results[KW > 1 ? PAGED_WAVES * 16 * PITCH : 4];
+  __shared__ __align__(16) float results[PAGED_WAVES * 16 * PITCH];
   __shared__ float stats[PAGED_WAVES][16][2];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 15, g = lane >> 4;
   const int kw = wave % KW, rw = wave / KW;
@@ -647,50 +655,38 @@ __global__ __launch_bounds__(PAGED_WAVES * 64, paged_two_waves(32 * NB, R, sizeo
     const float l = over_row(sum[r], [](float x, float y) { return x + y; });
     const float mean = l == 0.f ? 0.f : 1.f / l;
     const int row = first + r * 16 + c;
-    if constexpr (KW == 1) {
-      if (row < rows) {
+    if (r > 0) __syncthreads();
+    if (row < rows) {
 #pragma unroll
-        for (int x = 0; x < 8 * NB; x += 4) {
-          float o[4];
+      for (int x = 0; x < 8 * NB; x += 4) {
+        float4_t o;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[e] = acc[r][(x + e) % TILES][(x + e) / TILES] * mean;
-          paged_emit<T, DP>(a, paged_row(a, b, hk, row), split, 8 * NB * g + x, o, top[r], l);
-        }
+        for (int e = 0; e < 4; ++e) o[e] = acc[r][(x + e) % TILES][(x + e) / TILES] * mean;
+        *reinterpret_cast<float4_t*>(results + (wave * 16 + c) * PITCH + 8 * NB * g + x) = o;
       }
-    } else {
-      if (r > 0) __syncthreads();
-      if (row < rows) {
+      if (g == 0) { stats[wave][c][0] = top[r]; stats[wave][c][1] = l; }
+    }
+    __syncthreads();
+    for (int x = tid; x < RW * 16 * (DP / 4); x += PAGED_WAVES * 64) {
+      const int d = x % (DP / 4) * 4, i = x / (DP / 4) % 16, of = x / (DP / 4) / 16;     // of: which of the waves side by side
+      const int to = group_first + of * (R * 16) + r * 16 + i;
+      if (to >= rows) continue;
+      float w_top = PAGED_LOWEST, w_sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f}, weight[KW];
 #pragma unroll
-        for (int x = 0; x < 8 * NB; x += 4) {
-          float4_t o;
+      for (int w = 0; w < KW; ++w) w_top = fmaxf(w_top, stats[of * KW + w][i][0]);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[e] = acc[r][(x + e) % TILES][(x + e) / TILES] * mean;
-          *reinterpret_cast<float4_t*>(results + (wave * 16 + c) * PITCH + 8 * NB * g + x) = o;
-        }
-        if (g == 0) { stats[wave][c][0] = top[r]; stats[wave][c][1] = l; }
+      for (int w = 0; w < KW; ++w) {
+        weight[w] = stats[of * KW + w][i][1] * fast_exp2(stats[of * KW + w][i][0] - w_top);
+        w_sum += weight[w];
       }
-      __syncthreads();
-      for (int x = tid; x < RW * 16 * (DP / 4); x += PAGED_WAVES * 64) {
-        const int d = x % (DP / 4) * 4, i = x / (DP / 4) % 16, of = x / (DP / 4) / 16;     // of: which of the waves side by side
-        const int to = group_first + of * (R * 16) + r * 16 + i;
-        if (to >= rows) continue;
-        float w_top = PAGED_LOWEST, w_sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f}, weight[KW];
+      const float inverse = w_sum == 0.f ? 0.f : 1.f / w_sum;
 #pragma unroll
-        for (int w = 0; w < KW; ++w) w_top = fmaxf(w_top, stats[of * KW + w][i][0]);
+      for (int w = 0; w < KW; ++w) {
+        const float4_t y = *reinterpret_cast<const float4_t*>(results + ((of * KW + w) * 16 + i) * PITCH + d);
 #pragma unroll
-        for (int w = 0; w < KW; ++w) {
-          weight[w] = stats[of * KW + w][i][1] * fast_exp2(stats[of * KW + w][i][0] - w_top);
-          w_sum += weight[w];
-        }
-        const float inverse = w_sum == 0.f ? 0.f : 1.f / w_sum;
-#pragma unroll
-        for (int w = 0; w < KW; ++w) {
-          const float4_t y = *reinterpret_cast<const float4_t*>(results + ((of * KW + w) * 16 + i) * PITCH + d);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[e] = fmaf(y[e], weight[w] * inverse, o[e]);
-        }
-        paged_emit<T, DP>(a, paged_row(a, b, hk, to), split, d, o, w_top, w_sum);
+        for (int e = 0; e < 4; ++e) o[e] = fmaf(y[e], weight[w] * inverse, o[e]);
       }
+      paged_emit<T, DP>(a, paged_row(a, b, hk, to), split, d, o, w_top, w_sum);
     }
   }
 }
@@ -742,8 +738,7 @@ template <typename KV, typename T, int NB, int R, int RW> int32_t paged_launch(c
 template <typename KV, typename T, int NB> int32_t paged_launch_rows(const PagedAttnArgs& a, const PagedTile& tile, hipStream_t st) {
   if (tile.tiles == 1) return paged_launch<KV, T, NB, 1, 1>(a, st);
   if (tile.waves == 1) return paged_launch<KV, T, NB, 2, 1>(a, st);
-  if (tile.waves == 2) return paged_launch<KV, T, NB, 2, 2>(a, st);
-  return paged_launch<KV, T, NB, 2, 4>(a, st);
+  return paged_launch<KV, T, NB, 2, 2>(a, st);
 }
 template <typename KV> int32_t paged_launch_types(const PagedAttnArgs& a, const PagedTile& tile, bool f32_rows, hipStream_t st) {
   const int nb = kv_row_elems(a.pool.d_h) / 32;

@@ -11,7 +11,7 @@ namespace {
 // 2048 rows over 16 of 8191 in 1, 2, 4 326, 196, 212.
 int paged_auto_splits(int Bt, int T, int H, int H_kv, int d_p, int64_t S_max, bool f32_rows, photon_dtype kv_dt) {
   const int64_t rows = (int64_t)T * (H / H_kv);
-  const PagedTile tile = paged_tile(rows, f32_rows, kv_dt);
+  const PagedTile tile = paged_tile(rows, (int64_t)Bt * H_kv, f32_rows, kv_dt);
   const int64_t groups = (int64_t)Bt * H_kv * ((rows + tile.rows() - 1) / tile.rows());
   const int64_t steps = (S_max + PAGED_STEP - 1) / PAGED_STEP;
   int64_t splits = (tile.tiles == 1 ? 512 : 256) / groups;
@@ -96,7 +96,7 @@ extern "C" int32_t photon_paged_attn(const photon_paged_cache* cache, const void
   a.seq_len = seq_len; a.n_new = n_new; a.tree = tree; a.status = status;
   a.q_stride = q_stride; a.S_max = (int32_t)S_max; a.Bt = Bt; a.T = T; a.H = H; a.group = H / cache->H_kv; a.n_splits = n_splits;
   const int64_t rows = (int64_t)T * a.group;
-  const PagedTile tile = paged_tile(rows, f32, cache->kv_dt);
+  const PagedTile tile = paged_tile(rows, (int64_t)Bt * cache->H_kv, f32, cache->kv_dt);
   PHOTON_REQUIRE(rows <= PAGED_MOST_ROWS, PHOTON_ERR_UNSUPPORTED, "%s: T=%d queries of %d heads a K/V head are too many", __func__, T, a.group);
   const int64_t groups = (rows + tile.rows() - 1) / tile.rows(), units = (int64_t)Bt * cache->H_kv * n_splits;
   PHOTON_REQUIRE((units + 7) * groups <= (int64_t)0xffffffff / 512 && (int64_t)Bt * T * H <= (int64_t)0xffffffff / 32, PHOTON_ERR_UNSUPPORTED,

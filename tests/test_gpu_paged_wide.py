@@ -1,5 +1,5 @@
-"""Attention over the paged K/V cache where many rows share a K/V head (bf16 rows and pages take entries through LDS there), and what all
-of its kernels have to survive: pages that are not there, far scores, large values, scales of any kind, more splits than steps.
+"""Attention over the paged K/V cache where many rows share a K/V head (with many streams of bf16 rows and pages entries go through LDS there),
+and what all of its kernels have to survive: pages that are not there, far scores, large values, scales of any kind, more splits than steps.
 
 Tolerances as in tests/test_gpu_paged_attn.py."""
 import numpy as np
@@ -7,18 +7,100 @@ import pytest
 import torch
 
 import paged_plain as plain
+import test_gpu_paged_attn as base
 from test_gpu_paged_attn import BAD_PAGE, KV, check, filled, i32, i64, trees
 from util import require_gpu
 
 pytestmark = pytest.mark.gpu
 
 
-@pytest.fixture(scope="module")
-def ph():
+class Many:
+    """The library with every call turned into one of so many streams that workgroups take 64 rows and more: query heads are repeated until a
+    stream has more than `above` rows (64: what the wide kernel takes where rows and pages are bf16), K/V heads until streams are enough.
+    Equal streams have to give equal bits."""
+
+    def __init__(self, library, above):
+        self.library, self.above, self.calls = library, above, 0
+
+    def __getattr__(self, name):
+        return getattr(self.library, name)
+
+    def photon_paged_attn(self, q, cache, seq_len, out, workspace=None, n_splits=0, **kw):
+        Bt, T, H, d_h = q.shape
+        H_kv = cache.H_kv
+        group = H // H_kv
+        copies = self.above // (T * group) + 1
+        rows = T * group * copies
+        streams = 512 // (Bt * H_kv * -(-rows // 32)) + 1
+        assert rows > self.above and Bt * H_kv * streams * -(-rows // 32) > 512
+        many = self.library.PagedCache(*(p.repeat_interleave(streams, 1) for p in (cache.k_pages, cache.v_pages)), cache.page_table, d_h)
+        shape = (Bt, T, H_kv, streams, group, copies, d_h)
+
+        def spread(x):
+            return x.view(Bt, T, H_kv, 1, group, 1, d_h).expand(shape).reshape(Bt, T, -1, d_h).contiguous()
+
+        q_many, out_many = spread(q.contiguous()), spread(out)
+        if n_splits != 1:
+            size = self.library.photon_paged_attn_workspace_bytes(many, Bt, T, q_many.shape[2], kw.get("S_max"), n_splits)
+            workspace = torch.full((size + 16,), 255, dtype=torch.uint8, device="cuda")
+        self.library.photon_paged_attn(q_many, many, seq_len, out_many, workspace=workspace, n_splits=n_splits, **kw)
+        if n_splits != 1:
+            assert (workspace[size:] == 255).all()
+        got = out_many.view(shape)
+        bits = torch.int16 if q.dtype is torch.bfloat16 else torch.int32
+        assert torch.equal(got.view(bits), got[:, :, :, :1].expand(shape).contiguous().view(bits))
+        self.calls += 1
+        out.copy_(got[:, :, :, 0, :, self.calls % copies].reshape(out.shape))
+        return out
+
+
+@pytest.fixture(scope="module", params=["few streams", "many streams"])
+def ph(request):
     require_gpu()
     import paper_2512_20687_amd as m
     m.load_library()
-    return m
+    return m if request.param == "few streams" else Many(m, 64)
+
+
+@pytest.fixture(scope="module", params=[16, 64])
+def many(request):
+    require_gpu()
+    import paper_2512_20687_amd as m
+    m.load_library()
+    return Many(m, request.param)
+
+
+@pytest.mark.parametrize("rows", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("kv", list(KV))
+@pytest.mark.parametrize("Bt,T,H,H_kv,d_h,P,lengths,new,tree", base.CASES)
+def test_attention_of_many_streams(many, rows, kv, Bt, T, H, H_kv, d_h, P, lengths, new, tree):
+    for splits in (1, 3):
+        base.run(many, np.random.default_rng(T * d_h + P), rows, kv, Bt, T, H, H_kv, d_h, P, lengths, new, tree, splits)
+
+
+@pytest.mark.parametrize("rows,kv", [(torch.bfloat16, "bf16"), (torch.float32, "bf16"), (torch.bfloat16, "e4m3"), (torch.float32, "f32")])
+@pytest.mark.parametrize("splits", [0, 2, 7])
+@pytest.mark.parametrize("T,H,H_kv,tree", [(1, 8, 1, False), (12, 4, 2, True), (40, 8, 2, False)])
+def test_long_sequences_of_many_streams(many, rows, kv, splits, T, H, H_kv, tree):
+    base.run(many, np.random.default_rng(splits), rows, kv, 2, T, H, H_kv, 64, 32, [4001, 777], [T, max(1, T // 2)], tree, splits)
+
+
+@pytest.mark.parametrize("rows", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("kv", list(KV))
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("T,H,H_kv", [(9, 2, 2), (24, 4, 2), (40, 2, 1)])
+def test_what_is_not_seen_by_many_streams(many, rows, kv, tree, T, H, H_kv):
+    base.test_what_is_not_seen_may_hold_anything(many, rows, kv, tree, T, H, H_kv)
+
+
+def test_masks_lengths_and_pages_of_many_streams(many):
+    base.test_masks_of_any_kind(many)
+    for rows in (torch.float32, torch.bfloat16):
+        for kv in KV:
+            base.test_lengths_and_counts_out_of_range(many, rows, kv)
+    base.test_pages_outside_the_pool(many)
+    base.test_scores_far_from_zero(many, "bf16")
+    base.test_scores_far_from_zero(many, "f32")
 
 
 def attend(ph, q, cache, lengths, splits=1, **kw):
