@@ -224,8 +224,8 @@ PHOTON_API int32_t photon_mxfp4_decode_attn(const void* q, int64_t q_stride, con
  * page_size: 16, 32, 64, 128 or 256.  kv_dt: fp32, bf16, or E4M3 bytes (rounded
  * to nearest even, saturated at +-448, no scale), with rows of either dtype.
  * Pools must be 16-byte aligned and may not share memory.  Rows (q, k, v,
- * q_out, out) need the alignment of their elements only; whole multiples of 16
- * bytes (pointer, stride, d_h / 2) are read fastest.  d_h in [1, 128];
+ * q_out, out) need the alignment of their elements only; whole multiples of four
+ * elements (pointer, stride, d_h / 2) are read fastest.  d_h in [1, 128];
  * max_pages * page_size <= 2^31 - 256.  Bt == 0 or T == 0 is a no-op.
  * -------------------------------------------------------------------------- */
 typedef struct photon_paged_cache {   /* host struct of device pointers, read during the call only */

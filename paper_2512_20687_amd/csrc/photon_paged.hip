@@ -66,14 +66,14 @@ __device__ __forceinline__ uint32_t pack_e4m3x2(float lo, float hi) {
 }
 
 template <typename T, int VEC> __device__ __forceinline__ void load_piece(const T* p, float (&x)[VEC]) {
-  // as one access: the launch chose VEC so that pieces are aligned to 16 bytes, or to their size
-  struct alignas(VEC * sizeof(T) < 16 ? VEC * sizeof(T) : 16) Raw { T e[VEC]; };
+  // as one access: the launch chose VEC so that pieces are aligned to their size
+  struct alignas(VEC * sizeof(T)) Raw { T e[VEC]; };
   const Raw r = *reinterpret_cast<const Raw*>(p);
 #pragma unroll
   for (int e = 0; e < VEC; ++e) x[e] = to_f32<T>(r.e[e]);
 }
 template <typename T, int VEC> __device__ __forceinline__ void store_piece(T* p, const float (&x)[VEC]) {
-  struct alignas(VEC * sizeof(T) < 16 ? VEC * sizeof(T) : 16) Raw { T e[VEC]; };
+  struct alignas(VEC * sizeof(T)) Raw { T e[VEC]; };
   Raw r;
   if constexpr (sizeof(T) == 2 && VEC > 1) {
 #pragma unroll
@@ -243,15 +243,15 @@ template <typename T, typename KV, int VEC> void launch_write(WriteArgs a, const
   const int64_t items = (int64_t)((a.q ? a.H : 0) + 2 * a.pool.H_kv) * (a.half / VEC);
   const int64_t groups = (items + 255) / 256;
   const int threads = (int)(((items + groups - 1) / groups + 63) / 64 * 64);
-  // Rows of a workgroup: as many as share a table of angles well, but fewer while the chip is not full.
+  // Rows of a workgroup: as many as share a table of angles well, but fewer while workgroups are few: several rounds of them even out what
+  // their rows take (four prompts of 8192 rows with at least 2048, 4096, 8192 workgroups: 172, 164, 155 us; 64 ragged prompts 38, 34, 32).
   int rows = ROPE_ROWS;
-  while (rows > 1 && ((int64_t)Bt * ((a.T + rows - 1) / rows) * groups < 2048 || rows / 2 >= a.T)) rows /= 2;
+  while (rows > 1 && ((int64_t)Bt * ((a.T + rows - 1) / rows) * groups < 8192 || rows / 2 >= a.T)) rows /= 2;
   a.rows = rows;
   PHOTON_LAUNCH(KC_PAGED_CACHE, st, (paged_write_kernel<T, KV, VEC>), dim3((unsigned)((a.T + rows - 1) / rows), (unsigned)groups, Bt), dim3(threads), 0, st, a, rope);
 }
 template <typename T, typename KV> void launch_write_vec(const WriteArgs& a, const RopeTable& rope, int vec, int Bt, hipStream_t st) {
   switch (vec) {
-    case 8: return launch_write<T, KV, 8>(a, rope, Bt, st);
     case 4: return launch_write<T, KV, 4>(a, rope, Bt, st);
     case 2: return launch_write<T, KV, 2>(a, rope, Bt, st);
     default: return launch_write<T, KV, 1>(a, rope, Bt, st);
@@ -316,13 +316,15 @@ extern "C" int32_t photon_paged_cache_write(const photon_paged_cache* cache, con
       low = (uint64_t)next;
     }
   }
-  // Elements of a piece: they divide half a head (so pairs are whole pieces) and are aligned in every row that a piece is read from.
+  // Elements of a piece: they divide half a head (so pairs are whole pieces) and are aligned in every row that a piece is read from.  Four at
+  // most: eight leave registers for three or four waves a SIMD instead of eight (the four prompts 182 us, 172 with four; fp32 rows and pages
+  // 174, 161).
   const auto whole = [&](int vec) {
-    const size_t n = vec * esz < 16 ? vec * esz : 16;
+    const size_t n = vec * esz;
     const auto rows = [&](const void* p, int64_t stride) { return element_aligned(p, n) && stride * esz % n == 0; };
     return d_h % 2 == 0 && a.half % vec == 0 && rows(k, row_stride) && rows(v, row_stride) && (!q || (rows(q, q_stride) && rows(q_out, q_out_stride)));
   };
-  const int vec = whole(8) ? 8 : whole(4) ? 4 : whole(2) ? 2 : 1;
+  const int vec = whole(4) ? 4 : whole(2) ? 2 : 1;
   PHOTON_REQUIRE((int64_t)T * 256 <= 0xffffffffll && ((int64_t)(a.H + 2 * H_kv) * a.half / 256 + 1) <= 65535, PHOTON_ERR_UNSUPPORTED,
                  "%s: T=%d rows of %d heads are too many", __func__, T, a.H + 2 * H_kv);
   (dt == PHOTON_F32 ? launch_write_t<float> : launch_write_t<bf16_t>)(a, rope, vec, cache->kv_dt, Bt, (hipStream_t)stream);
