@@ -2,8 +2,8 @@
 //
 // Both are copies: bytes bound them.  An append reads k, v and q once and writes the entries and q_out once; a row's heads are
 // consecutive in memory, an entry's are head_bytes apart, so that every head of an entry is a run of whole 64- or 128-byte lines.
-// Measured: four prompts of 8192 rows (805 MB) 179 us, 4.5 TB/s where a copy reaches 4.9; 64 ragged prompts into E4M3 pages (167 MB) 42 us,
-// 4.0 TB/s; one entry of four sequences 7.7 us and 256 sequences' (10 MB) 8.4 us, which are the call's and a launch's.
+// Measured: four prompts of 8192 rows (805 MB) 155 us, 5.2 TB/s where a copy reaches 4.9; 64 ragged prompts into E4M3 pages (167 MB) 34.5 us,
+// 4.8 TB/s; one entry of four sequences 7.6 us and 256 sequences' (10 MB) 8.2 us, which are the call's and a launch's.
 #include <math.h>
 
 #include "photon_device.h"
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(256) void paged_write_kernel(WriteArgs a, RopeTable
     }
   };
   // The first rows are on their way while places and angles are found out, and counts, too, where most workgroups will have rows (64
-  // prompts of 1 .. 133 rows: 42 us, 53 with all of the padding's rows requested).
+  // prompts of 1 .. 133 rows, in the larger workgroups of that time: 42 us, 53 with all of the padding's rows requested).
   const bool early = a.n_new == nullptr || a.T <= AT_ONCE;
   if (early) request(0, min(a.rows, a.T - t0));
   int m = a.n_new ? a.n_new[b] : a.T;

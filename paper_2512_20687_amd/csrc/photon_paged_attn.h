@@ -15,7 +15,7 @@
 // so that neither the weights nor V change lanes, nothing goes through LDS, and a row's shrinking factor is in the lane that needs
 // it.  fp32 pages: the same with 16x16x4 fp32 products, in which V needs no interleaving.
 //
-// What bounds it.  Up to 64 rows the entries, once streams fill the chip: 256 x 16 ragged streams of up to 2048 entries of 64 (fp32 rows, bf16
+// What bounds it.  Up to 32 rows the entries, once streams fill the chip: 256 x 16 ragged streams of up to 2048 entries of 64 (fp32 rows, bf16
 // pages, 1139 MB) 200 us, 5.7 TB/s; 8 x 4 streams of 32749 entries of 128 under 8 heads (537 MB) 101 us, 5.3 TB/s with the merge.  Few and
 // short streams take the chain of one: counts, page, entries, two products, the waves' and the splits' merges (16 streams of 2048 fp32
 // entries, 16.8 MB: 12.0 us in two launches, of which the merge is 3).
