@@ -2,8 +2,8 @@
 //
 // Both are copies: bytes bound them.  An append reads k, v and q once and writes the entries and q_out once; a row's heads are
 // consecutive in memory, an entry's are head_bytes apart, so that every head of an entry is a run of whole 64- or 128-byte lines.
-// Measured: four prompts of 8192 rows (805 MB) 155 us, 5.2 TB/s where a copy reaches 4.9; 64 ragged prompts into E4M3 pages (167 MB) 34.5 us,
-// 4.8 TB/s; one entry of four sequences 7.6 us and 256 sequences' (10 MB) 8.2 us, which are the call's and a launch's.
+// Measured: four prompts of 8192 rows (805 MB) 152 us, 5.3 TB/s where a copy reaches 4.9; 64 ragged prompts into E4M3 pages (167 MB) 34.1 us,
+// 4.9 TB/s; one entry of four sequences 7.5 us and 256 sequences' (10 MB) 8.1 us, which are the call's and a launch's.
 #include <math.h>
 
 #include "photon_device.h"
@@ -57,7 +57,12 @@ struct WriteArgs {
   const int32_t *start, *n_new, *position;
   int32_t* status;
   int32_t T, H, rows, half, rotate;       // rows: of a workgroup; half: elements from one member of a rotary pair to the other
+  uint32_t by_half, by_pieces;            // ceil(2^32 / half), ceil(2^32 / (half / VEC)): see quotient()
 };
+
+// x / d by a multiplication, m = ceil(2^32 / d): exact where x d < 2^32 (x below 2^24 here, d up to 64).  A division is 20 instructions and more (128
+// sequences of 31 rows, one row a workgroup, and the move: 19.7 us with divisions, 19.2; the four prompts 155, 152).
+__device__ __forceinline__ int quotient(int x, int d, uint32_t m) { return d == 1 ? x : (int)__umulhi((uint32_t)x, m); }
 
 // Two values as E4M3: saturated, and NaN stays NaN.
 __device__ __forceinline__ uint32_t pack_e4m3x2(float lo, float hi) {
@@ -99,9 +104,9 @@ __global__ __launch_bounds__(256) void paged_write_kernel(WriteArgs a, RopeTable
   __shared__ float2_native angle[ROPE_ROWS][MOST_PAIRS];
   __shared__ int64_t place[ROPE_ROWS];                                       // byte offset of the entry of head 0; -1: none
   const int b = blockIdx.z, tid = threadIdx.x, t0 = blockIdx.x * a.rows;
-  const int pieces = a.half / VEC, x = blockIdx.y * blockDim.x + tid;
+  const int pieces = (int)((uint32_t)a.half / VEC), x = blockIdx.y * blockDim.x + tid;
   const int q_heads = a.q ? a.H : 0, H_kv = a.pool.H_kv, d_h = a.pool.d_h, heads = q_heads + 2 * H_kv;
-  const int head = min(x / pieces, heads - 1), c = (x - x / pieces * pieces) * VEC;         // threads behind the last head only help with the table
+  const int nth = quotient(x, pieces, a.by_pieces), head = min(nth, heads - 1), c = (x - nth * pieces) * VEC;         // threads behind the last head only help with the table
   const int kind = head < q_heads ? 0 : head < q_heads + H_kv ? 1 : 2;       // q, K, V
   const int h = kind == 0 ? head : kind == 1 ? head - q_heads : head - q_heads - H_kv;
   const int64_t stride = kind == 0 ? a.q_stride : a.row_stride;
@@ -143,7 +148,7 @@ __global__ __launch_bounds__(256) void paged_write_kernel(WriteArgs a, RopeTable
   }
   if (a.rotate) {
     for (int y = tid; y < rows * a.half; y += blockDim.x) {
-      const int r = y / a.half, i = y - r * a.half;
+      const int r = quotient(y, a.half, a.by_half), i = y - r * a.half;
       const int position = a.position ? a.position[(int64_t)b * a.T + t0 + r] : (int)((uint32_t)start + t0 + r);
       const uint64_t phase = (uint64_t)(int64_t)position * rope.turns[i];
       // the nearest quarter turn is taken off before the phase becomes a float: what is left is at most an eighth
@@ -155,7 +160,7 @@ __global__ __launch_bounds__(256) void paged_write_kernel(WriteArgs a, RopeTable
     }
   }
   __syncthreads();
-  if (x / pieces >= heads) return;
+  if (nth >= heads) return;
   T* q_to = (T*)a.q_out + ((int64_t)b * a.T + t0) * a.q_out_stride + (int64_t)h * d_h + c;
   uint8_t* pool = (kind == 1 ? a.pool.k : a.pool.v) + h * a.pool.head_bytes;
   const int d_p = a.pool.row_bytes / (int)sizeof(KV);
@@ -248,6 +253,9 @@ template <typename T, typename KV, int VEC> void launch_write(WriteArgs a, const
   int rows = ROPE_ROWS;
   while (rows > 1 && ((int64_t)Bt * ((a.T + rows - 1) / rows) * groups < 8192 || rows / 2 >= a.T)) rows /= 2;
   a.rows = rows;
+  const uint32_t pieces = (uint32_t)a.half / VEC;
+  a.by_half = (uint32_t)((0x100000000ull + a.half - 1) / a.half);          // 0 for 1, not used
+  a.by_pieces = (uint32_t)((0x100000000ull + pieces - 1) / pieces);
   PHOTON_LAUNCH(KC_PAGED_CACHE, st, (paged_write_kernel<T, KV, VEC>), dim3((unsigned)((a.T + rows - 1) / rows), (unsigned)groups, Bt), dim3(threads), 0, st, a, rope);
 }
 template <typename T, typename KV> void launch_write_vec(const WriteArgs& a, const RopeTable& rope, int vec, int Bt, hipStream_t st) {
