@@ -256,3 +256,38 @@ def test_nodes_that_do_not_see_themselves(ph, rows, kv, H, new):
         masks = np.zeros((1, new), np.uint64)
         for splits in (1, 2):
             check(attend(ph, q, cache, [n], splits, tree=i64(masks)), q, pools, table, [n], [new], d_h, masks)
+
+
+@pytest.mark.parametrize("rows,kv,T", [(torch.bfloat16, "bf16", 70), (torch.bfloat16, "bf16", 140), (torch.float32, "bf16", 40)])
+def test_captured_calls_of_many_streams(rows, kv, T):
+    """A captured call replayed with other lengths, pages and queries, eager calls in between: the eager call's bits."""
+    require_gpu()
+    import paper_2512_20687_amd as ph
+    rng = np.random.default_rng(T)
+    P, d_h, H, longest = 16, 128, 90, 400
+    table, n_pages = plain.table_of(rng, [longest, longest], P)
+    pools = [torch.from_numpy(rng.standard_normal((n_pages, H, P, d_h), dtype=np.float32)).to(KV[kv]).cuda() for _ in range(2)]
+    pages, lengths, new = i32(table), i32([longest, 300]), i32([T, T // 2])
+    cache = ph.PagedCache(pools[0], pools[1], pages, d_h)
+    q = queries(rng, (2, T, H, d_h), rows)
+    out, again = torch.zeros_like(q), torch.zeros_like(q)
+    sizes = ph.photon_paged_attn_workspace_bytes(cache, 2, T, H, None, 2)
+    ws, other = (torch.empty(sizes, dtype=torch.uint8, device="cuda") for _ in range(2))
+
+    def call(to, workspace):
+        ph.photon_paged_attn(q, cache, lengths, to, n_new=new, n_splits=2, workspace=workspace)
+
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        call(out, ws)
+    for step in range(4):
+        lengths.copy_(i32([longest - 37 * step, 300 - 90 * step]))
+        pages.copy_(i32(table[:, ::-1].copy() if step % 2 else table))
+        q.copy_(queries(rng, (2, T, H, d_h), rows))
+        out.fill_(5.0)
+        again.fill_(5.0)
+        graph.replay()
+        call(again, other)
+        torch.cuda.synchronize()
+        assert torch.equal(out, again) and not (out == 0).all()
