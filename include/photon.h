@@ -245,7 +245,8 @@ typedef struct photon_paged_cache {   /* host struct of device pointers, read du
  *   q, q_out   both NULL, or rows [Bt*T] of [H, d_h] dt, q_stride and q_out_stride elements apart: q_out receives the rows of q,
  *              rotated alike (q_out == q with one stride rotates in place; other overlaps are not allowed)
  *   start      [Bt] int32, device, or NULL: 0 (a prompt)
- *   n_new      [Bt] int32, device, or NULL: T; only the first n_new[b] rows of sequence b are used (a padded batch)
+ *   n_new      [Bt] int32, device, or NULL: T; only the first n_new[b] rows of sequence b are used (a padded batch:
+ *              the others may hold anything, in memory that may be read)
  *   position   [Bt][T] int32, device, or NULL: start[b] + t; the rotary position of a row where it is not its place (nodes of a
  *              drafted tree sit at their depth).  Any value; angles are formed to 2^-29 turns
  *   rope_theta 0: no rotation; else >= 1 and d_h even
@@ -272,7 +273,7 @@ PHOTON_API int32_t photon_paged_cache_move(const photon_paged_cache* cache, cons
  * the seq_len[b] entries are the queries' own (written before).  Query t < n_new[b] sees all entries before them and, of the own
  * ones, those up to t; or, with `tree`, own entry j where bit j of tree[b][t] is set (its ancestors and itself):
  *     out[b,t,h,:] = softmax(scale * q[b,t,h,:] . K) V   over what it sees; nothing: zeros.
- *   q        rows [Bt*T] of [H, d_h] dt, q_stride elements from one to the next
+ *   q        rows [Bt*T] of [H, d_h] dt, q_stride elements from one to the next; those past n_new[b] may hold anything
  *   seq_len  [Bt] int32, device; values outside [0, S_max] count as the nearer end.  Own entries before entry 0 are not there
  *   n_new    [Bt] int32, device, or NULL: T; queries past n_new[b] are skipped, their rows of out left as they were
  *   tree     [Bt][T] uint64, device, or NULL.  T <= 64 with it; bits n_new[b] and up count for nothing
