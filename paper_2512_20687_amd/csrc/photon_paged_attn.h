@@ -21,7 +21,7 @@
 // entries, 16.8 MB: 12.0 us in two launches, of which the merge is 3).
 //
 // Precision.  Products of bf16 and E4M3 entries (which bf16 holds exactly) run on the bf16 matrix cores.  fp32 queries enter as three
-// bf16 parts, weights as two parts (17 bits; the result is rounded to 9) for bf16 rows and as three for fp32 rows.
+// bf16 parts and so do weights, whatever the rows are: all of their 24 bits.
 #pragma once
 #include <float.h>
 
@@ -132,7 +132,7 @@ template <typename KV, typename T, int NB> struct PagedTypes {
   static constexpr int DP = 32 * NB, TILES = 2 * NB;                             // TILES of 16 elements: the value products of a row tile
   static constexpr int K_WORDS = 2 * NB * (int)sizeof(KV);                       // of a lane, per tile of 16 entries
   static constexpr int V_BYTES = 2 * NB * (int)sizeof(KV), V_WORDS = V_BYTES < 4 ? 1 : V_BYTES / 4;   // of a lane, per entry
-  static constexpr int Q_PARTS = F32 || sizeof(T) == 2 ? 1 : 3, P_PARTS = sizeof(T) == 2 ? 2 : 3;
+  static constexpr int Q_PARTS = F32 || sizeof(T) == 2 ? 1 : 3, P_PARTS = 3;
   static constexpr int Q_WORDS = F32 ? 8 * NB : 4 * NB * Q_PARTS;
 };
 

@@ -202,18 +202,23 @@ template <int NB, int WAVES, int PAGES> __global__ __launch_bounds__(WAVES * 64,
           some = __builtin_amdgcn_ballot_w64(bad && used) != 0;
         }
       }
-      bf16x8_t p[R][2];
+      bf16x8_t p[R][Y::P_PARTS];
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        uint4_t high, low;
+        uint4_t w[Y::P_PARTS];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float x = s[r][8 * half + 2 * i], y = s[r][8 * half + 2 * i + 1];
-          high[i] = high_halves(x, y);
-          low[i] = pack_bf16x2(x - high_part(x), y - high_part(y));
+          float x = s[r][8 * half + 2 * i], y = s[r][8 * half + 2 * i + 1];
+#pragma unroll
+          for (int part = 0; part + 1 < Y::P_PARTS; ++part) {
+            w[part][i] = high_halves(x, y);
+            x -= high_part(x);
+            y -= high_part(y);
+          }
+          w[Y::P_PARTS - 1][i] = pack_bf16x2(x, y);
         }
-        p[r][0] = as_bf16x8(high);
-        p[r][1] = as_bf16x8(low);
+#pragma unroll
+        for (int part = 0; part < Y::P_PARTS; ++part) p[r][part] = as_bf16x8(w[part]);
       }
       constexpr int SIDE = 2;                                                // operands side by side, as above, and as many requested ahead
       uint4_t ahead[SIDE];
@@ -250,7 +255,7 @@ template <int NB, int WAVES, int PAGES> __global__ __launch_bounds__(WAVES * 64,
           }
         }
 #pragma unroll
-        for (int part = 1; part >= 0; --part)
+        for (int part = Y::P_PARTS - 1; part >= 0; --part)
 #pragma unroll
           for (int t = 0; t < SIDE; ++t)
 #pragma unroll
