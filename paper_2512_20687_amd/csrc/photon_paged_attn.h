@@ -2,9 +2,9 @@
 //
 // Mathematics.  For the rows q_r of a stream (token t, query head h; T * H / H_kv of them share a K/V head), one pass over the
 // entries keeps per row the reference top_r, the sum l_r = sum_j 2^(s_rj - top_r) and o_r = sum_j 2^(s_rj - top_r) V_j, with
-// s_rj = q_r . K_j * scale * log2 e.  top_r rises only when weights pass RAISE (then l_r and o_r shrink), so that most steps need
-// nothing from another lane.  The result is o_r / l_r; parts of the entries are put together as means weighted by
-// l_r 2^top_r.
+// s_rj = q_r . K_j * scale * log2 e.  top_r rises only when a lane's weights add up to more than 1 (then l_r and o_r shrink), and to 8 above
+// the largest score, so that most steps need nothing from another lane and yet no weight is above 1: |o_r| stays within the sum of |V_j|.
+// The result is o_r / l_r; parts of the entries are put together as means weighted by l_r 2^top_r.
 //
 // Operands.  A wave takes R tiles of 16 rows over steps of 32 entries, in registers alone:
 //   S^T = K Q^T   A: 16 entries x elements, a lane's operand is what it loads of one entry's row; B: 16 rows x elements.  Lane
@@ -35,7 +35,8 @@ namespace photon {
 constexpr int PAGED_STEP = 32;                 // entries of a step
 constexpr int PAGED_WAVES = 4;                 // of a workgroup
 constexpr int64_t PAGED_MOST_ROWS = (1ll << 31) - 4096;   // that share a K/V head: row numbers, tiles' ends among them, are int32
-constexpr float PAGED_RAISE = 256.f;          // sum of a lane's eight weights of a step from which on the reference rises
+constexpr float PAGED_ABOVE = 8.f;             // a reference that rises is set so many powers of two above the row's largest weight
+constexpr float PAGED_RAISE = 1.f;             // sum of a lane's weights of a step from which on the reference rises
 constexpr float PAGED_LOWEST = -FLT_MAX;       // a row's reference before it saw a score
 
 struct PagedAttnArgs {
@@ -383,7 +384,7 @@ template <int R, int N> __device__ __forceinline__ void settle(f32x4_t (&d)[R][N
 }
 
 // Weights of a lane's scores d of its rows: p = 2^(d scale - top).  Whether one exceeds the reference too far is told by the sums, so
-// that an ordinary step has no comparisons; then references become the rows' maxima, and what was summed shrinks.  The product with
+// that an ordinary step has no comparisons; then references rise to ABOVE over the rows' maxima, and what was summed shrinks.  The product with
 // the scale is rounded, as the reference was: fused with the subtraction it would keep digits that the reference lost, which are an
 // exponent of their own once scores pass 2^24.  CAREFUL: 0 where `seen` has no bit.
 template <bool CAREFUL, int R, int N, int TILES>
@@ -418,7 +419,7 @@ __device__ __forceinline__ void paged_weights(const f32x4_t (&d)[R][N], float sc
 #pragma unroll
       for (int i = 0; i < 4 * N; ++i)
         if (!CAREFUL || ((seen[r] >> i) & 1u)) highest = fmaxf(highest, rounded_product(d[r][i / 4][i % 4], scale));
-      const float higher = fmaxf(top[r], over_row(highest, [](float x, float y) { return fmaxf(x, y); }));
+      const float higher = fmaxf(top[r], over_row(highest, [](float x, float y) { return fmaxf(x, y); }) + PAGED_ABOVE);
       const float shrink = fast_exp2(top[r] - higher);
       top[r] = higher;
       sum[r] *= shrink;

@@ -1,0 +1,89 @@
+"""The paged attention at the ends of fp32: values and scores as large as it holds, and infinities.
+
+Tolerances as in tests/test_gpu_paged_attn.py: relative to A = sum(p |v|), whatever its size."""
+import numpy as np
+import pytest
+import torch
+
+import paged_plain as plain
+from test_gpu_paged_attn import KV, check, i32
+from test_gpu_paged_wide import Many
+from util import require_gpu
+
+pytestmark = pytest.mark.gpu
+TYPES = [(torch.bfloat16, "bf16"), (torch.float32, "bf16"), (torch.float32, "f32"), (torch.bfloat16, "f32")]
+P, D_H, PAST = 32, 64, 250
+
+
+@pytest.fixture(scope="module", params=["few streams", "many streams"])
+def ph(request):
+    require_gpu()
+    import paper_2512_20687_amd as m
+    m.load_library()
+    return m if request.param == "few streams" else Many(m, 64)
+
+
+def pages_of(x, kv):
+    """Entries [n, d_h] of one head as a pool, entry s in row s % P of page s / P."""
+    pool = torch.zeros((-(-x.shape[0] // P), 1, P, D_H))
+    pool.view(-1, D_H)[: x.shape[0]] = torch.as_tensor(x)
+    return pool.to(KV[kv])
+
+
+def run(ph, rows, kv, q, k, v, splits, scale=None):
+    """out [T, H, d_h] in float64, and what the kernel was given: q, pools, table."""
+    pools = [pages_of(x, kv) for x in (k, v)]
+    table = np.arange(pools[0].shape[0], dtype=np.int32)[None]
+    cache = ph.PagedCache(pools[0].cuda(), pools[1].cuda(), i32(table), D_H)
+    q = torch.as_tensor(q, dtype=torch.float32).to(rows)[None].cuda()
+    out = torch.full_like(q, 5.0)
+    ws = torch.empty(ph.photon_paged_attn_workspace_bytes(cache, 1, q.shape[1], q.shape[2], None, splits) + 16, dtype=torch.uint8, device="cuda")
+    ph.photon_paged_attn(q, cache, i32([k.shape[0]]), out, n_splits=splits, workspace=ws, scale=scale)
+    return out, q, pools, table
+
+
+@pytest.mark.parametrize("rows,kv", TYPES)
+@pytest.mark.parametrize("T", [1, 20, 40])
+@pytest.mark.parametrize("at", [3, 35, 130, 249])
+def test_a_large_value_under_a_score_that_rises(ph, rows, kv, T, at):
+    """One entry is ahead of all others by so many powers of two in weight, and its V is 2^126, all others' 0: a row's result is 2^126
+    times the entry's share, wherever the reference of the others' weights was."""
+    k, v = np.zeros((PAST + T, D_H), np.float32), np.zeros((PAST + T, D_H), np.float32)
+    k[at, 0] = 1
+    v[at] = 2.0 ** 126
+    every = [0.0, 0.5, 2.9, 5.0, 7.2, 7.9, 8.1, 15.9, 120.0]
+    for rises in [[rise] for rise in every] + [every]:                # alone, and side by side: a wave's rows raise theirs together
+        q = np.zeros((T, len(rises), D_H), np.float32)
+        q[..., 0] = np.array(rises) * np.log(2.0)
+        for splits in (1, 2):
+            out, given, pools, table = run(ph, rows, kv, q, k, v, splits, scale=1.0)
+            check(out, given, pools, table, [PAST + T], [T], D_H, scale=1.0)
+
+
+@pytest.mark.parametrize("rows,kv", TYPES)
+@pytest.mark.parametrize("T", [1, 40])
+def test_values_that_add_up_to_the_largest(ph, rows, kv, T):
+    """Scores that rise by up to 2^8 in weight from step to step, and V of up to 2^119.5: the sum over 290 entries stays below 2^128."""
+    rng = np.random.default_rng(T)
+    k = np.zeros((PAST + T, D_H), np.float32)
+    k[:, 0] = np.arange(PAST + T) // 32 + rng.uniform(0, 1, PAST + T)
+    v = (rng.uniform(0.5, 1.0, (PAST + T, D_H)) * np.where(rng.uniform(size=D_H) < 0.5, -1, 1) * 2.0 ** 119.5).astype(np.float32)
+    for slopes in ([1.0], [3.0], [5.0], [5.4], [-5.4], [0.0, 1.0, 5.0, -5.4]):
+        q = np.zeros((T, len(slopes), D_H), np.float32)
+        q[..., 0] = np.array(slopes)
+        for splits in (1, 3):
+            out, given, pools, table = run(ph, rows, kv, q, k, v, splits, scale=1.0)
+            check(out, given, pools, table, [PAST + T], [T], D_H, scale=1.0)
+
+
+@pytest.mark.parametrize("rows,kv", TYPES)
+@pytest.mark.parametrize("T", [1, 40])
+@pytest.mark.parametrize("exponent", [-60, -100, -112])
+def test_small_values(ph, rows, kv, T, exponent):
+    """V of about 2^-112: as exact as elsewhere."""
+    rng = np.random.default_rng(T)
+    k, v = (rng.standard_normal((PAST + T, D_H)).astype(np.float32) for _ in range(2))
+    q = rng.standard_normal((T, 4, D_H)).astype(np.float32)
+    out, given, pools, table = run(ph, rows, kv, q, k, v * np.float32(2.0 ** exponent), 1)
+    x = torch.ldexp(out.float(), torch.tensor(-exponent, device="cuda")).to(out.dtype)
+    check(x, given, [pools[0], torch.ldexp(pools[1].float(), torch.tensor(-exponent)).to(pools[1].dtype)], table, [PAST + T], [T], D_H)
