@@ -5,6 +5,7 @@
 // s_rj = q_r . K_j * scale * log2 e.  top_r rises only when a lane's weights add up to more than 1 (then l_r and o_r shrink), and to 8 above
 // the largest score, so that most steps need nothing from another lane and yet no weight is above 1: |o_r| stays within the sum of |V_j|.
 // The result is o_r / l_r; parts of the entries are put together as means weighted by l_r 2^top_r.
+// References are kept, compared and stored as half of that exponent: log2 e times a score of up to FLT_MAX would pass it.
 //
 // Operands.  A wave takes R tiles of 16 rows over steps of 32 entries, in registers alone:
 //   S^T = K Q^T   A: 16 entries x elements, a lane's operand is what it loads of one entry's row; B: 16 rows x elements.  Lane
@@ -35,9 +36,9 @@ namespace photon {
 constexpr int PAGED_STEP = 32;                 // entries of a step
 constexpr int PAGED_WAVES = 4;                 // of a workgroup
 constexpr int64_t PAGED_MOST_ROWS = (1ll << 31) - 4096;   // that share a K/V head: row numbers, tiles' ends among them, are int32
-constexpr float PAGED_ABOVE = 8.f;             // a reference that rises is set so many powers of two above the row's largest weight
+constexpr float PAGED_ABOVE = 4.f;             // a reference that rises is set so far above the row's largest score: weights of 2^-8
 constexpr float PAGED_RAISE = 1.f;             // sum of a lane's weights of a step from which on the reference rises
-constexpr float PAGED_LOWEST = -FLT_MAX;       // a row's reference before it saw a score
+constexpr float PAGED_LOWEST = -FLT_MAX;       // a row's reference before it saw a score: below every score that fp32 holds, halved
 
 struct PagedAttnArgs {
   PagedPools pool;
@@ -49,7 +50,7 @@ struct PagedAttnArgs {
   int32_t* status;
   int64_t q_stride;
   int32_t S_max, Bt, T, H, group, row_groups, n_splits, units;   // units: streams * splits
-  float scale_log2e;
+  float half_scale;                            // scale * log2 e / 2
   bool q_pieces, out_pieces;                   // rows of q, of out: aligned to 4 elements
 };
 
@@ -386,16 +387,23 @@ template <int R, int N> __device__ __forceinline__ void settle(f32x4_t (&d)[R][N
 // Weights of a lane's scores d of its rows: p = 2^(d scale - top).  Whether one exceeds the reference too far is told by the sums, so
 // that an ordinary step has no comparisons; then references rise to ABOVE over the rows' maxima, and what was summed shrinks.  The product with
 // the scale is rounded, as the reference was: fused with the subtraction it would keep digits that the reference lost, which are an
-// exponent of their own once scores pass 2^24.  CAREFUL: 0 where `seen` has no bit.
+// exponent of their own once scores pass 2^24.  Where it passes FLT_MAX, or no score was seen before, sums are infinite or NaN; then,
+// and with care, scores are halved as references are (scaling by 2 rounds nothing, so that weights are the same bits in either form).
+// CAREFUL: 0 where `seen` has no bit.
 template <bool CAREFUL, int R, int N, int TILES>
-__device__ __forceinline__ void paged_weights(const f32x4_t (&d)[R][N], float scale, const uint32_t (&seen)[R], float (&top)[R], float (&sum)[R],
+__device__ __forceinline__ void paged_weights(const f32x4_t (&d)[R][N], float half_scale, const uint32_t (&seen)[R], float (&top)[R], float (&sum)[R],
                                               f32x4_t (&acc)[R][TILES], float (&p)[R][4 * N]) {
   float s[R];
-  auto weigh = [&]() {
+  const float scale = 2.f * half_scale;
+  auto weigh = [&](auto halved) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
+      const float whole = rounded_product(top[r], 2.f);          // may be infinite: fused with the subtraction it would not be
 #pragma unroll
-      for (int i = 0; i < 4 * N; ++i) p[r][i] = rounded_product(d[r][i / 4][i % 4], scale) - top[r];
+      for (int i = 0; i < 4 * N; ++i) {
+        const float x = d[r][i / 4][i % 4];
+        p[r][i] = decltype(halved)::value ? 2.f * (rounded_product(x, half_scale) - top[r]) : rounded_product(x, scale) - whole;
+      }
       if constexpr (CAREFUL) {
 #pragma unroll
         for (int i = 0; i < 4 * N; ++i) p[r][i] = (seen[r] >> i) & 1u ? p[r][i] : -INFINITY;
@@ -409,24 +417,24 @@ __device__ __forceinline__ void paged_weights(const f32x4_t (&d)[R][N], float sc
       if constexpr (N == 4) s[r] += part[2] + part[3];
     }
   };
-  weigh();
-  bool above = s[0] > PAGED_RAISE;
-  if constexpr (R == 2) above = above || s[1] > PAGED_RAISE;
+  weigh(std::bool_constant<CAREFUL>{});
+  bool above = !(s[0] <= PAGED_RAISE);
+  if constexpr (R == 2) above = above || !(s[1] <= PAGED_RAISE);
   if (__builtin_expect(__builtin_amdgcn_ballot_w64(above) != 0, 0)) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       float highest = PAGED_LOWEST;
 #pragma unroll
       for (int i = 0; i < 4 * N; ++i)
-        if (!CAREFUL || ((seen[r] >> i) & 1u)) highest = fmaxf(highest, rounded_product(d[r][i / 4][i % 4], scale));
+        if (!CAREFUL || ((seen[r] >> i) & 1u)) highest = fmaxf(highest, rounded_product(d[r][i / 4][i % 4], half_scale));
       const float higher = fmaxf(top[r], over_row(highest, [](float x, float y) { return fmaxf(x, y); }) + PAGED_ABOVE);
-      const float shrink = fast_exp2(top[r] - higher);
+      const float shrink = fast_exp2(2.f * (top[r] - higher));
       top[r] = higher;
       sum[r] *= shrink;
 #pragma unroll
       for (int j = 0; j < TILES; ++j) acc[r][j] *= shrink;
     }
-    weigh();
+    weigh(std::true_type{});
   }
 #pragma unroll
   for (int r = 0; r < R; ++r) sum[r] += s[r];
@@ -555,7 +563,7 @@ __global__ __launch_bounds__(PAGED_WAVES * 64, paged_two_waves(32 * NB, R, sizeo
 #pragma unroll
       for (int r = 0; r < R; ++r) seen[r] = q.template seen<2>(a, r, base, g, n, past, there);
     }
-    paged_weights<CAREFUL, R, 2, TILES>(d, a.scale_log2e, seen, top, sum, acc, s);
+    paged_weights<CAREFUL, R, 2, TILES>(d, a.half_scale, seen, top, sum, acc, s);
     bool some = false;                                                      // an infinity or NaN that some row sees
     if constexpr (CAREFUL) {
       // Entries that no row sees may hold anything: zeros.
@@ -677,7 +685,7 @@ __global__ __launch_bounds__(PAGED_WAVES * 64, paged_two_waves(32 * NB, R, sizeo
       for (int w = 0; w < KW; ++w) w_top = fmaxf(w_top, stats[of * KW + w][i][0]);
 #pragma unroll
       for (int w = 0; w < KW; ++w) {
-        weight[w] = stats[of * KW + w][i][1] * fast_exp2(stats[of * KW + w][i][0] - w_top);
+        weight[w] = stats[of * KW + w][i][1] * fast_exp2(2.f * (stats[of * KW + w][i][0] - w_top));
         w_sum += weight[w];
       }
       const float inverse = w_sum == 0.f ? 0.f : 1.f / w_sum;
@@ -708,12 +716,12 @@ template <typename T, int NB, int SIDE> __global__ __launch_bounds__(256) void p
 #pragma unroll 8
   for (int s = 0; s < a.n_splits; ++s) top = fmaxf(top, stats[s].x);
 #pragma unroll 8
-  for (int s = 0; s < a.n_splits; ++s) sum += stats[s].y * fast_exp2(stats[s].x - top);
+  for (int s = 0; s < a.n_splits; ++s) sum += stats[s].y * fast_exp2(2.f * (stats[s].x - top));
   const float inverse = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll 4
   for (int s = side; s < a.n_splits; s += SIDE) {
     const float4_t y = *reinterpret_cast<const float4_t*>(values + (int64_t)s * DP);
-    const float w = stats[s].y * fast_exp2(stats[s].x - top) * inverse;
+    const float w = stats[s].y * fast_exp2(2.f * (stats[s].x - top)) * inverse;
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] = fmaf(y[e], w, o[e]);
   }

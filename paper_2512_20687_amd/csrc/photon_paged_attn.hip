@@ -102,7 +102,7 @@ extern "C" int32_t photon_paged_attn(const photon_paged_cache* cache, const void
   PHOTON_REQUIRE((units + 7) * groups <= (int64_t)0xffffffff / 512 && (int64_t)Bt * T * H <= (int64_t)0xffffffff / 32, PHOTON_ERR_UNSUPPORTED,
                  "%s: Bt=%d, T=%d, H=%d, n_splits=%d are too many workgroups", __func__, Bt, T, H, n_splits);
   a.row_groups = (int32_t)groups; a.units = (int32_t)units;
-  a.scale_log2e = scale * LOG2E;
+  a.half_scale = scale * (0.5f * LOG2E);
   a.q_pieces = d_h % 4 == 0 && q_stride % 4 == 0 && element_aligned(q, 4 * esz);
   a.out_pieces = d_h % 4 == 0 && element_aligned(out, 4 * esz);
   hipStream_t st = (hipStream_t)stream;

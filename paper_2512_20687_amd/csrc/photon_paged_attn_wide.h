@@ -168,7 +168,7 @@ template <int NB, int WAVES, int PAGES> __global__ __launch_bounds__(WAVES * 64,
 #pragma unroll
       for (int r = 0; r < R; ++r) seen[r] = q.template seen<4>(a, r, base, g, n, past, there);
     }
-    paged_weights<CAREFUL, R, 4, TILES>(d, a.scale_log2e, seen, top, sum, acc, s);
+    paged_weights<CAREFUL, R, 4, TILES>(d, a.half_scale, seen, top, sum, acc, s);
   };
   // The values under those weights, V in LDS at `in`, 32 entries at a time.
   auto add_values = [&](auto careful, const char* in, int base, uint32_t now) {

@@ -87,3 +87,37 @@ def test_small_values(ph, rows, kv, T, exponent):
     out, given, pools, table = run(ph, rows, kv, q, k, v * np.float32(2.0 ** exponent), 1)
     x = torch.ldexp(out.float(), torch.tensor(-exponent, device="cuda")).to(out.dtype)
     check(x, given, [pools[0], torch.ldexp(pools[1].float(), torch.tensor(-exponent)).to(pools[1].dtype)], table, [PAST + T], [T], D_H)
+
+
+@pytest.mark.parametrize("rows,kv", TYPES)
+@pytest.mark.parametrize("T,past", [(1, 0), (1, 7), (40, 0), (1, 250), (20, 250), (40, 250)])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("scale", [1.0, 4.0])
+def test_scores_at_the_end_of_fp32(ph, rows, kv, T, past, sign, scale):
+    """Scores of 2.9e38 to 3.3e38 of either sign, in any order: finite in fp32, though not times log2 e.  The largest that a row sees takes
+    all; neighbours are 2^-7 of it apart."""
+    rng = np.random.default_rng(past + T)
+    n = past + T
+    k = np.zeros((n, D_H), np.float32)
+    k[:, 0] = (1 + rng.permutation(n) % 16 / 128.0) * 2.0 ** 60
+    v = rng.standard_normal((n, D_H)).astype(np.float32)
+    q = np.zeros((T, 2, D_H), np.float32)
+    q[..., 0] = sign * 2.9e38 / 2.0 ** 60 / scale
+    for splits in (1, 2):
+        out, given, pools, table = run(ph, rows, kv, q, k, v, splits, scale=scale)
+        check(out, given, pools, table, [n], [T], D_H, scale=scale)
+
+
+@pytest.mark.parametrize("rows,kv", TYPES)
+@pytest.mark.parametrize("T", [1, 40])
+def test_a_scale_at_the_end_of_fp32(ph, rows, kv, T):
+    """scale = 3e38, whose product with log2 e is not finite, over scores of up to about 1."""
+    n = PAST + T
+    rng = np.random.default_rng(T)
+    k, v = np.zeros((n, D_H), np.float32), rng.standard_normal((n, D_H)).astype(np.float32)
+    k[:, 0] = rng.integers(-16, 17, n) / 16.0
+    q = np.zeros((T, 2, D_H), np.float32)
+    q[..., 0] = 2.0 ** -120
+    q[:, 1, 0] = 0.0
+    out, given, pools, table = run(ph, rows, kv, q, k, v, 1, scale=3e38)
+    check(out, given, pools, table, [n], [T], D_H, scale=float(np.float32(3e38)))
