@@ -216,6 +216,9 @@ template <typename T> __device__ __forceinline__ void store_result4(T* row, int 
 // What one row sees and another does not may be an infinity or NaN, and 0 times it is not 0.  Such steps put zeros in the products, and
 // a second product tells which rows see which: operands of 2^16 for NaN, 2^8 for -infinity, 1 for infinity, 0 else, times 1 where a
 // row sees an entry.  Sums over 32 entries are exact, and their digits say what is added to the row's element.
+//
+// What all rows see may be infinite, too, and a weight, or one of its parts, may be 0.  Ordinary steps do not look: elements that end
+// infinite or NaN are found out at the end, see restore_unbounded().
 __device__ __forceinline__ float unbounded_code(float x) { return fabsf(x) <= FLT_MAX ? 0.f : x != x ? 0x1p16f : x < 0.f ? 0x1p8f : 1.f; }
 __device__ __forceinline__ uint4_t unbounded_codes(uint4_t w) {               // of bf16 pairs
 #pragma unroll
@@ -440,6 +443,89 @@ __device__ __forceinline__ void paged_weights(const f32x4_t (&d)[R][N], float ha
   for (int r = 0; r < R; ++r) sum[r] += s[r];
 }
 
+// Whether one of a lane's sums is infinite or NaN.
+template <int R, int TILES> __device__ __forceinline__ bool any_unbounded(const f32x4_t (&acc)[R][TILES]) {
+  f32x4_t x = acc[0][0] * 0.f;                                               // four chains, not one of them all
+#pragma unroll
+  for (int i = 1; i < R * TILES; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = fmaf(acc[i / TILES][i % TILES][e], 0.f, x[e]);
+  const float y = (x[0] + x[1]) + (x[2] + x[3]);
+  return y != y;
+}
+
+// Elements of a wave's rows that are infinite or NaN: infinite, or NaN, as the V that the row sees in the steps `step`, `step` + `by`, ... before
+// `end` are, whatever their weights were; left as they are where none of those is (weights are NaN, sums too large).  Every element of V is
+// looked at once more, which nothing else waits for.  element(j, i): which of a head's acc[.][j][i % 4] of lane group i / 4 is.
+template <typename KV, typename Rows, int R, int TILES, typename Element>
+__device__ __forceinline__ void restore_unbounded(const PagedAttnArgs& a, const Rows& q, f32x4_t (&acc)[R][TILES], const int32_t* table, int hk, int n,
+                                                  int past, int step, int end, int by, int c, int g, Element element) {
+  uint32_t found[R][TILES] = {};                                             // three bits an element: infinity, -infinity, NaN
+#pragma unroll 1
+  for (; step < end; step += by) {
+    int64_t at[2];
+    bool there[2], bad = false;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int entry = step * PAGED_STEP + 16 * i;
+      at[i] = paged_place(a, table[min(entry, n - 1) >> a.pool.page_shift], hk, entry, n, bad);
+      there[i] = at[i] >= 0;
+    }
+    uint4_t sees[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) sees[r] = seen_operand(q.template seen<2>(a, r, step * PAGED_STEP, g, n, past, there));
+#pragma unroll
+    for (int j = 0; j < TILES; ++j) {
+      float code[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint8_t* from = a.pool.v + (at[i / 4] < 0 ? 0 : at[i / 4]) + (4 * g + i % 4) * a.pool.row_bytes;
+        const float x = to_f32<KV>(reinterpret_cast<const KV*>(from)[element(j, c)]);
+        code[i] = step * PAGED_STEP + (i / 4) * 16 + 4 * g + i % 4 < n && there[i / 4] ? unbounded_code(x) : 0.f;
+      }
+      const uint4_t codes = {high_halves(code[0], code[1]), high_halves(code[2], code[3]), high_halves(code[4], code[5]), high_halves(code[6], code[7])};
+      f32x4_t digits[R][1];
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        digits[r][0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(codes), as_bf16x8(sees[r]), f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+      settle(digits);
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t t = (uint32_t)digits[r][0][e];
+          found[r][j] |= ((t & 0xffu ? 1u : 0u) | (t & 0xff00u ? 2u : 0u) | (t >> 16 ? 4u : 0u)) << (3 * e);
+        }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int j = 0; j < TILES; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t t = (found[r][j] >> (3 * e)) & 7u;
+        if (t != 0 && !(fabsf(acc[r][j][e]) <= FLT_MAX)) acc[r][j][e] = t == 1 ? INFINITY : t == 2 ? -INFINITY : NAN;
+      }
+}
+
+// o = the sum of y w over the pairs that `each` hands on, where y is a mean of what was seen: an infinite one stays infinite however small
+// its weight is.  Ordinary sums pay for one comparison.
+template <typename Each> __device__ __forceinline__ void weighted_sum(float (&o)[4], Each each) {
+  each([&](const float4_t& y, float w) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = fmaf(y[e], w, o[e]);
+  });
+  if (__builtin_expect(!(fabsf(fmaf(o[0], 0.f, fmaf(o[1], 0.f, fmaf(o[2], 0.f, o[3] * 0.f)))) <= 0.f), 0)) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = 0.f;
+    each([&](const float4_t& y, float w) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = fabsf(y[e]) <= FLT_MAX ? fmaf(y[e], w, o[e]) : o[e] + y[e];
+    });
+  }
+}
+
 // R row tiles a wave, RW waves side by side over rows; the KW waves of the same rows deal the steps among themselves.  Fewer waves lose even
 // where streams are many (256 x 16 ragged streams of up to 2048 entries of 64 fp32-row bf16 pages: 206 us, 215 with two waves, 231 with one).
 // Two waves a SIMD are asked for wherever their registers suffice: left to itself, the compiler moves sums to accumulation registers and back
@@ -447,9 +533,14 @@ __device__ __forceinline__ void paged_weights(const f32x4_t (&d)[R][N], float ha
 // 4096: 1439 us, now 1306).  Two tiles of 128 elements with fp32 rows or pages spill 130 registers and more at two waves (512 rows, 32
 // streams of 2000: 84 us, 54 at one).
 constexpr bool paged_two_waves(int d_p, int tiles, bool f32) { return !(d_p == 128 && tiles == 2 && f32); }
+// Waves a SIMD that are asked for.  One tile of 32 fp32 elements takes 97 registers if it may, one more than five waves have (3480 streams of
+// up to 7 entries: 17.4 us, 16.0 with five).
+template <typename KV, typename T, int NB, int R> constexpr int paged_least_waves() {
+  return sizeof(KV) == 4 && NB == 1 && R == 1 ? 5 : paged_two_waves(32 * NB, R, sizeof(KV) == 4 || sizeof(T) == 4) ? 2 : 1;
+}
 
 template <typename KV, typename T, int NB, int R, int RW>
-__global__ __launch_bounds__(PAGED_WAVES * 64, paged_two_waves(32 * NB, R, sizeof(KV) == 4 || sizeof(T) == 4) ? 2 : 1) void paged_attn_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(PAGED_WAVES * 64, (paged_least_waves<KV, T, NB, R>())) void paged_attn_kernel(PagedAttnArgs a) {
   using Y = PagedTypes<KV, T, NB>;
   constexpr int DP = Y::DP, TILES = Y::TILES, KW = PAGED_WAVES / RW, PITCH = DP + 4;
   __shared__ __align__(16) float results[PAGED_WAVES * 16 * PITCH];
@@ -655,6 +746,10 @@ __global__ __launch_bounds__(PAGED_WAVES * 64, paged_two_waves(32 * NB, R, sizeo
 #pragma unroll 1
   while (has_rows && step < s1) take(std::true_type{});
   settle(acc);
+  if constexpr (sizeof(KV) > 1) {                                            // E4M3 has no infinities
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(any_unbounded(acc)) != 0, 0) && has_rows)
+      restore_unbounded<KV>(a, q, acc, table, hk, n, past, s0 + kw, s1, KW, c, g, [](int j, int i) { return 2 * NB * i + j; });
+  }
   paged_say(a, bad, lane);
 
   // Results: lane (c, g) holds elements 8 NB g .. + 8 NB - 1 of its rows.  Each wave divides by its sum, and waves are put together as
@@ -689,12 +784,10 @@ __global__ __launch_bounds__(PAGED_WAVES * 64, paged_two_waves(32 * NB, R, sizeo
         w_sum += weight[w];
       }
       const float inverse = w_sum == 0.f ? 0.f : 1.f / w_sum;
+      weighted_sum(o, [&](auto add) {
 #pragma unroll
-      for (int w = 0; w < KW; ++w) {
-        const float4_t y = *reinterpret_cast<const float4_t*>(results + ((of * KW + w) * 16 + i) * PITCH + d);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = fmaf(y[e], weight[w] * inverse, o[e]);
-      }
+        for (int w = 0; w < KW; ++w) add(*reinterpret_cast<const float4_t*>(results + ((of * KW + w) * 16 + i) * PITCH + d), weight[w] * inverse);
+      });
       paged_emit<T, DP>(a, paged_row(a, b, hk, to), split, d, o, w_top, w_sum);
     }
   }
@@ -718,13 +811,11 @@ template <typename T, int NB, int SIDE> __global__ __launch_bounds__(256) void p
 #pragma unroll 8
   for (int s = 0; s < a.n_splits; ++s) sum += stats[s].y * fast_exp2(2.f * (stats[s].x - top));
   const float inverse = sum == 0.f ? 0.f : 1.f / sum;
+  weighted_sum(o, [&](auto add) {
 #pragma unroll 4
-  for (int s = side; s < a.n_splits; s += SIDE) {
-    const float4_t y = *reinterpret_cast<const float4_t*>(values + (int64_t)s * DP);
-    const float w = stats[s].y * fast_exp2(2.f * (stats[s].x - top)) * inverse;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = fmaf(y[e], w, o[e]);
-  }
+    for (int s = side; s < a.n_splits; s += SIDE)
+      add(*reinterpret_cast<const float4_t*>(values + (int64_t)s * DP), stats[s].y * fast_exp2(2.f * (stats[s].x - top)) * inverse);
+  });
   if constexpr (SIDE > 1) {
     *reinterpret_cast<float4_t*>(part + threadIdx.x * 4) = float4_t{o[0], o[1], o[2], o[3]};
     __syncthreads();

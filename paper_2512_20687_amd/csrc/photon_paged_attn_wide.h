@@ -333,6 +333,8 @@ template <int NB, int WAVES, int PAGES> __global__ __launch_bounds__(WAVES * 64,
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                         // no load outlives the workgroup's LDS
   settle(acc);
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(any_unbounded(acc)) != 0, 0) && has_rows)
+    restore_unbounded<bf16_t>(a, q, acc, table, hk, n, past, 2 * s0, 2 * s1, 1, c, g, [](int j, int i) { return 16 * j + i; });
   paged_say(a, bad_page, lane);
 
   // lane (c, g) holds elements 16 j + 4 g .. + 3 of its rows

@@ -108,6 +108,53 @@ def test_scores_at_the_end_of_fp32(ph, rows, kv, T, past, sign, scale):
         check(out, given, pools, table, [n], [T], D_H, scale=scale)
 
 
+def with_unbounded(k, v, see, x, scale):
+    """Row x [H, d_h]'s result where V has infinities and NaN: by their definition; elsewhere the finite one."""
+    ref, size = plain.attended(x, k, np.where(np.isfinite(v), v, 0.0), see, scale)
+    bad = np.where(np.isfinite(v[0][see]), 0.0, v[0][see])
+    with np.errstate(invalid="ignore"):
+        return ref + bad.sum(0), size
+
+
+@pytest.mark.parametrize("rows,kv", TYPES)
+@pytest.mark.parametrize("T", [1, 9, 40])
+@pytest.mark.parametrize("slope", [0.0, 1.0, 5.0, -5.0])
+def test_infinities_in_values(ph, rows, kv, T, slope):
+    """Infinities and NaN in V anywhere: what a row sees is in its result, with its sign, be its weight 1, 2^-80 or too small for fp32."""
+    rng = np.random.default_rng(T)
+    n = PAST + T
+    k, v = np.zeros((n, D_H), np.float32), rng.standard_normal((n, D_H)).astype(np.float32)
+    k[:, 0] = np.arange(n) // 4 * 4 / 32.0
+    k[:, 1:] = 0.25 * rng.standard_normal((n, D_H - 1))
+    q = rng.standard_normal((T, 3, D_H)).astype(np.float32)
+    q[..., 0] = slope
+    inf, nan = np.inf, np.nan
+    for e, d, x in ((0, 0, inf), (7, 1, -inf), (8, 5, inf), (140, 5, inf), (20, 33, inf), (240, 33, -inf), (130, 40, nan), (131, 62, nan), (9, 62, inf),
+                    (PAST - 1, 63, -inf), (n - 1, 17, inf), (PAST + T // 2, 18, -inf), (100, 24, inf), (101, 25, -inf), (199, 31, inf)):
+        v[e, d] = x
+    for splits in (1, 2, 12):
+        out, given, pools, table = run(ph, rows, kv, q, k, v, splits)
+        ks, vs = (plain.entries(plain.values(p), table[0], n, D_H) for p in pools)
+        got, x = out[0].float().cpu().numpy().astype(np.float64), given[0].float().cpu().numpy()
+        for t in range(T):
+            ref, size = with_unbounded(ks, vs, plain.seen(n, T, t), x[t], D_H ** -0.5)
+            fine = np.isfinite(ref)
+            np.testing.assert_array_equal(np.where(fine, 0.0, got[t]), np.where(fine, 0.0, ref), err_msg=str((splits, t)))
+            bound = 1e-5 * size.max() if rows == torch.float32 else 2.0 ** -8 * np.abs(ref) + 2.0 ** -15 * size
+            assert (np.abs(got[t][fine] - ref[fine]) <= np.broadcast_to(bound, ref.shape)[fine]).all(), (splits, t)
+
+
+def test_sums_that_are_too_large_stay_infinite(ph):
+    """Nothing infinite in V, but a sum that fp32 does not hold: what the sum became, not a smaller number."""
+    for rows, kv in TYPES:
+        for T in (1, 40):
+            n = PAST + T
+            k, v = np.zeros((n, D_H), np.float32), np.full((n, D_H), 2.0 ** 127, np.float32)
+            v[:, 1::2] = -v[:, 1::2]
+            out = run(ph, rows, kv, np.zeros((T, 2, D_H)), k, v, 1)[0].float()
+            assert not (out.abs() < 2.0 ** 126).any()
+
+
 @pytest.mark.parametrize("rows,kv", TYPES)
 @pytest.mark.parametrize("T", [1, 40])
 def test_a_scale_at_the_end_of_fp32(ph, rows, kv, T):
