@@ -281,9 +281,10 @@ PHOTON_API int32_t photon_paged_cache_move(const photon_paged_cache* cache, cons
  *   status   NULL, or a device word that PHOTON_STATUS_BAD_PAGE is ORed into
  *   S_max    the most entries that a sequence has, at most max_pages * page_size (a bound that is close chooses better splits)
  * Scores, softmax, weights and sums are in fp32 for either dt; a bf16 result is rounded once.  Entries that a query does not see
- * do not touch its result, whatever they hold; of those it does see, an infinity or NaN in V makes its element of the result one (NaN,
- * where infinities of both signs meet), whatever its weight is.  Results are finite wherever q . K, scale * q . K and, but for its rounding (2^-20 of
- * it), the sum of |V| over the entries seen are, in fp32.
+ * do not touch its result, whatever they hold.  Of those it does see, an infinity or NaN in V makes its element of the result one
+ * (NaN, where infinities of both signs meet), whatever its weight is; a score of -infinity is a weight of 0, and a query that has no
+ * other gets zeros.  Results are finite wherever q . K, scale * q . K and, but for its rounding (2^-20 of it), the sum of |V| over the
+ * entries seen are, in fp32.
  * The entries are split over n_splits workgroups per stream (0 = choose from shape and dt); partial results are merged in a fixed
  * order, so the result is run-to-run deterministic for a given n_splits.  The workspace holds them:
  * photon_paged_attn_workspace_bytes() of the same arguments, for either dt (0 bytes for n_splits == 1, or where 0 chooses 1; no

@@ -301,6 +301,13 @@ __device__ __forceinline__ void paged_say(const PagedAttnArgs& a, bool bad, int 
   if (bad && a.status && lane == 0) atomicOr(a.status, (int)PHOTON_STATUS_BAD_PAGE);
 }
 
+// What of an element x of q is left behind a part's 8 bits, for the next one.  Never 0 where entries may be infinite: 0 times infinity is NaN,
+// and x times it is not.  2^-30 of x is added, below the digits that parts hold of x, so that only what would be 0 changes.
+template <typename KV> __device__ __forceinline__ float rest_of_query(float part, float x) {
+  const float rest = part - high_part(part);
+  return sizeof(KV) == 2 ? fmaf(x, 0x1p-30f, rest) : rest;
+}
+
 // R tiles of 16 rows as a wave holds them: operands of the score products, and what each row sees.
 template <typename KV, typename T, int NB, int R> struct PagedRows {
   using Y = PagedTypes<KV, T, NB>;
@@ -335,8 +342,8 @@ template <typename KV, typename T, int NB, int R> struct PagedRows {
 #pragma unroll
               for (int part = 0; part < Y::Q_PARTS; ++part) {
                 w[r][(part * NB + f) * 4 + half * 2 + e / 2] = high_halves(u, v);
-                u -= high_part(u);
-                v -= high_part(v);
+                u = rest_of_query<KV>(u, x[e]);
+                v = rest_of_query<KV>(v, x[e + 1]);
               }
             }
           }

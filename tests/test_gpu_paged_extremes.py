@@ -144,6 +144,32 @@ def test_infinities_in_values(ph, rows, kv, T, slope):
             assert (np.abs(got[t][fine] - ref[fine]) <= np.broadcast_to(bound, ref.shape)[fine]).all(), (splits, t)
 
 
+@pytest.mark.parametrize("rows,kv", TYPES)
+@pytest.mark.parametrize("T", [1, 9, 40])
+@pytest.mark.parametrize("at", [0, 40, 130, 249, 250])
+def test_infinities_in_keys(ph, rows, kv, T, at):
+    """K of infinity: a query whose element there is negative does not see the entry, a positive one has no finite result.  Elements of few
+    digits, whose lower parts are 0, and of many."""
+    rng = np.random.default_rng(T)
+    n = PAST + T
+    k, v = (rng.standard_normal((n, D_H)).astype(np.float32) for _ in range(2))
+    k[at, 7] = np.inf
+    q = rng.standard_normal((T, 6, D_H)).astype(np.float32)
+    q[..., 7] = [-1.0, -1.2345678, 1.0, 2.0 ** -60, -(2.0 ** -60), 0.0]
+    for splits in (1, 2):
+        out, given, pools, table = run(ph, rows, kv, q, k, v, splits)
+        ks, vs = (plain.entries(plain.values(p), table[0], n, D_H) for p in pools)
+        got, x = out[0].float().cpu().numpy().astype(np.float64), given[0].float().cpu().numpy()
+        for t in range(T):
+            with np.errstate(invalid="ignore"):
+                ref, size = plain.attended(x[t], ks, vs, plain.seen(n, T, t), D_H ** -0.5)
+            fine = ~np.isnan(ref)
+            assert (fine.all(1) == [True, True, at > PAST + t, at > PAST + t, True, at > PAST + t]).all()
+            assert np.isnan(got[t][~fine]).all()
+            bound = 1e-5 * size[fine].max() if rows == torch.float32 else 2.0 ** -8 * np.abs(ref) + 2.0 ** -15 * size
+            assert (np.abs(got[t][fine] - ref[fine]) <= np.broadcast_to(bound, ref.shape)[fine]).all(), (splits, t)
+
+
 def test_sums_that_are_too_large_stay_infinite(ph):
     """Nothing infinite in V, but a sum that fp32 does not hold: what the sum became, not a smaller number."""
     for rows, kv in TYPES:
