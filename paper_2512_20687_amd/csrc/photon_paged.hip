@@ -149,10 +149,12 @@ __global__ __launch_bounds__(256) void paged_write_kernel(WriteArgs a, RopeTable
   if (a.rotate) {
     for (int y = tid; y < rows * a.half; y += blockDim.x) {
       const int r = quotient(y, a.half, a.by_half), i = y - r * a.half;
-      const int position = a.position ? a.position[(int64_t)b * a.T + t0 + r] : (int)((uint32_t)start + t0 + r);
-      const uint64_t phase = (uint64_t)(int64_t)position * rope.turns[i];
+      // the low word of the position and its sign: start + t may pass 2^31 (q_out is written all the same), and stays below 2^32
+      const int given = a.position ? a.position[(int64_t)b * a.T + t0 + r] : start;
+      const uint32_t low = (uint32_t)given + (a.position ? 0u : (uint32_t)(t0 + r)), frequency = (uint32_t)rope.turns[i];
+      const bool negative = given < 0 && (int)low < 0;
       // the nearest quarter turn is taken off before the phase becomes a float: what is left is at most an eighth
-      const uint32_t turn = (uint32_t)(phase >> 32), quarter = (turn + 0x20000000u) >> 30;
+      const uint32_t turn = __umulhi(low, frequency) + low * (uint32_t)(rope.turns[i] >> 32) - (negative ? frequency : 0u), quarter = (turn + 0x20000000u) >> 30;
       float sn, cs;
       sincospif((float)(int32_t)(turn - (quarter << 30)) * 0x1p-31f, &sn, &cs);
       const float co = quarter & 1 ? -sn : cs, si = quarter & 1 ? cs : sn;
