@@ -248,7 +248,7 @@ typedef struct photon_paged_cache {   /* host struct of device pointers, read du
  *   n_new      [Bt] int32, device, or NULL: T; only the first n_new[b] rows of sequence b are used (a padded batch:
  *              the others may hold anything, in memory that may be read)
  *   position   [Bt][T] int32, device, or NULL: start[b] + t; the rotary position of a row where it is not its place (nodes of a
- *              drafted tree sit at their depth).  Any value; angles are formed to 2^-29 turns
+ *              drafted tree sit at their depth).  Any value; angles are formed to 2^-27 turns
  *   rope_theta 0: no rotation; else >= 1 and d_h even
  *   status     NULL, or a device word: PHOTON_STATUS_CACHE_FULL is ORed into it when a row's entry is outside [0, max_pages *
  *              page_size) (it is not written), PHOTON_STATUS_BAD_PAGE as above.  q_out does not depend on either

@@ -153,7 +153,7 @@ __global__ __launch_bounds__(256) void paged_write_kernel(WriteArgs a, RopeTable
       const int given = a.position ? a.position[(int64_t)b * a.T + t0 + r] : start;
       const uint32_t low = (uint32_t)given + (a.position ? 0u : (uint32_t)(t0 + r)), frequency = (uint32_t)rope.turns[i];
       const bool negative = given < 0 && (int)low < 0;
-      // the nearest quarter turn is taken off before the phase becomes a float: what is left is at most an eighth
+      // the nearest quarter turn is taken off before the phase becomes a float: what is left is at most an eighth, rounded to 2^-28 turns
       const uint32_t turn = __umulhi(low, frequency) + low * (uint32_t)(rope.turns[i] >> 32) - (negative ? frequency : 0u), quarter = (turn + 0x20000000u) >> 30;
       float sn, cs;
       sincospif((float)(int32_t)(turn - (quarter << 30)) * 0x1p-31f, &sn, &cs);
@@ -314,7 +314,7 @@ extern "C" int32_t photon_paged_cache_write(const photon_paged_cache* cache, con
   RopeTable rope;
   if (a.rotate) {
     // theta^(-2i/d_h) / (2 pi) as fractions of 2^128, one a product of the one before with theta^(-2/d_h) as a fraction of 2^64, which is
-    // within 2^-65: within 2^-29 turns of the angle at every 32-bit position.
+    // within 2^-64: the last of 64 within 63 / (2 pi) 2^-64, which is 2^-28 turns at positions of up to 2^32.
     const long double ratio = powl((long double)rope_theta, -2.0L / d_h);
     const uint64_t r = ratio < 1.0L ? (uint64_t)ldexpl(ratio, 64) : 0;       // 0: all alike
     uint64_t high = 0x28be60db9391054aull, low = 0x7f09d5f47d4d3770ull;      // 1 / (2 pi)
