@@ -5,23 +5,30 @@ namespace photon {
 namespace {
 
 // Workgroups over the entries of a stream: as many as the chip holds at once (two a unit; one where a workgroup's registers fill it), but
-// none with fewer than two steps (wide: eight) a wave, and none where that leaves fewer than four: the merge is a launch.  Microseconds:
-// 16 streams of 2048 entries of 64 bf16 in 1, 2, 4, 8, 16 workgroups 16.7, 13.4, 10.5, 9.0, 8.3; of 512 in 1, 2, 4 7.5, 8.8, 8.1; 128 of
-// 8192 in 2, 4, 8 45.5, 45.0, 48.1; 32 of 32749 of 128 in 4, 8, 16 127, 99, 100; 256 rows over 128 streams of 4096 in 1, 2, 4 181, 125, 150;
-// 2048 rows over 16 of 8191 in 1, 2, 4 326, 196, 212.
+// none with less than a step a wave (wide: eight steps, which all waves take), and none where that leaves fewer than eight: the merge is a launch.
+// Microseconds, with 1, 2, 4, 8, 16 workgroups, the rule's marked:
+//   one row, 16 streams of 2048 entries of 64     fp32 33.6, 22.7, 15.7, 12.2, 10.7*      bf16 15.6, 13.5, 10.9, 9.8, 9.6*
+//   one row, 16 streams of 1024 of 64             fp32 17.8, 14.6, 11.5, 10.4*, 9.8       bf16 10.0, 10.9, 9.7, 9.4*, 9.8
+//   one row, 64 streams of 2048 of 64             fp32 35.0, 23.7, 18.2, 18.5*, 21.0      bf16 18.7, 15.3, 12.8, 12.8*, 13.4
+//   one row, 16 and 64 streams of 600 of 64       bf16 9.1*, 11.4, 10.7, 10.2, 9.9 and 9.0*, 11.0, 10.5, 11.2, 11.2; fp32 13.1*, 13.2, 11.6, 10.6, 9.8
+//   one row, 32 streams of 32749 of 128           bf16 414, 220, 125, 99, 100*
+//   20 rows, 8 streams of 3000 of 128             bf16 -, -, 21.6, 18.1, 16.8; 23 workgroups* 16.7
+//   256 rows, 128 streams of 4096 of 128          wide 214, 146*, 165
+//   2048 rows, 16 streams of 8191 of 128          wide 395, 236*, 251
 int paged_auto_splits(int Bt, int T, int H, int H_kv, int d_p, int64_t S_max, bool f32_rows, photon_dtype kv_dt) {
   const int64_t rows = (int64_t)T * (H / H_kv);
   const PagedTile tile = paged_tile(rows, (int64_t)Bt * H_kv, f32_rows, kv_dt);
   const int64_t groups = (int64_t)Bt * H_kv * ((rows + tile.rows() - 1) / tile.rows());
   const int64_t steps = (S_max + PAGED_STEP - 1) / PAGED_STEP;
   int64_t splits = (tile.tiles == 1 ? 512 : 256) / groups;
-  // Two tiles a wave leave more to merge: their second workgroup a unit has to have 32 steps a wave (128 rows over E4M3 pages, 256 streams of
-  // 4096 entries: 194 us with one split, 144 with two; 32 streams of 3000 in 8, 16: 34, 44).
+  // Two tiles a wave leave more to merge: their second workgroup a unit has to have 16 steps a wave (64 rows over 128 streams of 2000, 4000
+  // and 8000 entries of 128, with one split and with two: E4M3 pages 30.6 and 33.1, 55.5 and 51.0, 116 and 87 us; bf16 37.8 and 40.4, 73.9
+  // and 69.2, 133 and 119).
   const bool held = tile.tiles == 2 && !tile.wide && paged_two_waves(d_p, 2, f32_rows || kv_dt == PHOTON_F32);
-  if (held && steps * tile.waves / PAGED_WAVES / 32 >= 512 / groups) splits = 512 / groups;
-  const int64_t most = tile.wide ? steps / 8 : steps * tile.waves / (2 * PAGED_WAVES);
+  if (held && steps * tile.waves / PAGED_WAVES / 16 >= 512 / groups) splits = 512 / groups;
+  const int64_t most = tile.wide ? steps / 8 : steps * tile.waves / PAGED_WAVES;
   splits = splits > most ? most : splits;
-  if (!tile.wide && most < 4) splits = 1;
+  if (!tile.wide && most < 8) splits = 1;
   return (int)(splits < 1 ? 1 : splits > 256 ? 256 : splits);
 }
 int paged_most_splits(const photon_paged_cache* c, int Bt, int T, int H, int64_t S_max) {   // of either dtype of rows
