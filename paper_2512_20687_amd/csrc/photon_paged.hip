@@ -2,7 +2,7 @@
 //
 // Both are copies: bytes bound them.  An append reads k, v and q once and writes the entries and q_out once; a row's heads are
 // consecutive in memory, an entry's are head_bytes apart, so that every head of an entry is a run of whole 64- or 128-byte lines.
-// Measured: four prompts of 8192 rows (805 MB) 152 us, 5.3 TB/s where a copy reaches 4.9; 64 ragged prompts into E4M3 pages (167 MB) 34.1 us,
+// Measured: four prompts of 8192 rows (805 MB) 153 us, 5.3 TB/s where a copy reaches 4.9; 64 ragged prompts into E4M3 pages (167 MB) 34.4 us,
 // 4.9 TB/s; one entry of four sequences 7.5 us and 256 sequences' (10 MB) 8.1 us, which are the call's and a launch's.
 #include <math.h>
 
@@ -251,7 +251,8 @@ template <typename T, typename KV, int VEC> void launch_write(WriteArgs a, const
   const int64_t groups = (items + 255) / 256;
   const int threads = (int)(((items + groups - 1) / groups + 63) / 64 * 64);
   // Rows of a workgroup: as many as share a table of angles well, but fewer while workgroups are few: several rounds of them even out what
-  // their rows take (four prompts of 8192 rows with at least 2048, 4096, 8192 workgroups: 172, 164, 155 us; 64 ragged prompts 38, 34, 32).
+  // their rows take (two sets of inputs in turn; at least 2048, 4096, 8192 workgroups: four prompts of 8192 rows 172, 164, 155 us; 64 ragged
+  // prompts into 8 bits 38, 33, 31; four of 4096 fp32 rows 134, 131, 125; rows and move of 128 trees 21 all).
   int rows = ROPE_ROWS;
   while (rows > 1 && ((int64_t)Bt * ((a.T + rows - 1) / rows) * groups < 8192 || rows / 2 >= a.T)) rows /= 2;
   a.rows = rows;

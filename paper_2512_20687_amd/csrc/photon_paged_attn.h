@@ -19,7 +19,7 @@
 // What bounds it.  Up to 32 rows the entries, once streams fill the chip: 256 x 16 ragged streams of up to 2048 entries of 64 (fp32 rows, bf16
 // pages, 1139 MB) 200 us, 5.7 TB/s; 8 x 4 streams of 32749 entries of 128 under 8 heads (537 MB) 101 us, 5.3 TB/s with the merge.  Few and
 // short streams take the chain of one: counts, page, entries, two products, the waves' and the splits' merges (16 streams of 2048 fp32
-// entries, 16.8 MB: 12.0 us in two launches, of which the merge is 3).
+// entries, 16.8 MB: 11.2 us in two launches, of which the merge is 3).
 //
 // Precision.  Products of bf16 and E4M3 entries (which bf16 holds exactly) run on the bf16 matrix cores.  fp32 queries enter as three
 // bf16 parts and so do weights, whatever the rows are: all of their 24 bits.
@@ -58,14 +58,14 @@ struct PagedAttnArgs {
 // workgroups of 32 rows at once (512: two a unit), these win whatever the rows: all four waves go along the entries.  From there on entries are to
 // be read fewer times: by workgroups of 64 rows, or the wide kernel's of 128 and 256, where rows and pages are bf16.  Microseconds, bf16
 // rows (32-row workgroups / 64-row ones / wide):
-//   84 rows, 16 x 8 ragged streams of up to 3000 entries of 128    E4M3 pages 39 / 63     bf16 pages 50 / - / 62
-//   128 rows, 8 streams of 3000                                    E4M3 18 / 24           bf16 20 / - / 31
-//   512 rows, 4 x 8 streams of 3000                                E4M3 55 / 66           bf16 72 / - / 71
-//   48 rows, 64 x 8 ragged streams of up to 1000                   E4M3 41 / 34           bf16 56 / 44
-//   512 rows, 32 x 8 streams of 4096                               E4M3 509 / 484         bf16 - / - / 395
-// The wide kernel's eight waves instead of four for up to 128 rows cost ragged streams dear (1024 of up to 1000 entries of 32: 71 us, 50) and
-// gain 2 us in 36 at best.  24 rows in two workgroups of one tile: 20.4 us for 32 streams of 3000 (in one of two tiles 21.3), but 110 for 256 of
-// 4096 (98).
+//   84 rows, 16 x 8 ragged streams of up to 3000 entries of 128    E4M3 pages 45 / 67     bf16 pages 50 / 71 / 71
+//   128 rows, 8 streams of 3000                                    E4M3 19 / 25           bf16 21 / 24 / 34
+//   512 rows, 4 x 8 streams of 3000                                E4M3 65 / 72           bf16 73 / 76 / 76
+//   48 rows, 64 x 8 ragged streams of up to 1000                   E4M3 44 / 38           bf16 56 / 45 / 61
+//   512 rows, 32 x 8 streams of 4096                               E4M3 560 / 534         bf16 676 / 643 / 467
+// The wide kernel's eight waves instead of four for up to 128 rows cost ragged streams dear (1024 of up to 1000 entries of 32: 80 us, 57) and
+// gain nothing elsewhere (80 rows, 208 streams of 8000 of 52: 191 both).  24 rows in two workgroups of one tile: 19.8 us for 32 streams of 3000
+// (in one of two tiles 21.4), but 107 for 256 of 4096 (99).
 struct PagedTile {
   int tiles, waves;
   bool wide;                                   // photon_paged_attn_wide.h's
@@ -379,9 +379,10 @@ template <typename KV, typename T, int NB, int R> struct PagedRows {
   }
 };
 
-// Score products are used behind a branch, where this compiler (clang 22 of ROCm 7.2) does not keep the distance that a matrix
-// instruction's result needs on the path that skips the branch's body: entries 4 g + 3 of a step were read too early.  The distance, 19
-// instructions for the longest product here, is kept by hand: results pass through this before anything reads them.
+// Products are used behind a branch.  Where this compiler (clang 22 of ROCm 7.2) keeps their sums in accumulation registers, it reads them
+// (v_accvgpr_read) without the distance that a matrix instruction's result needs on the path that skips the branch's body: entries 4 g + 3
+// of a step were read too early.  The distance, 19 instructions for the longest product here, is kept by hand: results pass through this
+// before anything reads them.
 template <int R, int N> __device__ __forceinline__ void settle(f32x4_t (&d)[R][N]) {
 #pragma unroll
   for (int r = 0; r < R; ++r)
@@ -536,7 +537,7 @@ template <typename Each> __device__ __forceinline__ void weighted_sum(float (&o)
 // R row tiles a wave, RW waves side by side over rows; the KW waves of the same rows deal the steps among themselves.  Fewer waves lose even
 // where streams are many (256 x 16 ragged streams of up to 2048 entries of 64 fp32-row bf16 pages: 206 us, 215 with two waves, 231 with one).
 // Two waves a SIMD are asked for wherever their registers suffice: left to itself, the compiler moves sums to accumulation registers and back
-// and then fits one (13 nodes over E4M3 pages, 1024 streams of up to 1000 entries: 21.3 us, now 17.8; 512 rows over fp32 pages, 256 streams of
+// and then fits one (13 nodes over E4M3 pages, 1024 streams of up to 1000 entries: 21.3 us, now 17.6; 512 rows over fp32 pages, 256 streams of
 // 4096: 1439 us, now 1306).  Two tiles of 128 elements with fp32 rows or pages spill 130 registers and more at two waves (512 rows, 32
 // streams of 2000: 84 us, 54 at one).
 constexpr bool paged_two_waves(int d_p, int tiles, bool f32) { return !(d_p == 128 && tiles == 2 && f32); }
@@ -802,6 +803,7 @@ __global__ __launch_bounds__(PAGED_WAVES * 64, (paged_least_waves<KV, T, NB, R>(
 
 // The splits' results of a row.  DP / 4 lanes hold a row's elements; with many splits a workgroup's SIDE groups of lanes take every
 // SIDE-th one, and their results are put together in order (16 streams of 512 entries in 64 splits: 12 us in all, 24 with one group).
+// References and sums of all splits are read by every lane in either case.
 template <typename T, int NB, int SIDE> __global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a) {
   constexpr int DP = 32 * NB, LANES = DP / 4, ROWS = 256 / (LANES * SIDE);
   __shared__ __align__(16) float part[SIDE > 1 ? 256 * 4 : 4];

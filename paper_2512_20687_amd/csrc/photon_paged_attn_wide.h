@@ -3,8 +3,8 @@
 // The mathematics is photon_paged_attn.h's.  With more than 64 rows and many streams the matrix cores and the softmax bound it, not the entries: a workgroup
 // of WAVES waves of 32 rows stages 64 entries of K and V at a time in LDS (K in two buffers, V in three, loads straight to LDS while the
 // other buffers are worked on, one barrier per stage), so that entries are read once for all its rows.  Measured: 64 nodes under 4 heads,
-// 16 x 8 streams of 4096 entries of 128 121 to 127 us; 2048 rows, 16 streams of 8191 entries 191 us, 700 TFLOP/s of the definition's products, 1040
-// with the weights' second part counted.  Matrix cores are busy for 49 % of the cycles, vector units for 47 %.
+// 16 x 8 streams of 4096 entries of 128 139 to 145 us; 2048 rows, 16 streams of 8191 entries 230 us, 580 TFLOP/s of the definition's products, 1160
+// with the weights' second and third parts counted.  Matrix cores are busy for 54 % of the cycles, vector units for 52 %.
 //   K     16-byte chunks of a row are permuted by row, so that the 16 rows of an operand lie in different banks
 //   V     pairs of chunks likewise; ds_read_b64_tr_b16 hands a lane four entries of one element, as the contraction over entries takes
 //         them: the interleaving of the register kernel is the LDS's work here
