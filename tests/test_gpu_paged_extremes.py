@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paged_plain as plain
-from test_gpu_paged_attn import KV, check, i32
+from test_gpu_paged_attn import BAD_PAGE, KV, check, filled, i32, i64, trees
 from test_gpu_paged_wide import Many
 from util import require_gpu
 
@@ -194,3 +194,44 @@ def test_a_scale_at_the_end_of_fp32(ph, rows, kv, T):
     q[:, 1, 0] = 0.0
     out, given, pools, table = run(ph, rows, kv, q, k, v, 1, scale=3e38)
     check(out, given, pools, table, [n], [T], D_H, scale=float(np.float32(3e38)))
+
+
+@pytest.mark.parametrize("rows,kv", TYPES + [(torch.bfloat16, "e4m3"), (torch.float32, "e4m3")])
+@pytest.mark.parametrize("T,H,H_kv", [(1, 2, 2), (1, 10, 1), (12, 4, 2), (40, 2, 1)])
+def test_infinities_in_pages_trees_and_heads(ph, rows, kv, T, H, H_kv):
+    """Several sequences and K/V heads, pages that are not there, a tree: what a row sees, of its own head, decides.  Unused places hold NaN."""
+    rng = np.random.default_rng(10 * T + H)
+    lengths = [170 + T, 90 + T, T]
+    table, n_pages = plain.table_of(rng, lengths, P)
+    pools = [filled(rng, n_pages, H_kv, D_H, P, kv, table, lengths) for _ in range(2)]
+    for p in pools:
+        p[table[0, 1]] = 255 if kv == "e4m3" else float("nan")                  # the page that goes
+    wrong = table.copy()
+    wrong[0, 1], wrong[1, 1] = n_pages + 3, -7
+    e4m3 = kv == "e4m3"
+    for b, e, h, d, x in ((0, 3, 0, 1, "inf"), (0, 100, 0, 5, "-inf"), (0, 101, H_kv - 1, 5, "inf"), (0, 160, 0, 63, "nan"), (0, 169 + T, 0, 8, "inf"), (1, 10, H_kv - 1, 9, "-inf"),
+                          (1, 70, 0, 20, "inf"), (1, 89 + (T + 1) // 2, 0, 21, "-inf"), (2, T - 1, 0, 40, "inf"), (2, 0, H_kv - 1, 41, "nan")):
+        pools[1][table[b, e // P], h, e % P, d] = 255 if e4m3 else float(x)
+    masks = trees(rng, 3, T) if T > 1 else None
+    cache = ph.PagedCache(pools[0].cuda(), pools[1].cuda(), i32(wrong), D_H)
+    q = torch.from_numpy(rng.standard_normal((3, T, H, D_H)).astype(np.float32)).to(rows)
+    values = [plain.values(p) for p in pools]
+    for splits in (1, 3):
+        out, status = torch.empty_like(q, device="cuda"), i32([0])
+        ws = torch.empty(ph.photon_paged_attn_workspace_bytes(cache, 3, T, H, None, splits) + 16, dtype=torch.uint8, device="cuda")
+        ph.photon_paged_attn(q.cuda(), cache, i32(lengths), out, tree=i64(masks), n_splits=splits, workspace=ws, status=status)
+        assert int(status) == BAD_PAGE
+        got = out.float().cpu().numpy().astype(np.float64)
+        for b, n in enumerate(lengths):
+            ks, vs = (plain.entries(p, table[b], n, D_H) for p in values)
+            there = np.array([0 <= wrong[b, e // P] < n_pages for e in range(n)])
+            for t in range(T):
+                see = plain.seen(n, T, t, None if masks is None else masks[b, t]) & there
+                x = q[b, t].float().numpy()
+                for h in range(H):
+                    kk, vv = (a[h // (H // H_kv)][None] for a in (ks, vs))
+                    ref, size = with_unbounded(kk, vv, see, x[h : h + 1], D_H ** -0.5)
+                    fine = np.isfinite(ref[0])
+                    np.testing.assert_array_equal(np.where(fine, 0.0, got[b, t, h]), np.where(fine, 0.0, ref[0]), err_msg=str((splits, b, t, h)))
+                    bound = 1e-5 * size.max() if rows == torch.float32 else 2.0 ** -8 * np.abs(ref[0]) + 2.0 ** -15 * size[0]
+                    assert (np.abs(got[b, t, h][fine] - ref[0][fine]) <= np.broadcast_to(bound, ref[0].shape)[fine]).all(), (splits, b, t, h)
