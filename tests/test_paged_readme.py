@@ -34,6 +34,9 @@ def names(device):
 
 def test_its_pools_have_the_heads_they_are_for():
     import paper_2512_20687_amd as ph
+    if not os.path.exists(ph.lib_path()):
+        from paper_2512_20687_amd import build
+        build.build(verbose=False)
     on_cpu = types.SimpleNamespace(PagedCache=ph.PagedCache, paged_pool=lambda *a, **k: ph.paged_pool(*a, device="cpu", **k))
     scope = dict(names("cpu"), ph=on_cpu)
     line = example()[0]
